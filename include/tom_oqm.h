@@ -325,6 +325,123 @@ tom_status_t tom_oqm_retrieve_noalloc(const tom_oqm_t* h, int32_t layer0, int32_
 /* Size in bytes of the static scratch array tom_oqm_retrieve_noalloc works in. */
 size_t tom_oqm_static_scratch_bytes(void);
 
+/* ---- beside the memory: positions, attention over it, its groups ---------- */
+
+/* A tensor of [heads][rows][channels] (in whatever order heads and rows lie): element (h, r, c) at
+ * data + h * head_stride + r * row_stride + c, strides in elements and >= 0, channels contiguous. */
+typedef struct {
+    void* data;          /* device                                  */
+    int64_t head_stride; /* elements                                */
+    int64_t row_stride;
+    int32_t heads, rows, channels;
+    int32_t dtype;       /* tom_dtype_t                             */
+} tom_oqm_view_t;
+
+typedef enum {
+    TOM_ROTARY_HALF = 0, /* channel i of a head turns with channel i + rotary_dim / 2 */
+    TOM_ROTARY_PAIRS = 1 /* channel 2i turns with channel 2i + 1                      */
+} tom_rotary_layout_t;
+
+/* How the angles change where a stream is longer than the model was trained for.  f_i below is the
+ * plain frequency base^(-2i / rotary_dim) of pair i, in radians a position. */
+typedef enum {
+    TOM_ROTARY_PLAIN = 0,    /* f_i                                                                     */
+    TOM_ROTARY_LINEAR = 1,   /* f_i / factor                                                            */
+    TOM_ROTARY_BASE = 2,     /* base * factor^(rotary_dim / (rotary_dim - 2)) in base's place           */
+    TOM_ROTARY_BY_PARTS = 3, /* pairs that turn 32 times or more within original_length stay f_i, those that turn
+                                once or less get f_i / factor, by the pair's number in between; the turned
+                                channels are multiplied by 0.1 ln(factor) + 1                           */
+    TOM_ROTARY_BY_WAVELENGTH = 4 /* wavelengths up to original_length / 4 stay f_i, those from original_length
+                                up get f_i / factor, by the turns within original_length in between     */
+} tom_rotary_scaling_t;
+
+typedef struct {
+    int32_t rotary_dim;      /* channels of a head that turn: even, 2 .. 2048 (>= 4 with TOM_ROTARY_BASE) */
+    int32_t layout;          /* tom_rotary_layout_t                                                       */
+    int32_t scaling;         /* tom_rotary_scaling_t                                                      */
+    int32_t original_length; /* >= 1; used by the last two scalings                                       */
+    double base;             /* > 1                                                                       */
+    double factor;           /* >= 1                                                                      */
+} tom_oqm_rotary_t;
+
+/* Fills turns[rotary_dim / 2] (host) with what a position turns each pair by, in whole turns (radians / 2 pi),
+ * and *amplitude with the factor on the turned channels.  The caller keeps the array on the device for
+ * tom_oqm_rotate.  Host only. */
+tom_status_t tom_oqm_rotary_turns(const tom_oqm_rotary_t* rotary, double* turns, float* amplitude);
+
+/*
+ * Turns the queries and keys of new tokens to their positions, after a norm of every head where weights are given,
+ * and copies their values, in one launch: what stands between a projection and the cache.
+ *   x' = x * w / sqrt(mean(x^2) + norm_eps)                    with a norm, else x' = x
+ *   (a, b) -> amplitude * (a cos t - b sin t, b cos t + a sin t)     for every pair, t = position * turns
+ * Channels from rotary_dim up are not turned (they are normed).  Angles are reduced in float64, everything else is
+ * float32, rounded once to the outputs' type.
+ *   turns_device      what tom_oqm_rotary_turns gave, on the device; `rotary` and `amplitude` likewise
+ *   positions_device  int64, one for each row; any value
+ *   q, k, v           inputs [heads][tokens][channels], each with its output of the same shape; each pair may be NULL
+ *                     (v needs no position).  All of one dtype, one number of rows and of channels (rotary_dim .. 2048).
+ *                     An output may be its own input, with the same strides; otherwise outputs overlap nothing.
+ *   q_norm, k_norm    device, [channels] of the same dtype, or NULL
+ * Every multiple of the element size is a valid address and stride; multiples of 16 bytes are fastest.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 1 rows times heads), HIP.  No rows: a no-op.
+ */
+tom_status_t tom_oqm_rotate(const tom_oqm_rotary_t* rotary, const double* turns_device, float amplitude,
+                            const int64_t* positions_device, const tom_oqm_view_t* q, const tom_oqm_view_t* q_out,
+                            const tom_oqm_view_t* k, const tom_oqm_view_t* k_out, const tom_oqm_view_t* v,
+                            const tom_oqm_view_t* v_out, const void* q_norm_device, const void* k_norm_device,
+                            float norm_eps, void* hip_stream);
+
+/* Bytes of device workspace tom_oqm_attend needs for t_q new tokens over `rows` rows in all (front + k_eff * G +
+ * recent; it grows with rows, so those of the longest call of the same t_q will do).  0: none is needed, or arguments
+ * that call would refuse. */
+size_t tom_oqm_attend_workspace_bytes(const tom_oqm_t* h, int32_t t_q, int64_t rows);
+
+/*
+ * Attention of t_q new tokens of one layer over rows in front (system tokens, or an active buffer), stored groups as
+ * they are stored, and recent rows, in one softmax, without a reconstructed copy of the groups:
+ *   out = sum_j p_j v_j,   p = softmax_j(w_j),   w_j = scale <q, k_j>, or softcap * tanh(scale <q, k_j> / softcap)
+ * over the front rows, the G rows code * s + m of each group, and the recent rows.  Query head i reads KV head
+ * i / (H_q / H_k).  Codes enter the products as they are and (s, m) in float32 where quant-groups have 32 channels or
+ * more; other forms split what they reconstruct into two 16-bit parts.  Scores, softmax and sums are float32.
+ *   q, out     [H_q][t_q][d] of cfg.out_dtype, any strides that are multiples of 16 bytes
+ *   idx        device int32 [k_eff]: the groups, in any order, each as often as it stands there; an index outside [0, T)
+ *              is a hole that nobody sees.  NULL: the groups 0 .. k_eff - 1, k_eff <= T
+ *   front_k .. recent_v  [H_k][rows][d] of cfg.out_dtype, both of a pair or neither (NULL or no rows)
+ *   causal     non-zero: the last t_q recent rows are the new tokens' own, and token t sees the recent rows j with
+ *              j <= t + recent - t_q (so none where that is negative); otherwise every token sees all
+ *   softcap    0: none
+ *   lse        device float32 [H_q][t_q] or NULL: the natural logarithm of the sum of exp(w_j).  Where a token sees
+ *              nothing its output is 0 and its lse -inf.
+ *   workspace  device, 16-byte aligned, tom_oqm_attend_workspace_bytes(h, t_q, rows) bytes
+ * Errors: INVALID_ARG, NOT_BOUND, UNSUPPORTED (head_dim above 256, more than 2^20 tokens, or 2^31 - 1 rows), HIP.
+ * t_q == 0 is a no-op.
+ */
+tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_view_t* q, const tom_oqm_view_t* out,
+                            const int32_t* idx_device, int32_t k_eff, const tom_oqm_view_t* front_k,
+                            const tom_oqm_view_t* front_v, const tom_oqm_view_t* recent_k,
+                            const tom_oqm_view_t* recent_v, int32_t causal, float scale, float softcap,
+                            float* lse_device, void* workspace_device, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Drops all stored groups but n: group idx[i] moves to slot i (codes, pairs and summary keys of every layer), in
+ * place and without a workspace, and the memory then holds n groups.
+ *   idx   device int32 [n], strictly ascending.  (Any other order leaves unspecified codes, pairs and keys.)  An index
+ *         outside [0, T) leaves slot i as it is.
+ * Errors: INVALID_ARG (n outside [0, T], NULL), NOT_BOUND, HIP.
+ */
+tom_status_t tom_oqm_keep_groups(tom_oqm_t* h, const int32_t* idx_device, int32_t n, void* hip_stream);
+
+/*
+ * Appends n groups of one memory to another (or to itself): group idx[i] of `from` goes to slot T + i of `to`, T =
+ * tom_oqm_num_groups(to), which then holds T + n.
+ *   idx   device int32 [n], in any order, repeats allowed; an index outside `from` leaves its slot as it is.
+ * The two agree in layers, KV heads, head_dim, group_tokens, bits, qaxis, qgroup (HEAD_DIM axis) and meta_dtype.
+ * Errors: INVALID_ARG (they do not, n < 0, NULL, storage that overlaps without being the same memory's), CAPACITY,
+ * NOT_BOUND, HIP.
+ */
+tom_status_t tom_oqm_copy_groups(tom_oqm_t* to, const tom_oqm_t* from, const int32_t* idx_device, int32_t n,
+                                 void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -12,14 +12,15 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <cmath>
 #include <cstdint>
 
 #include "tom_oqm.h"
 
 namespace {
 
-PyObject *g_raise, *g_int32, *g_int64, *g_void_p, *g_is_initialized, *g_get_device, *g_get_raw_stream, *g_slow_stream;
-PyObject *s_is_cuda, *s_data_ptr, *s_numel, *s_element_size, *s_stride, *s_cuda_stream;
+PyObject *g_raise, *g_int32, *g_int64, *g_void_p, *g_is_initialized, *g_get_device, *g_get_raw_stream, *g_slow_stream, *g_dtypes;
+PyObject *s_is_cuda, *s_data_ptr, *s_numel, *s_element_size, *s_stride, *s_cuda_stream, *s_shape, *s_dtype, *s_is_contiguous;
 
 // What ctypes does with c_int32 / c_int64: a Python int is truncated; `slow`, a callable registered by oqm.py, makes
 // one of whatever else ctypes takes (__index__, its own integer objects) or raises its error.
@@ -321,12 +322,168 @@ PyObject* retrieve_noalloc(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return arity(n, 17) ? retrieve_with(a, false) : nullptr;
 }
 
-// The Python callables that the functions above need, in the order of the globals.
+// Codes of the dtypes that are not tom_dtype_t; oqm.py registers the same.
+constexpr int32_t kInt32 = 100, kInt64 = 101;
+
+// The dtype code of a tensor, out of the dictionary that oqm.py registered.
+bool to_dtype(PyObject* o, int32_t& out) {
+    PyObject* t = PyObject_GetAttr(o, s_dtype);
+    if (!t) return false;
+    PyObject* code = PyDict_GetItemWithError(g_dtypes, t);  // borrowed
+    Py_DECREF(t);
+    if (!code) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_AssertionError, "tensor of another dtype expected");
+        return false;
+    }
+    return to_i32(code, out);
+}
+
+bool fits_i32(int64_t v) { return v == (int32_t)v; }
+
+// A tensor on the device, of [heads][rows][channels] or (rows_first) [rows][heads][channels]; `given` is false for None.
+bool to_view(PyObject* o, bool rows_first, tom_oqm_view_t& v, bool& given) {
+    given = o != Py_None;
+    v = tom_oqm_view_t{};
+    if (!given) return true;
+    if (PyLong_Check(o)) {
+        PyErr_SetString(PyExc_AssertionError, "device tensor expected");
+        return false;
+    }
+    if (!to_ptr(o, v.data) || !to_dtype(o, v.dtype)) return false;
+    if (v.dtype == kInt32 || v.dtype == kInt64) {
+        PyErr_SetString(PyExc_AssertionError, "float32, bfloat16 or float16 tensor expected");
+        return false;
+    }
+    PyObject* shape = PyObject_GetAttr(o, s_shape);
+    if (!shape) return false;
+    PyObject* strides = strides_of(o);
+    bool ok = strides && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 3 && PyTuple_GET_SIZE(strides) == 3;
+    int64_t n[3] = {}, s[3] = {};
+    for (int i = 0; i < 3 && ok; ++i) ok = to_i64(PyTuple_GET_ITEM(shape, i), n[i]) && to_i64(PyTuple_GET_ITEM(strides, i), s[i]);
+    Py_XDECREF(strides);
+    Py_DECREF(shape);
+    ok = ok && fits_i32(n[0]) && fits_i32(n[1]) && fits_i32(n[2]) && (s[2] == 1 || n[2] == 1);
+    if (!ok) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_AssertionError, "tensor of three dimensions with a contiguous channel axis expected");
+        return false;
+    }
+    v.heads = (int32_t)n[rows_first ? 1 : 0];
+    v.rows = (int32_t)n[rows_first ? 0 : 1];
+    v.channels = (int32_t)n[2];
+    v.head_stride = s[rows_first ? 1 : 0];
+    v.row_stride = s[rows_first ? 0 : 1];
+    return true;
+}
+
+// None, a raw address, or a contiguous tensor of at least `want` elements of that dtype.
+bool to_array(PyObject* o, int64_t want, int32_t dtype, const char* what, void*& out) {
+    if (!to_ptr(o, out)) return false;
+    if (o == Py_None || PyLong_Check(o)) return true;
+    int64_t n;
+    int32_t own;
+    if (!method_i64(o, s_numel, n) || !to_dtype(o, own)) return false;
+    PyObject* flat = PyObject_CallMethodNoArgs(o, s_is_contiguous);
+    if (!flat) return false;
+    const int in_a_row = PyObject_IsTrue(flat);
+    Py_DECREF(flat);
+    if (in_a_row < 0) return false;
+    if (own == dtype && n >= want && in_a_row) return true;
+    PyErr_Format(PyExc_AssertionError, "%s: a contiguous tensor of at least %lld elements of the right dtype expected", what, (long long)want);
+    return false;
+}
+
+// rotary (address of a tom_oqm_rotary_t), turns, amplitude, positions, q, q_out, k, k_out, v, v_out, q_norm, k_norm, norm_eps, stream
+PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void *rotary, *turns, *positions, *norms[2], *stream;
+    tom_oqm_view_t view[6];
+    bool given[6];
+    if (!arity(n, 14) || !to_void_p(a[0], rotary) || !to_ptr(a[1], turns)) return nullptr;
+    const double amplitude = PyFloat_AsDouble(a[2]), eps = PyFloat_AsDouble(a[12]);
+    if (PyErr_Occurred()) return nullptr;
+    int32_t rows = 0;
+    for (int i = 0; i < 6; ++i) {
+        if (!to_view(a[4 + i], true, view[i], given[i])) return nullptr;
+        if (given[i]) rows = view[i].rows;
+    }
+    if (!to_array(a[3], rows, kInt64, "positions", positions)) return nullptr;
+    for (int i = 0; i < 2; ++i)
+        if (!to_array(a[10 + i], view[2 * i].channels, view[2 * i].dtype, "norm weights", norms[i])) return nullptr;
+    if (!to_stream(a[13], stream)) return nullptr;
+    const tom_oqm_view_t* p[6];
+    for (int i = 0; i < 6; ++i) p[i] = given[i] ? &view[i] : nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = tom_oqm_rotate(static_cast<const tom_oqm_rotary_t*>(rotary), static_cast<const double*>(turns), (float)amplitude,
+                        static_cast<const int64_t*>(positions), p[0], p[1], p[2], p[3], p[4], p[5], norms[0], norms[1], (float)eps, stream);
+    Py_END_ALLOW_THREADS
+    return finish_none(st);
+}
+
+// h, layer, q, out, idx, k_eff, front_k, front_v, recent_k, recent_v, causal, scale (None: channels^-0.5), softcap, lse, workspace, stream
+PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    tom_oqm_t* h;
+    int32_t layer, k_eff;
+    void *idx, *lse, *ws, *stream;
+    size_t ws_bytes;
+    tom_oqm_view_t view[6];
+    bool given[6];
+    static const int at[6] = {2, 3, 6, 7, 8, 9};
+    if (!arity(n, 16) || !to_handle(a[0], h) || !to_i32(a[1], layer) || !to_i32(a[5], k_eff) || !to_array(a[4], k_eff, kInt32, "idx", idx)) return nullptr;
+    for (int i = 0; i < 6; ++i)
+        if (!to_view(a[at[i]], false, view[i], given[i])) return nullptr;
+    const int causal = PyObject_IsTrue(a[10]);
+    if (causal < 0) return nullptr;
+    double scale = 0.0;
+    if (a[11] != Py_None) scale = PyFloat_AsDouble(a[11]);
+    else if (given[0] && view[0].channels > 0) scale = 1.0 / std::sqrt((double)view[0].channels);
+    const double softcap = PyFloat_AsDouble(a[12]);
+    if (PyErr_Occurred() || !to_array(a[13], (int64_t)view[0].heads * view[0].rows, TOM_F32, "lse", lse) || !to_workspace(a[14], ws, ws_bytes) ||
+        !to_stream(a[15], stream))
+        return nullptr;
+    const tom_oqm_view_t* p[6];
+    for (int i = 0; i < 6; ++i) p[i] = given[i] ? &view[i] : nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = tom_oqm_attend(h, layer, p[0], p[1], static_cast<const int32_t*>(idx), k_eff, p[2], p[3], p[4], p[5], causal, (float)scale, (float)softcap,
+                        static_cast<float*>(lse), ws, ws_bytes, stream);
+    Py_END_ALLOW_THREADS
+    return finish_none(st);
+}
+
+// h, idx, n, stream
+PyObject* keep_groups(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    tom_oqm_t* h;
+    void *idx, *stream;
+    int32_t count;
+    if (!arity(n, 4) || !to_handle(a[0], h) || !to_i32(a[2], count) || !to_array(a[1], count, kInt32, "idx", idx) || !to_stream(a[3], stream)) return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = tom_oqm_keep_groups(h, static_cast<const int32_t*>(idx), count, stream);
+    Py_END_ALLOW_THREADS
+    return finish_none(st);
+}
+
+// to, from, idx, n, stream
+PyObject* copy_groups(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    tom_oqm_t *to, *from;
+    void *idx, *stream;
+    int32_t count;
+    if (!arity(n, 5) || !to_handle(a[0], to) || !to_handle(a[1], from) || !to_i32(a[3], count) || !to_array(a[2], count, kInt32, "idx", idx) ||
+        !to_stream(a[4], stream))
+        return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = tom_oqm_copy_groups(to, from, static_cast<const int32_t*>(idx), count, stream);
+    Py_END_ALLOW_THREADS
+    return finish_none(st);
+}
+
+// The Python callables that the functions above need, in the order of the globals, and the dictionary of dtypes.
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!arity(n, 8)) return nullptr;
-    PyObject** const slots[8] = {&g_raise, &g_int32, &g_int64, &g_void_p, &g_is_initialized, &g_get_device, &g_get_raw_stream,
-                                 &g_slow_stream};
-    for (int i = 0; i < 8; ++i) {
+    if (!arity(n, 9)) return nullptr;
+    PyObject** const slots[9] = {&g_raise, &g_int32, &g_int64, &g_void_p, &g_is_initialized, &g_get_device, &g_get_raw_stream,
+                                 &g_slow_stream, &g_dtypes};
+    for (int i = 0; i < 9; ++i) {
         Py_INCREF(a[i]);
         Py_XSETREF(*slots[i], a[i]);
     }
@@ -336,6 +493,7 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(setup), FAST(set_num_groups), FAST(quantize_append), FAST(score_groups), FAST(topk),
                          FAST(dequant_gather), FAST(assemble_active), FAST(retrieve), FAST(retrieve_noalloc),
+                         FAST(rotate), FAST(attend), FAST(keep_groups), FAST(copy_groups),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_oqm_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -348,6 +506,9 @@ PyMODINIT_FUNC PyInit__oqm_binding(void) {
     s_element_size = PyUnicode_InternFromString("element_size");
     s_stride = PyUnicode_InternFromString("stride");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-    if (!s_is_cuda || !s_data_ptr || !s_numel || !s_element_size || !s_stride || !s_cuda_stream) return nullptr;
+    s_shape = PyUnicode_InternFromString("shape");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    if (!s_is_cuda || !s_data_ptr || !s_numel || !s_element_size || !s_stride || !s_cuda_stream || !s_shape || !s_dtype || !s_is_contiguous) return nullptr;
     return PyModule_Create(&module);
 }

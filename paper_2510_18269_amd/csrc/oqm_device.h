@@ -315,6 +315,10 @@ template <typename T> struct elem_bytes;
 template <> struct elem_bytes<In_f32> { static constexpr int value = 4; };
 template <> struct elem_bytes<In_bf16> { static constexpr int value = 2; };
 template <> struct elem_bytes<In_f16> { static constexpr int value = 2; };
+template <typename T> struct Element;
+template <> struct Element<In_f32> { typedef float type; };
+template <> struct Element<In_bf16> { typedef __bf16 type; };
+template <> struct Element<In_f16> { typedef _Float16 type; };
 
 // ---- storing consecutive float32 values, narrowed round-to-nearest-even ---
 __device__ __forceinline__ u32x4 pack_items(In_bf16, const float (&x)[8]) {

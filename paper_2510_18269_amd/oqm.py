@@ -24,6 +24,8 @@ TOM_QAXIS_HEAD_DIM, TOM_QAXIS_TOKENS = 0, 1
 TOM_SIM_DOT, TOM_SIM_COSINE = 0, 1
 TOM_ORDER_INDEX_ASC, TOM_ORDER_SCORE_DESC = 0, 1
 TOM_SCORE_AUTO, TOM_SCORE_MEAN_QUERY, TOM_SCORE_TOKEN_GEMM = 0, 1, 2
+TOM_ROTARY_HALF, TOM_ROTARY_PAIRS = 0, 1
+TOM_ROTARY_PLAIN, TOM_ROTARY_LINEAR, TOM_ROTARY_BASE, TOM_ROTARY_BY_PARTS, TOM_ROTARY_BY_WAVELENGTH = range(5)
 
 _STATUS_NAMES = ["TOM_OK", "TOM_ERR_INVALID_ARG", "TOM_ERR_CAPACITY", "TOM_ERR_UNSUPPORTED",
                  "TOM_ERR_NOT_BOUND", "TOM_ERR_HIP"]
@@ -33,7 +35,8 @@ EXPORTS = ["tom_oqm_query_sizes", "tom_oqm_create", "tom_oqm_bind", "tom_oqm_res
            "tom_oqm_k_from_budget", "tom_oqm_quantize_append", "tom_oqm_score_workspace_bytes",
            "tom_oqm_score_groups", "tom_oqm_topk", "tom_oqm_dequant_gather",
            "tom_oqm_assemble_active", "tom_oqm_retrieve", "tom_oqm_retrieve_noalloc",
-           "tom_oqm_static_scratch_bytes"]
+           "tom_oqm_static_scratch_bytes", "tom_oqm_rotary_turns", "tom_oqm_rotate",
+           "tom_oqm_attend_workspace_bytes", "tom_oqm_attend", "tom_oqm_keep_groups", "tom_oqm_copy_groups"]
 
 
 class TomError(RuntimeError):
@@ -50,6 +53,16 @@ class tom_oqm_config_t(C.Structure):
 
 class tom_oqm_sizes_t(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in ("codes", "meta", "keys")]
+
+
+class tom_oqm_rotary_t(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rotary_dim", "layout", "scaling", "original_length")] + \
+               [(n, C.c_double) for n in ("base", "factor")]
+
+
+class tom_oqm_view_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("head_stride", C.c_int64), ("row_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("heads", "rows", "channels", "dtype")]
 
 
 def _load():
@@ -86,10 +99,18 @@ def _load():
                                            vp, vp, vp, C.POINTER(i32), vp]
     L.tom_oqm_static_scratch_bytes.argtypes = []
     L.tom_oqm_static_scratch_bytes.restype = C.c_size_t
+    viewp, f32 = C.POINTER(tom_oqm_view_t), C.c_float
+    L.tom_oqm_rotary_turns.argtypes = [C.POINTER(tom_oqm_rotary_t), C.POINTER(C.c_double), C.POINTER(f32)]
+    L.tom_oqm_rotate.argtypes = [C.POINTER(tom_oqm_rotary_t), vp, f32, vp] + [viewp] * 6 + [vp, vp, f32, vp]
+    L.tom_oqm_attend_workspace_bytes.argtypes = [vp, i32, i64]
+    L.tom_oqm_attend_workspace_bytes.restype = C.c_size_t
+    L.tom_oqm_attend.argtypes = [vp, i32, viewp, viewp, vp, i32] + [viewp] * 4 + [i32, f32, f32, vp, vp, C.c_size_t, vp]
+    L.tom_oqm_keep_groups.argtypes = [vp, vp, i32, vp]
+    L.tom_oqm_copy_groups.argtypes = [vp, vp, vp, i32, vp]
     for name in EXPORTS:
         fn = getattr(L, name)
         if name not in ("tom_oqm_destroy", "tom_last_error", "tom_oqm_score_workspace_bytes",
-                        "tom_oqm_static_scratch_bytes"):
+                        "tom_oqm_static_scratch_bytes", "tom_oqm_attend_workspace_bytes"):
             fn.restype = i32
     return L
 
@@ -159,7 +180,8 @@ def _no_device(*_) -> int:
 
 _native.setup(_raise, _integer(C.c_int32), _integer(C.c_int64), _void_p, torch.cuda.is_initialized,
               getattr(torch._C, "_cuda_getDevice", _no_device),
-              getattr(torch._C, "_cuda_getCurrentRawStream", _no_device), _first_stream)
+              getattr(torch._C, "_cuda_getCurrentRawStream", _no_device), _first_stream,
+              {**_DTYPE_OF_TORCH, torch.int32: 100, torch.int64: 101})
 
 
 def tom_oqm_query_sizes(cfg: tom_oqm_config_t) -> tom_oqm_sizes_t:
@@ -263,6 +285,63 @@ def tom_oqm_retrieve_noalloc(h: int, layer0: int, n_layers: int, q, t_q: int, k:
 
 def tom_oqm_static_scratch_bytes() -> int:
     return lib.tom_oqm_static_scratch_bytes()
+
+
+def tom_oqm_rotary_turns(rotary: tom_oqm_rotary_t) -> tuple[list[float], float]:
+    """What a position turns each pair of channels by, in whole turns, and the factor on the turned channels."""
+    turns, amplitude = (C.c_double * max(1, rotary.rotary_dim // 2))(), C.c_float()
+    _check(lib.tom_oqm_rotary_turns(C.byref(rotary), turns, C.byref(amplitude)))
+    return list(turns), amplitude.value
+
+
+@dataclass
+class Rotary:
+    """A rotary embedding, and its angles on the device (what a program makes once and keeps)."""
+    config: tom_oqm_rotary_t
+    turns: torch.Tensor    # float64 [rotary_dim / 2]: whole turns a position
+    amplitude: float
+
+    def __post_init__(self):
+        self._address = C.addressof(self.config)
+
+    @staticmethod
+    def create(rotary_dim: int, layout: int = TOM_ROTARY_HALF, base: float = 10000.0, scaling: int = TOM_ROTARY_PLAIN,
+               factor: float = 1.0, original_length: int = 1, device="cuda") -> "Rotary":
+        config = tom_oqm_rotary_t(rotary_dim, layout, scaling, original_length, base, factor)
+        turns, amplitude = tom_oqm_rotary_turns(config)
+        return Rotary(config, torch.tensor(turns, dtype=torch.float64, device=device), amplitude)
+
+
+def tom_oqm_rotate(rotary: Rotary, positions, q=None, q_out=None, k=None, k_out=None, v=None, v_out=None, q_norm=None,
+                   k_norm=None, norm_eps: float = 1e-6, stream=None) -> None:
+    """Queries, keys and values [tokens][heads][channels] of any strides: q and k normed where weights are given and
+    turned to `positions` (int64), v copied, each into its output (which may be the input itself)."""
+    _native.rotate(rotary._address, rotary.turns, rotary.amplitude, positions, q, q_out, k, k_out, v, v_out, q_norm, k_norm,
+                   norm_eps, stream)
+
+
+def tom_oqm_attend_workspace_bytes(h: int, t_q: int, rows: int) -> int:
+    """`rows`: front + k_eff * G + recent of the longest call."""
+    return lib.tom_oqm_attend_workspace_bytes(h, t_q, rows)
+
+
+def tom_oqm_attend(h: int, layer: int, q, out, idx=None, k_eff: int = 0, front_k=None, front_v=None, recent_k=None,
+                   recent_v=None, causal: bool = True, scale: float | None = None, softcap: float = 0.0, lse=None,
+                   workspace=None, stream=None) -> None:
+    """q, out [H_q][t_q][d], rows [H_k][rows][d], of the memory's out_dtype and any strides that are multiples of 16
+    bytes.  scale None: d ** -0.5."""
+    _native.attend(h, layer, q, out, idx, k_eff, front_k, front_v, recent_k, recent_v, causal, scale, softcap, lse, workspace,
+                   stream)
+
+
+def tom_oqm_keep_groups(h: int, idx, n: int, stream=None) -> None:
+    """The groups idx[0 .. n), ascending (int32 on the device), move to the front; the others are dropped."""
+    _native.keep_groups(h, idx, n, stream)
+
+
+def tom_oqm_copy_groups(to: int, source: int, idx, n: int, stream=None) -> None:
+    """Groups idx[0 .. n) of `source` are appended to `to`."""
+    _native.copy_groups(to, source, idx, n, stream)
 
 
 # --------------------------------------------------------------------------- convenience
