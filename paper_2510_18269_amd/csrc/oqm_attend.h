@@ -61,6 +61,38 @@ struct AttendArgs {
     int32_t splits, row_blocks;
 };
 
-hipError_t launch_attend(const AttendArgs& a, int dtype, hipStream_t s);
+// The kernel a call takes: `rows` query rows of a KV head a workgroup (general: a wave).
+struct AttendForm {
+    bool folded;
+    int32_t rows;
+};
+// Folded: 16-bit rows of 64, 128 or 256 channels in quant-groups of 32 channels or more of one token, so that a step of the matrix
+// cores (32 channels of keys, 16 of values) lies in one group.
+inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
+    const bool folded = c.out_dtype != TOM_F32 && c.qaxis == TOM_QAXIS_HEAD_DIM && c.qgroup >= 32 &&
+                        (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256);
+    if (!folded) return {false, 16};
+    const int64_t rows = (int64_t)(c.n_q_heads / c.n_kv_heads) * t_q;
+    return {true, rows <= 16 ? 16 : rows <= 64 ? 64 : 128};
+}
+
+// Parts that the rows of a call are cut into, each with its own maximum and sum.  Never fewer where there are more rows: the
+// workspace of the longest call serves the others.
+inline int32_t attend_cuts(const tom_oqm_config_t& c, int32_t t_q, int64_t rows) {
+    const AttendForm f = attend_form(c, t_q);
+    const int64_t blocks = ((int64_t)(c.n_q_heads / c.n_kv_heads) * t_q + f.rows - 1) / f.rows * c.n_kv_heads;
+    int64_t target = 2048, least = 64;  // waves: two a SIMD
+    if (f.folded && f.rows == 16) target = 1024, least = 128;
+    else if (f.folded) target = 512, least = 256;
+    int64_t n = target / blocks;
+    if (n > (rows + least - 1) / least) n = (rows + least - 1) / least;
+    return n < 1 ? 1 : (int32_t)n;
+}
+
+hipError_t launch_attend(const AttendArgs& a, const AttendForm& form, int dtype, hipStream_t s);
+void start_attend_bf16_4bit(const AttendArgs& g, const AttendForm& form, hipStream_t s);
+void start_attend_bf16_2bit(const AttendArgs& g, const AttendForm& form, hipStream_t s);
+void start_attend_f16_4bit(const AttendArgs& g, const AttendForm& form, hipStream_t s);
+void start_attend_f16_2bit(const AttendArgs& g, const AttendForm& form, hipStream_t s);
 
 }  // namespace oqm

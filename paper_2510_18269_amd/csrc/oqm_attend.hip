@@ -5,99 +5,9 @@
 // One pass over the keys and values with the running maximum and sum of each query row.  The keys' product is taken transposed,
 // S^T = K Q^T on the matrix cores: a lane then holds, for one query row, the scores of the very tokens whose values it feeds as
 // the other operand of O^T = V^T P^T, so that the probabilities never leave their lane.
-#include "oqm_attend.h"
-#include "oqm_common.h"
-#include "oqm_device.h"
+#include "oqm_attend_device.h"
 
 namespace oqm {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kTile = 32;  // tokens
-
-__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// softcap * tanh(y) in units of log 2.  Near zero, where 1 - 2 / (1 + e^2y) cancels, the series.
-__device__ __forceinline__ float capped(float y, float cap_log2) {
-    const float z = y * y;
-    const float small = y * fmaf(z, fmaf(z, fmaf(z, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-    const float wide = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + exp2_of(2.0f * kLog2e * y)), 1.0f);
-    return cap_log2 * (z < 0.015625f ? small : wide);
-}
-
-// ---- operands: 8 consecutive k of a row of a 16 x 16 x 32 product (16-bit types), or 8 products of one k a lane (float32) ----
-template <typename T> struct Operand;
-template <> struct Operand<In_bf16> {
-    u32x4 w;
-};
-template <> struct Operand<In_f16> {
-    u32x4 w;
-};
-template <> struct Operand<In_f32> {
-    float x[8];
-};
-__device__ __forceinline__ f32x4 product(const Operand<In_bf16>& a, const Operand<In_bf16>& b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.w), __builtin_bit_cast(bf16x8, b.w), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 product(const Operand<In_f16>& a, const Operand<In_f16>& b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.w), __builtin_bit_cast(f16x8, b.w), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 product(const Operand<In_f32>& a, const Operand<In_f32>& b, f32x4 c) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i], b.x[i], c, 0, 0, 0);
-    return c;
-}
-// x = hi + lo + a rest of 2^-17 of it (bfloat16) or 2^-23 (binary16); float32 has no rest in hi.
-__device__ __forceinline__ void split(const float (&x)[8], Operand<In_bf16>& hi, Operand<In_bf16>& lo) {
-    hi.w = pack_items(In_bf16{}, x);
-    float r[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r[2 * i] = x[2 * i] - __uint_as_float(hi.w[i] << 16);
-        r[2 * i + 1] = x[2 * i + 1] - __uint_as_float(hi.w[i] & 0xffff0000u);
-    }
-    lo.w = pack_items(In_bf16{}, r);
-}
-__device__ __forceinline__ void split(const float (&x)[8], Operand<In_f16>& hi, Operand<In_f16>& lo) {
-    f16x8 h, l;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        h[i] = (_Float16)x[i];
-        l[i] = (_Float16)(x[i] - (float)h[i]);
-    }
-    hi.w = __builtin_bit_cast(u32x4, h);
-    lo.w = __builtin_bit_cast(u32x4, l);
-}
-__device__ __forceinline__ void split(const float (&x)[8], Operand<In_f32>& hi, Operand<In_f32>&) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) hi.x[i] = x[i];
-}
-
-// N (4 or 8) consecutive channels of a row in 32 bits.
-template <typename T, int N>
-__device__ __forceinline__ void load_row(const char* p, float* x) {
-    if constexpr (N == 8) {
-        Raw8<T> r;
-        load_raw(p, r);
-        float y[8];
-        widen(r, y);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = y[i];
-    } else if constexpr (elem_bytes<T>::value == 4) {
-        const f32x4 r = *reinterpret_cast<const f32x4*>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = r[i];
-    } else {
-        const u32x2 r = *reinterpret_cast<const u32x2*>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint16_t h = (uint16_t)(r[i / 2] >> (16 * (i % 2)));
-            if constexpr (__is_same(T, In_bf16)) x[i] = __uint_as_float((uint32_t)h << 16);
-            else x[i] = (float)__builtin_bit_cast(_Float16, h);
-        }
-    }
-}
 
 __device__ __forceinline__ f32x2 load_pair(const char* meta, int64_t i, bool bf16) {
     if (bf16) return widen_pair(reinterpret_cast<const uint32_t*>(meta)[i]);
@@ -384,19 +294,32 @@ __global__ __launch_bounds__(kBlock) void attend_join_kernel(AttendArgs g) {
 }
 
 template <typename T>
-hipError_t launch_attend_of(const AttendArgs& g, hipStream_t s) {
+void start_general(const AttendArgs& g, hipStream_t s) {
     const uint64_t items = (uint64_t)g.row_blocks * (uint64_t)g.splits * (uint64_t)g.kv_heads;
     const dim3 grid((uint32_t)((items + kBlock / 64 - 1) / (kBlock / 64))), block(kBlock);
     if (g.channels <= 64) launch(attend_kernel<T, 64>, grid, block, 0, s, g);
     else if (g.channels <= 128) launch(attend_kernel<T, 128>, grid, block, 0, s, g);
     else launch(attend_kernel<T, 256>, grid, block, 0, s, g);
-    if (g.splits > 1) launch(attend_join_kernel<T>, dim3((uint32_t)(g.kv_heads * g.repeat * g.t_q)), block, 0, s, g);
-    return hipGetLastError();
 }
 
-hipError_t launch_attend(const AttendArgs& g, int dtype, hipStream_t s) {
-    if (dtype == TOM_F32) return launch_attend_of<In_f32>(g, s);
-    return dtype == TOM_BF16 ? launch_attend_of<In_bf16>(g, s) : launch_attend_of<In_f16>(g, s);
+hipError_t launch_attend(const AttendArgs& g, const AttendForm& form, int dtype, hipStream_t s) {
+    if (form.folded) {
+        if (dtype == TOM_BF16) (g.bits == 4 ? start_attend_bf16_4bit : start_attend_bf16_2bit)(g, form, s);
+        else (g.bits == 4 ? start_attend_f16_4bit : start_attend_f16_2bit)(g, form, s);
+    } else if (dtype == TOM_F32) {
+        start_general<In_f32>(g, s);
+    } else if (dtype == TOM_BF16) {
+        start_general<In_bf16>(g, s);
+    } else {
+        start_general<In_f16>(g, s);
+    }
+    if (g.splits > 1) {
+        const dim3 grid((uint32_t)(g.kv_heads * g.repeat * g.t_q)), block(kBlock);
+        if (dtype == TOM_F32) launch(attend_join_kernel<In_f32>, grid, block, 0, s, g);
+        else if (dtype == TOM_BF16) launch(attend_join_kernel<In_bf16>, grid, block, 0, s, g);
+        else launch(attend_join_kernel<In_f16>, grid, block, 0, s, g);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace oqm

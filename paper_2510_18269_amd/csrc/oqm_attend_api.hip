@@ -9,15 +9,6 @@ static int bytes_of(int32_t dtype) { return dtype == TOM_F32 ? 4 : 2; }
 constexpr int32_t kMaxNewTokens = 1 << 20;
 constexpr int64_t kMaxRows = 0x7fffffff - 4096;  // a tile's last token stays inside 32 bits
 
-// Parts that the rows of a call are cut into, each with its own maximum and sum.  Never fewer where there are more rows: the
-// workspace of the longest call serves the others.
-static int32_t cuts(const tom_oqm_config_t& c, int32_t t_q, int64_t rows) {
-    const int64_t blocks = ((int64_t)(c.n_q_heads / c.n_kv_heads) * t_q + 15) / 16 * c.n_kv_heads;
-    int64_t n = 2048 / blocks;  // waves: two a SIMD
-    if (n > (rows + 63) / 64) n = (rows + 63) / 64;
-    return n < 1 ? 1 : (int32_t)n;
-}
-
 static size_t part_bytes(const tom_oqm_config_t& c, int32_t t_q, int32_t splits) {
     if (splits <= 1) return 0;
     return (size_t)c.n_q_heads * (size_t)t_q * (size_t)splits * ((size_t)c.head_dim * sizeof(float) + sizeof(f32pair));
@@ -63,7 +54,7 @@ extern "C" {
 
 size_t tom_oqm_attend_workspace_bytes(const tom_oqm_t* h, int32_t t_q, int64_t rows) {
     if (!h || t_q < 1 || t_q > kMaxNewTokens || rows < 0 || rows > kMaxRows || h->cfg.head_dim > 256) return 0;
-    return part_bytes(h->cfg, t_q, cuts(h->cfg, t_q, rows));
+    return part_bytes(h->cfg, t_q, attend_cuts(h->cfg, t_q, rows));
 }
 
 tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_view_t* q, const tom_oqm_view_t* out, const int32_t* idx,
@@ -95,7 +86,8 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
     if (tom_status_t st = check_rows(recent_k, recent_v, "recent_k", "recent_v", c, a.recent)) return st;
     const int64_t rows = (int64_t)a.front.rows + (int64_t)k_eff * c.group_tokens + a.recent.rows;
     if (rows > kMaxRows) return fail(TOM_ERR_UNSUPPORTED, "%lld rows: at most %lld per call", (long long)rows, (long long)kMaxRows);
-    a.splits = cuts(c, t_q, rows);
+    const AttendForm form = attend_form(c, t_q);
+    a.splits = attend_cuts(c, t_q, rows);
     const size_t need = part_bytes(c, t_q, a.splits);
     if (need > 0) {
         if (!workspace || workspace_bytes < need)
@@ -139,9 +131,9 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
     constexpr float kLog2e = 1.4426950408889634f;
     a.scale_log2 = softcap > 0.0f ? scale / softcap : scale * kLog2e;
     a.cap_log2 = softcap * kLog2e;
-    a.row_blocks = (a.repeat * t_q + 15) / 16;
+    a.row_blocks = (a.repeat * t_q + form.rows - 1) / form.rows;
     (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's
-    const hipError_t err = launch_attend(a, c.out_dtype, static_cast<hipStream_t>(hip_stream));
+    const hipError_t err = launch_attend(a, form, c.out_dtype, static_cast<hipStream_t>(hip_stream));
     if (err != hipSuccess) return fail(TOM_ERR_HIP, "attend launch: %s", hipGetErrorString(err));
     return TOM_OK;
 }

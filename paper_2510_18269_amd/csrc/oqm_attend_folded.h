@@ -1,0 +1,708 @@
+// Attention over stored groups without reconstructing them: codes enter the matrix products as they are.
+//
+// With x = code * s + m and (s, m) the same for all channels of a quant-group g of a token t,
+//   <q, k_t>      = sum_g s_tg <q, code_t>_g + m_tg sum(q)_g
+//   sum_t p_t v_t = sum_t (p_t s_tg) code_t + sum_t p_t m_tg            in the channels of g
+// so both products run over the codes, and scales and zeros touch only scores and probabilities, in float32.  A code is exact in
+// bfloat16, and cheap: its bits alone are the sub-normal code * 2^-133, which the matrix cores take as such (queries and
+// probabilities are scaled by 2^64 against it, so that sums are normal numbers).  An AND gives two operand elements; codes that
+// lie higher in a byte come out multiplied by a power of two, which the queries' channels, or the sums at the end, take back.
+// Queries of binary16 are split into two bfloat16 parts (exactly), probabilities too (2^-17).
+#pragma once
+
+#include "oqm_attend_device.h"
+
+namespace oqm {
+
+// What the lanes of a wave wrote to LDS is read by others of it: the wave's LDS operations run in order, so only the compiler must
+// keep it.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+constexpr float kUp = 0x1p64f, kDown = 0x1p69f;  // 2^64 * 2^-133 = 2^-69
+
+template <typename T, int DP_, int GS_, int BITS_, int MT_, int NW_>
+struct Folded {
+    typedef T type;
+    static constexpr int DP = DP_, GS = GS_, BITS = BITS_;
+    static constexpr int MT = MT_;                  // blocks of 16 query rows of a wave
+    static constexpr int NW = NW_;                  // waves that share a staged tile
+    static constexpr int TT = NW == 1 ? 32 : 64;    // tokens staged
+    static constexpr int NG = DP / GS;              // quant-groups of a token
+    static constexpr int VU = GS / 16, VN = NG;     // channels of a group a lane holds as rows of V^T; groups
+    static constexpr int SPG = GS / 32, STEPS = DP / 32;
+    static constexpr int PARTS = __is_same(T, In_f16) ? 2 : 1;  // of a query element
+    static constexpr int ROW = DP * BITS / 8;       // bytes of a token's codes
+    static constexpr int STRIDE = ROW + 16;         // in LDS: rows spread over the banks
+    static constexpr int PIECES = TT * ROW / 16;    // of 16 bytes, of K or of V
+    static constexpr int LOADS = (PIECES + NW * 64 - 1) / (NW * 64);
+    static constexpr int META = TT * NG * 8;        // bytes of K's or V's pairs in LDS
+    static constexpr int STAGE = 2 * TT * STRIDE + 2 * META;
+    static constexpr int LDS = NW == 1 ? 4 * STAGE : 2 * STAGE;
+
+    f32x4 o[MT][DP / 16];
+    float zero[MT][NG];  // sum of p * m of the lane's tokens
+    float top[MT], sum[MT];
+
+    // ---- staging ----
+    struct Fetch {
+        u32x4 k[LOADS], v[LOADS];
+        uint32_t meta[2 * NG];
+        bool seen;        // the token whose pairs the lane holds is one
+        uint64_t valid;   // of the tile's tokens
+    };
+    // The tokens of a tile lie in two groups at most where a group is as long as a tile: their slots are the wave's.
+    struct Place {
+        int32_t rank, tok, slot0, slot1;
+    };
+    static __device__ __forceinline__ int32_t slot_at(const AttendArgs& g, int32_t rank) {
+        if (rank >= g.k_eff) return -1;
+        const int32_t slot = g.idx ? g.idx[rank] : rank;
+        return slot >= 0 && slot < g.n_groups ? slot : -1;
+    }
+    static __device__ __forceinline__ Place place(const AttendArgs& g, int32_t t0) {
+        Place p;
+        p.rank = (int32_t)div_by((uint32_t)t0, (uint32_t)g.group_tokens, g.inv_group_tokens);
+        p.rank = __builtin_amdgcn_readfirstlane(p.rank);
+        p.tok = t0 - p.rank * g.group_tokens;
+        p.slot0 = p.slot1 = 0;
+        if (g.group_tokens >= TT) {
+            p.slot0 = __builtin_amdgcn_readfirstlane(slot_at(g, p.rank));
+            p.slot1 = __builtin_amdgcn_readfirstlane(slot_at(g, p.rank + 1));
+        }
+        return p;
+    }
+    // Slot and row of the tile's token dt; a hole, or what lies behind the last token, is read from slot 0 and not used.
+    static __device__ __forceinline__ bool find(const AttendArgs& g, const Place& p, int32_t t0, int32_t tokens, int dt, int32_t& slot, int32_t& tok) {
+        if (g.group_tokens >= TT) {
+            tok = p.tok + dt;
+            slot = p.slot0;
+            if (tok >= g.group_tokens) {
+                tok -= g.group_tokens;
+                slot = p.slot1;
+            }
+        } else {
+            const uint32_t rest = (uint32_t)(p.tok + dt), more = div_by(rest, (uint32_t)g.group_tokens, g.inv_group_tokens);
+            tok = (int32_t)(rest - more * (uint32_t)g.group_tokens);
+            slot = slot_at(g, p.rank + (int32_t)more);
+        }
+        const bool is = slot >= 0 && t0 + dt < tokens;
+        if (!is) slot = 0;
+        return is;
+    }
+    static __device__ __forceinline__ void fetch(const AttendArgs& g, int head, int32_t t0, int32_t tokens, Fetch& f) {
+        const int tid = NW == 1 ? (int)__lane_id() : (int)threadIdx.x;
+        const Place p = place(g, t0);
+        const char* kc = g.codes[0] + head * g.code_head;
+        const char* vc = g.codes[1] + head * g.code_head;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int piece = i * NW * 64 + tid;
+            int32_t slot, tok;
+            find(g, p, t0, tokens, (piece / (ROW / 16)) % TT, slot, tok);
+            const int64_t at = slot * g.code_slot + (int64_t)tok * ROW + (piece % (ROW / 16)) * 16;
+            f.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kc + at));
+            f.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vc + at));
+        }
+        int32_t slot, tok;
+        f.seen = find(g, p, t0, tokens, tid % TT, slot, tok);
+        f.valid = __ballot(f.seen);
+        if (tid < 2 * TT) {
+            const char* m = g.meta[0] + (tid < TT ? 0 : g.meta[1] - g.meta[0]) + head * g.meta_head + slot * g.meta_slot;
+            if (g.meta_bf16) {
+                const uint32_t* w = reinterpret_cast<const uint32_t*>(m + (int64_t)tok * NG * 4);
+#pragma unroll
+                for (int i = 0; i < NG; ++i) f.meta[i] = w[i];
+            } else {
+                const u32x2* w = reinterpret_cast<const u32x2*>(m + (int64_t)tok * NG * 8);
+#pragma unroll
+                for (int i = 0; i < NG; ++i) {
+                    const u32x2 x = w[i];
+                    f.meta[2 * i] = x[0];
+                    f.meta[2 * i + 1] = x[1];
+                }
+            }
+        }
+    }
+    static __device__ __forceinline__ void stage(const AttendArgs& g, const Fetch& f, char* lds) {
+        const int tid = NW == 1 ? (int)__lane_id() : (int)threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int piece = i * NW * 64 + tid;
+            if (PIECES % (NW * 64) == 0 || piece < PIECES) {
+                char* at = lds + piece / (ROW / 16) * STRIDE + piece % (ROW / 16) * 16;
+                *reinterpret_cast<u32x4*>(at) = f.k[i];
+                *reinterpret_cast<u32x4*>(at + TT * STRIDE) = f.v[i];
+            }
+        }
+        if (tid < 2 * TT) {
+            f32x2* at = reinterpret_cast<f32x2*>(lds + 2 * TT * STRIDE + tid * NG * 8);
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                f32x2 p = {0.f, 0.f};  // a token that is not there must not bring a NaN
+                if (f.seen) p = g.meta_bf16 ? widen_pair(f.meta[i]) : f32x2{__uint_as_float(f.meta[2 * i]), __uint_as_float(f.meta[2 * i + 1])};
+                at[i] = p;
+            }
+        }
+    }
+
+    // ---- operands from packed codes ----
+    // Step s of the keys' product in a group: 8 codes of a lane's CQ = GS / 4 channels of it.  `w`: those channels' words.
+    static constexpr int CQ = GS / 4, CQ_BYTES = CQ * BITS / 8, CQ_WORDS = CQ_BYTES < 4 ? 1 : CQ_BYTES / 4;
+    static __device__ __forceinline__ void key_words(const char* p, uint32_t (&w)[CQ_WORDS]) {
+        if constexpr (CQ_BYTES == 2) {
+            const uint32_t x = *reinterpret_cast<const uint16_t*>(p);
+            w[0] = __builtin_amdgcn_perm(x, x, 0x0c010c00u);  // a byte in each half
+        } else if constexpr (CQ_BYTES == 4) {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else if constexpr (CQ_BYTES == 8) {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+            w[0] = x[0];
+            w[1] = x[1];
+        } else {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = x[i];
+        }
+    }
+    static __device__ __forceinline__ Operand<In_bf16> key_operand(const uint32_t (&w)[CQ_WORDS], int s) {
+        Operand<In_bf16> a;
+        if constexpr (BITS == 4) {
+            const uint32_t x = w[s], y = x >> 8;
+            a.w = u32x4{x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u};
+        } else {
+            const uint32_t x = GS == 32 ? w[0] : s % 2 == 0 ? w[s / 2] : w[s / 2] >> 8;
+            a.w = u32x4{x & 0x00030003u, x & 0x000c000cu, x & 0x00300030u, x & 0x00c000c0u};
+        }
+        return a;
+    }
+    // The channel of operand element j of step s among the lane's CQ, and what the code is multiplied by there.
+    static __device__ __forceinline__ constexpr int key_channel(int s, int j) {
+        if (BITS == 4) return 8 * s + j / 2 + 4 * (j % 2);
+        if (GS == 32) return j / 2 + 4 * (j % 2);
+        return 16 * (s / 2) + 4 * (s % 2) + j / 2 + 8 * (j % 2);
+    }
+    static __device__ __forceinline__ constexpr float key_factor(int j) {
+        return BITS == 4 ? ((j / 2) % 2 ? 16.0f : 1.0f) : j / 2 == 0 ? 1.0f : j / 2 == 1 ? 4.0f : j / 2 == 2 ? 16.0f : 64.0f;
+    }
+    // Rows of V^T: block n of a group holds channel VU * lane + n of it, for the lane's 8 tokens.
+    static __device__ __forceinline__ constexpr float value_factor(int n) {
+        return BITS == 4 ? (n % 2 ? 16.0f : 1.0f) : n % 4 == 0 ? 1.0f : n % 4 == 1 ? 4.0f : n % 4 == 2 ? 16.0f : 64.0f;
+    }
+    static constexpr int VU_BITS = VU * BITS;
+    struct ValueWords {
+        uint32_t lo[4], hi[4];  // of two tokens each; hi only where a lane's channels of a token fill 32 bits
+    };
+    static __device__ __forceinline__ void value_words(const char* row0, int a, ValueWords& v) {
+        // row0: the group's codes of the lane's first token; its others are 1, 2, 3 and 16 .. 19 rows on
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const char* p = row0 + (i < 2 ? 2 * i : 12 + 2 * i) * STRIDE;
+            if constexpr (VU_BITS == 32) {
+                const uint32_t x = reinterpret_cast<const uint32_t*>(p)[a], y = reinterpret_cast<const uint32_t*>(p + STRIDE)[a];
+                v.lo[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                v.hi[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            } else if constexpr (VU_BITS == 16) {
+                const uint32_t x = reinterpret_cast<const uint16_t*>(p)[a], y = reinterpret_cast<const uint16_t*>(p + STRIDE)[a];
+                v.lo[i] = x | y << 16;
+            } else if constexpr (VU_BITS == 8) {
+                const uint32_t x = reinterpret_cast<const uint8_t*>(p)[a], y = reinterpret_cast<const uint8_t*>(p + STRIDE)[a];
+                v.lo[i] = x | y << 16;
+            } else {
+                const uint32_t x = reinterpret_cast<const uint8_t*>(p)[a / 2], y = reinterpret_cast<const uint8_t*>(p + STRIDE)[a / 2];
+                v.lo[i] = (x | y << 16) >> (4 * (a % 2));
+            }
+        }
+    }
+    static __device__ __forceinline__ Operand<In_bf16> value_operand(const ValueWords& v, int n) {
+        Operand<In_bf16> r;
+        const uint32_t mask = BITS == 4 ? (n % 2 ? 0x00f000f0u : 0x000f000fu) : 0x00030003u << (2 * (n % 4));
+        const bool high = BITS == 4 ? n % 4 >= 2 : n >= 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = VU_BITS == 32 && n >= 4 ? v.hi[i] : v.lo[i];
+            r.w[i] = (high ? x >> 8 : x) & mask;
+        }
+        return r;
+    }
+
+    // ---- softmax of a tile's scores ----
+    __device__ __forceinline__ void probabilities(float (&w)[MT][8]) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float high = w[m][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) high = fmaxf(high, w[m][i]);
+            high = fmaxf(high, __shfl_xor(high, 16, 64));
+            high = fmaxf(high, __shfl_xor(high, 32, 64));
+            if (__any(high > top[m])) {
+                const float next = fmaxf(top[m], high);
+                const float by = next == -__builtin_inff() ? 1.0f : exp2_of(top[m] - next);
+                top[m] = next;
+                sum[m] *= by;
+#pragma unroll
+                for (int n = 0; n < DP / 16; ++n) o[m][n] *= by;
+#pragma unroll
+                for (int n = 0; n < NG; ++n) zero[m][n] *= by;
+            }
+            const float from = top[m] == -__builtin_inff() ? 0.0f : top[m];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[m][i] = exp2_of(w[m][i] - from);
+                sum[m] += w[m][i];
+            }
+        }
+    }
+
+    // 32 tokens of a staged tile, from its row `sub`.  q: scaled as the codes want it; q_sum: sums of the group's channels in units
+    // of the scores; valid: of the 32 tokens, or of no interest where all are.
+    __device__ __forceinline__ void stored(const AttendArgs& g, const char* lds, int sub, const Operand<In_bf16> (&q)[MT][PARTS][STEPS],
+                                           const float (&q_sum)[MT][NG], uint32_t valid) {
+        const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
+        const char* kc = lds + sub * STRIDE;
+        const char* vc = lds + (TT + sub) * STRIDE;
+        const f32x2* km = reinterpret_cast<const f32x2*>(lds + 2 * TT * STRIDE) + sub * NG;
+        const f32x2* vm = km + TT * NG;
+        float w[MT][8];
+        const float unit = g.scale_log2 * kDown;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f32x4 d[MT][NG];
+#pragma unroll
+            for (int i = 0; i < NG; ++i) {
+                uint32_t words[CQ_WORDS];
+                key_words(kc + (16 * half + a) * STRIDE + i * (GS * BITS / 8) + quarter * CQ_BYTES, words);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) d[m][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < SPG; ++s) {
+                    const Operand<In_bf16> x = key_operand(words, s);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part) d[m][i] = product(x, q[m][part][i * SPG + s], d[m][i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x2* pair = km + (16 * half + 4 * quarter + i) * NG;
+                float scaled[MT], plain[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) scaled[m] = plain[m] = 0.0f;
+#pragma unroll
+                for (int n = 0; n < NG; ++n) {
+                    const f32x2 p = pair[n];
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        scaled[m] = __builtin_fmaf(p[0], d[m][n][i], scaled[m]);
+                        plain[m] = __builtin_fmaf(p[1], q_sum[m][n], plain[m]);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < MT; ++m) w[m][4 * half + i] = __builtin_fmaf(scaled[m], unit, plain[m]);
+            }
+        }
+        finish_scores(g, w);
+        if (valid != 0xffffffffu) {
+            const uint32_t mine = valid >> (4 * quarter);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!(mine >> (16 * (i / 4) + i % 4) & 1u))
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) w[m][i] = -__builtin_inff();
+        }
+        probabilities(w);
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            Operand<In_bf16> hi[MT], lo[MT];
+            float scaled[MT][8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const f32x2 p = vm[(16 * (i / 4) + 4 * quarter + i % 4) * NG + n];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    scaled[m][i] = w[m][i] * (p[0] * kUp);
+                    zero[m][n] = __builtin_fmaf(w[m][i], p[1], zero[m][n]);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) split(scaled[m], hi[m], lo[m]);
+            ValueWords v;
+            value_words(vc + 4 * quarter * STRIDE + n * (GS * BITS / 8), a, v);
+#pragma unroll
+            for (int u = 0; u < VU; ++u) {
+                const Operand<In_bf16> x = value_operand(v, u);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    o[m][n * VU + u] = product(x, hi[m], o[m][n * VU + u]);
+                    o[m][n * VU + u] = product(x, lo[m], o[m][n * VU + u]);
+                }
+            }
+        }
+    }
+    static __device__ __forceinline__ void finish_scores(const AttendArgs& g, float (&w)[MT][8]) {
+        if (g.cap_log2 != 0.0f) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[m][i] = capped(w[m][i], g.cap_log2);
+        }
+    }
+
+    static __device__ __forceinline__ void load_query(const char* p, bool there, int quarter, Operand<T> (&q)[STEPS]) {
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) {
+            q[u].w = u32x4{0u, 0u, 0u, 0u};
+            if (there) q[u].w = *reinterpret_cast<const u32x4*>(p + (quarter * (DP / 4) + 8 * u) * 2);
+        }
+    }
+    // 32 tokens of rows as the model has them, from t0; `seen`: of the rows from the first, how many each query row sees.
+    __device__ __forceinline__ void rows(const AttendArgs& g, const AttendRows& r, int head, int32_t t0, int32_t tokens, const Operand<T> (&q)[MT][STEPS],
+                                         const int32_t (&seen)[MT]) {
+        const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
+        const char* k = r.k + head * r.k_head + quarter * (DP / 4) * 2;
+        const char* v = r.v + head * r.v_head + a * VU * 2;
+        typedef uint32_t Piece __attribute__((ext_vector_type(VU / 2)));
+        // what lies behind the last row is read from the last row, and seen by nobody
+        u32x4 kx[2][STEPS];
+        Piece vx[8][VN];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const char* p = k + (int64_t)min(t0 + 16 * half + a, tokens - 1) * r.k_row;
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) kx[half][u] = *reinterpret_cast<const u32x4*>(p + 16 * u);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const char* p = v + (int64_t)min(t0 + 16 * (i / 4) + 4 * quarter + i % 4, tokens - 1) * r.v_row;
+#pragma unroll
+            for (int n = 0; n < VN; ++n) vx[i][n] = *reinterpret_cast<const Piece*>(p + n * GS * 2);
+        }
+        float w[MT][8];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f32x4 d[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) d[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                Operand<T> x;
+                x.w = kx[half][u];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) d[m] = product(x, q[m][u], d[m]);
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[m][4 * half + i] = d[m][i] * g.scale_log2;
+        }
+        finish_scores(g, w);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (t0 + 16 * (i / 4) + 4 * quarter + i % 4 >= seen[m]) w[m][i] = -__builtin_inff();
+        probabilities(w);
+        Operand<T> hi[MT], lo[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) split(w[m], hi[m], lo[m]);
+#pragma unroll
+        for (int n = 0; n < VN; ++n)
+#pragma unroll
+            for (int u = 0; u < VU; u += 2) {
+                Operand<T> even, odd;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x = vx[2 * i][n][u / 2], y = vx[2 * i + 1][n][u / 2];
+                    even.w[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                    odd.w[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                }
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    f32x4 &e = o[m][n * VU + u], &f = o[m][n * VU + u + 1];
+                    e = product(even, hi[m], e);
+                    e = product(even, lo[m], e);
+                    f = product(odd, hi[m], f);
+                    f = product(odd, lo[m], f);
+                }
+            }
+    }
+    // The sums' units: of the rows (1), or of the codes.
+    template <bool TO_CODES>
+    __device__ __forceinline__ void rescale() {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < DP / 16; ++n) {
+                const float f = value_factor(n % VU) / kDown;
+                o[m][n] *= TO_CODES ? f : 1.0f / f;
+            }
+    }
+};
+
+// Tiles of the three segments in one numbering, and what of them a workgroup takes.
+struct Segments {
+    int32_t front, stored, recent_rows, front_tiles, stored_tiles, begin, end;
+};
+__device__ __forceinline__ Segments segments_of(const AttendArgs& g, int32_t last_token, uint32_t cut, int tile_tokens) {
+    Segments s;
+    s.front = g.front.rows;
+    s.stored = g.k_eff * g.group_tokens;
+    s.recent_rows = g.recent.rows;  // as far as any row of the block sees
+    if (g.causal) s.recent_rows = max(0, min(s.recent_rows, last_token + 1 + g.recent.rows - g.t_q));
+    s.front_tiles = (s.front + tile_tokens - 1) / tile_tokens;
+    s.stored_tiles = (s.stored + tile_tokens - 1) / tile_tokens;
+    const int32_t tiles = s.front_tiles + s.stored_tiles + (s.recent_rows + tile_tokens - 1) / tile_tokens;
+    s.begin = (int32_t)((int64_t)tiles * cut / g.splits);
+    s.end = (int32_t)((int64_t)tiles * (cut + 1) / g.splits);
+    return s;
+}
+
+// NW == 1: the workgroup's four waves have the same 16 MT query rows, take its tiles in turn, each staging its own, and join at
+// the end.  NW == 4: they have 16 MT rows each and share every tile.
+template <typename F>
+__global__ __launch_bounds__(kBlock) void attend_folded_kernel(AttendArgs g) {
+    typedef typename F::type T;
+    constexpr int MT = F::MT, NW = F::NW, TT = F::TT, DP = F::DP, NG = F::NG, STEPS = F::STEPS, VU = F::VU;
+    constexpr int kJoin = NW == 1 ? 4 * (16 * MT * (DP + 4)) * 4 : 0;  // the waves' sums, at the end
+    __shared__ __align__(16) char lds[F::LDS > kJoin ? F::LDS : kJoin];
+    const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
+    const uint32_t block = blockIdx.x % (uint32_t)g.row_blocks, rest = blockIdx.x / (uint32_t)g.row_blocks;
+    const uint32_t cut = rest % (uint32_t)g.splits;
+    const int head = (int)(rest / (uint32_t)g.splits);
+    constexpr int kBlockRows = 16 * MT * NW;
+    const int32_t rows = g.t_q * g.repeat;
+    const int32_t first_row = (int32_t)block * kBlockRows, wave_row = first_row + (NW == 1 ? 0 : wave * 16 * MT);
+
+    F f;
+    bool there[MT];
+    int32_t token[MT], q_head[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int32_t row = wave_row + 16 * m + a;
+        there[m] = row < rows;
+        token[m] = there[m] ? (int32_t)div_by((uint32_t)row, (uint32_t)g.repeat, g.inv_repeat) : 0;
+        q_head[m] = head * g.repeat + (there[m] ? row - token[m] * g.repeat : 0);
+        f.top[m] = -__builtin_inff();
+        f.sum[m] = 0.0f;
+#pragma unroll
+        for (int n = 0; n < DP / 16; ++n) f.o[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < NG; ++n) f.zero[m][n] = 0.0f;
+    }
+    const bool works = NW == 1 || wave_row < rows;  // a wave of a block's end has no rows but stages with the others
+    const int32_t last_token = (min(first_row + kBlockRows, rows) - 1) / g.repeat;
+    const int32_t wave_last = (min(wave_row + 16 * MT, rows) - 1) / g.repeat;
+    const Segments s = segments_of(g, last_token, cut, TT);
+    constexpr int kStep = NW == 1 ? 4 : 1;
+    const int32_t begin = s.begin + (NW == 1 ? wave : 0);
+
+    auto rows_of = [&](const AttendRows& r, int32_t from, int32_t to, int32_t first, int32_t tokens, bool recent) {
+        if (from >= to || !works) return;
+        Operand<T> q[MT][STEPS];
+        int32_t seen[MT], all = tokens;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            F::load_query(g.q + q_head[m] * g.q_head + token[m] * g.q_row, there[m], quarter, q[m]);
+            seen[m] = tokens;
+            if (recent && g.causal) seen[m] = min(tokens, token[m] + 1 + g.recent.rows - g.t_q);
+        }
+        if (recent && g.causal) all = min(tokens, wave_last + 1 + g.recent.rows - g.t_q);
+        for (int32_t t = from; t < to; t += kStep)
+#pragma unroll 1
+            for (int sub = 0; sub < TT; sub += 32) {
+                const int32_t t0 = (t - first) * TT + sub;
+                if (t0 < all) f.rows(g, r, head, t0, tokens, q, seen);
+            }
+    };
+    auto from_in = [&](int32_t lo) { return begin >= lo ? begin : begin + (lo - begin + kStep - 1) / kStep * kStep; };
+
+    rows_of(g.front, from_in(0), min(s.end, s.front_tiles), 0, s.front, false);
+
+    const int32_t stored_end = min(s.end, s.front_tiles + s.stored_tiles);
+    if (from_in(s.front_tiles) < stored_end) {
+        Operand<In_bf16> q[MT][F::PARTS][STEPS];
+        float q_sum[MT][NG];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const char* p = g.q + q_head[m] * g.q_head + token[m] * g.q_row;
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+                float x[F::CQ], total = 0.0f;
+#pragma unroll
+                for (int c = 0; c < F::CQ; c += 8) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[c + i] = 0.0f;
+                    if (there[m]) load_row<T, 8>(p + (n * F::GS + quarter * F::CQ + c) * 2, x + c);
+                }
+#pragma unroll
+                for (int c = 0; c < F::CQ; ++c) total += x[c];
+#pragma unroll
+                for (int step = 0; step < F::SPG; ++step) {
+                    float y[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) y[j] = x[F::key_channel(step, j)] * (kUp / F::key_factor(j));
+                    Operand<In_bf16> hi, lo;
+                    split(y, hi, lo);
+                    q[m][0][n * F::SPG + step] = hi;
+                    if constexpr (F::PARTS == 2) q[m][1][n * F::SPG + step] = lo;
+                }
+                total += __shfl_xor(total, 16, 64);
+                total += __shfl_xor(total, 32, 64);
+                q_sum[m][n] = total * g.scale_log2;
+            }
+        }
+        f.template rescale<true>();
+        char* const mine = lds + (NW == 1 ? wave * F::STAGE : 0);
+        typename F::Fetch next;
+        int32_t t = from_in(s.front_tiles);
+        F::fetch(g, head, (t - s.front_tiles) * TT, s.stored, next);
+        for (int buffer = 0; t < stored_end; t += kStep, buffer ^= 1) {
+            char* const here = mine + (NW == 1 ? 0 : buffer * F::STAGE);
+            const uint64_t valid = next.valid;
+            F::stage(g, next, here);
+            if constexpr (NW == 1) wave_sync();
+            else __syncthreads();  // the other buffer is written only behind the next of these, when all have read it
+            if (t + kStep < stored_end) F::fetch(g, head, (t + kStep - s.front_tiles) * TT, s.stored, next);
+            if (works) {
+#pragma unroll 1
+                for (int sub = 0; sub < TT; sub += 32)
+                    if ((uint32_t)(valid >> sub)) f.stored(g, here, sub, q, q_sum, (uint32_t)(valid >> sub));
+            }
+            if constexpr (NW == 1) wave_sync();
+        }
+        f.template rescale<false>();
+    }
+
+    rows_of(g.recent, from_in(s.front_tiles + s.stored_tiles), s.end, s.front_tiles + s.stored_tiles, s.recent_rows, true);
+
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        f.sum[m] += __shfl_xor(f.sum[m], 16, 64);
+        f.sum[m] += __shfl_xor(f.sum[m], 32, 64);
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            float& z = f.zero[m][n];
+            z += __shfl_xor(z, 16, 64);
+            z += __shfl_xor(z, 32, 64);
+#pragma unroll
+            for (int u = 0; u < VU; ++u) f.o[m][n * VU + u] += z;
+        }
+    }
+
+    typedef typename Element<T>::type E;
+    if constexpr (NW == 1) {
+        // the waves' sums by LDS: [wave][row][DP + 4], the row's maximum and sum behind it
+        constexpr int kRow = DP + 4;
+        float* const mine = reinterpret_cast<float*>(lds) + wave * 16 * MT * kRow;
+        __syncthreads();  // staged tiles have been read
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float* const row = mine + (16 * m + a) * kRow;
+#pragma unroll
+            for (int n = 0; n < NG; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int u = 0; u < VU; u += 2)
+                        *reinterpret_cast<f32x2*>(row + n * F::GS + (4 * quarter + i) * VU + u) = f32x2{f.o[m][n * VU + u][i], f.o[m][n * VU + u + 1][i]};
+            if (quarter == 0) *reinterpret_cast<f32x2*>(row + DP) = f32x2{f.top[m], f.sum[m]};
+        }
+        __syncthreads();
+        constexpr int kLanes = DP / 4;  // of a row
+        const float* const base = reinterpret_cast<const float*>(lds);
+        for (int r = (int)threadIdx.x / kLanes; r < min(16 * MT, rows - first_row); r += kBlock / kLanes) {
+            const int c = (int)threadIdx.x % kLanes * 4;
+            f32x2 stat[4];
+            float high = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                stat[w] = *reinterpret_cast<const f32x2*>(base + (w * 16 * MT + r) * kRow + DP);
+                high = fmaxf(high, stat[w][0]);
+            }
+            const float from = high == -__builtin_inff() ? 0.0f : high;
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float by = exp2_of(stat[w][0] - from);
+                total = __builtin_fmaf(by, stat[w][1], total);
+                x += *reinterpret_cast<const f32x4*>(base + (w * 16 * MT + r) * kRow + c) * by;
+            }
+            const int32_t tok = (int32_t)div_by((uint32_t)(first_row + r), (uint32_t)g.repeat, g.inv_repeat);
+            const int32_t qh = head * g.repeat + first_row + r - tok * g.repeat;
+            const int64_t at = (int64_t)qh * g.t_q + tok;
+            if (g.splits > 1) {
+                *reinterpret_cast<f32x4*>(g.part_out + (at * g.splits + cut) * DP + c) = x;
+                if (c == 0) g.part_stat[at * g.splits + cut] = f32pair{high, total};
+            } else {
+                const float by = total > 0.0f ? 1.0f / total : 0.0f;
+                typedef E Vec __attribute__((ext_vector_type(4)));
+                Vec y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = (E)(x[i] * by);
+                *reinterpret_cast<Vec*>(g.out + qh * g.out_head + tok * g.out_row + (int64_t)c * 2) = y;
+                if (c == 0 && g.lse) g.lse[at] = total > 0.0f ? (high + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff();
+            }
+        }
+    } else {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if (!there[m]) continue;
+            const int64_t at = (int64_t)q_head[m] * g.t_q + token[m];
+            const float by = f.sum[m] > 0.0f ? 1.0f / f.sum[m] : 0.0f;
+#pragma unroll
+            for (int n = 0; n < NG; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = n * F::GS + (4 * quarter + i) * VU;
+                    if (g.splits > 1) {
+                        typedef float Vec __attribute__((ext_vector_type(VU)));
+                        Vec y;
+#pragma unroll
+                        for (int u = 0; u < VU; ++u) y[u] = f.o[m][n * VU + u][i];
+                        *reinterpret_cast<Vec*>(g.part_out + (at * g.splits + cut) * DP + c) = y;
+                    } else {
+                        typedef E Vec __attribute__((ext_vector_type(VU)));
+                        Vec y;
+#pragma unroll
+                        for (int u = 0; u < VU; ++u) y[u] = (E)(f.o[m][n * VU + u][i] * by);
+                        *reinterpret_cast<Vec*>(g.out + q_head[m] * g.out_head + token[m] * g.out_row + (int64_t)c * 2) = y;
+                    }
+                }
+            if (quarter == 0) {
+                if (g.splits > 1) g.part_stat[at * g.splits + cut] = f32pair{f.top[m], f.sum[m]};
+                else if (g.lse) g.lse[at] = f.sum[m] > 0.0f ? (f.top[m] + __builtin_amdgcn_logf(f.sum[m])) * kLn2 : -__builtin_inff();
+            }
+        }
+    }
+}
+
+template <typename T, int DP, int GS, int BITS>
+void start_folded(const AttendArgs& g, const AttendForm& form, hipStream_t s) {
+    const dim3 grid((uint32_t)((int64_t)g.row_blocks * g.splits * g.kv_heads)), block(kBlock);
+    if (form.rows == 16) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 1>>, grid, block, 0, s, g);
+    else if (form.rows == 64) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 4>>, grid, block, 0, s, g);
+    else launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 2, 4>>, grid, block, 0, s, g);
+}
+
+template <typename T, int BITS>
+void start_folded_of(const AttendArgs& g, const AttendForm& form, hipStream_t s) {
+    const int gs = 1 << g.qgroup_log2;
+    if (g.channels == 64) {
+        if (gs == 32) start_folded<T, 64, 32, BITS>(g, form, s);
+        else start_folded<T, 64, 64, BITS>(g, form, s);
+    } else if (g.channels == 128) {
+        if (gs == 32) start_folded<T, 128, 32, BITS>(g, form, s);
+        else if (gs == 64) start_folded<T, 128, 64, BITS>(g, form, s);
+        else start_folded<T, 128, 128, BITS>(g, form, s);
+    } else {
+        if (gs == 32) start_folded<T, 256, 32, BITS>(g, form, s);
+        else if (gs == 64) start_folded<T, 256, 64, BITS>(g, form, s);
+        else start_folded<T, 256, 128, BITS>(g, form, s);
+    }
+}
+
+}  // namespace oqm
