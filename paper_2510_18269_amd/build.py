@@ -1,6 +1,7 @@
 """Builds libtom_oqm.so (gfx950 kernels + C ABI) in-tree with hipcc."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
@@ -14,6 +15,8 @@ LIB = os.path.join(HERE, "libtom_oqm.so")
 OBJ = os.path.join(HERE, "_build")
 # with the interpreter's tag: one of another version refuses the file instead of loading it
 BINDING = os.path.join(HERE, "_oqm_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
+# the binding reads tensors as this PyTorch lays them out; its libraries are loaded before the binding is
+TORCH = os.path.dirname(importlib.util.find_spec("torch").origin)
 SELFCHECK = os.path.join(HERE, "selfcheck_division.bin")
 
 SOURCES = ["oqm_api.hip", "oqm_quantize.hip", "oqm_quantize_tokens.hip", "oqm_dequant.hip", "oqm_score.hip",
@@ -57,10 +60,11 @@ def build(verbose: bool = False) -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
-    # the Python side's argument marshalling: host code only, linked against the library beside it
+    # the Python side's argument marshalling: host code only, linked against the library beside it and PyTorch's
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-I", INCLUDE,
-           "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "oqm_binding.cpp"), "-o", BINDING,
-           "-L", HERE, "-ltom_oqm", "-Wl,-rpath,$ORIGIN"]
+           "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(TORCH, "include"),
+           os.path.join(CSRC, "oqm_binding.cpp"), "-o", BINDING, "-L", HERE, "-ltom_oqm", "-Wl,-rpath,$ORIGIN",
+           "-L", os.path.join(TORCH, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"binding build failed:\n{r.stdout}\n{r.stderr}")

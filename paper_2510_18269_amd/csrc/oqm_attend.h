@@ -73,7 +73,7 @@ inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
                         (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256);
     if (!folded) return {false, 16};
     const int64_t rows = (int64_t)(c.n_q_heads / c.n_kv_heads) * t_q;
-    return {true, rows <= 16 ? 16 : rows <= 64 ? 64 : 128};
+    return {true, rows <= 16 ? 16 : rows <= 64 || c.head_dim == 256 ? 64 : 128};
 }
 
 // Parts that the rows of a call are cut into, each with its own maximum and sum.  Never fewer where there are more rows: the

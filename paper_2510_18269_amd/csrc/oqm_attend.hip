@@ -243,54 +243,100 @@ __global__ __launch_bounds__(kBlock) void attend_kernel(AttendArgs g) {
 }
 
 // ---- joining the parts ---------------------------------------------------------------------------------------------------------
-// A workgroup takes a query row: weights 2^(M_s - M) of its parts, their sum, and the weighted sum of their rows.
-template <typename T>
-__global__ __launch_bounds__(kBlock) void attend_join_kernel(AttendArgs g) {
-    __shared__ float shared[kBlock / 64];
-    __shared__ f32x4 rows[kBlock];
-    __shared__ float sums[kBlock];
-    const int64_t at = blockIdx.x;
-    const int32_t q_head = (int32_t)(at / g.t_q), token = (int32_t)(at - (int64_t)q_head * g.t_q);
-    const f32pair* stat = g.part_stat + at * g.splits;
-    float top = -__builtin_inff();
-    for (int s = threadIdx.x; s < g.splits; s += kBlock) top = fmaxf(top, stat[s].x);
-    for (int m = 32; m > 0; m /= 2) top = fmaxf(top, __shfl_xor(top, m, 64));
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x / 64] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
-    const float from = top == -__builtin_inff() ? 0.0f : top;
-    // lanes of a part: a power of two that holds the channels by fours
-    int lanes_log2 = 1;
-    while ((4 << lanes_log2) < g.channels) ++lanes_log2;
-    const int lanes = 1 << lanes_log2, lane = (int)threadIdx.x & (lanes - 1), first = (int)threadIdx.x >> lanes_log2;
-    const bool there = 4 * lane < g.channels;
+// The rows of the parts, weighted by 2^(M_s - M), and the sum of their sums.  A lane takes four channels and some of the parts, with
+// the running maximum again, so that no load waits for another; four parts are in flight.
+struct Joined {
+    float top = -__builtin_inff(), total = 0.0f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.0f;
-    const float* part = g.part_out + at * g.splits * g.channels + 4 * lane;
-    for (int s = first; s < g.splits; s += kBlock >> lanes_log2) {
-        const f32pair p = stat[s];
-        const float by = exp2_of(p.x - from);
-        total = fmaf(by, p.y, total);
-        if (there) sum += *reinterpret_cast<const f32x4*>(part + (int64_t)s * g.channels) * by;
+    __device__ __forceinline__ void add(float their_top, float their_total, const f32x4& their_sum) {
+        const float next = fmaxf(top, their_top), from = next == -__builtin_inff() ? 0.0f : next;
+        const float mine = exp2_of(top - from), theirs = exp2_of(their_top - from);
+        top = next;
+        total = total * mine + their_total * theirs;
+        sum = sum * mine + their_sum * theirs;
     }
-    rows[threadIdx.x] = sum;
-    sums[threadIdx.x] = total;
-    __syncthreads();
-    if (first != 0) return;
-    for (int s = 1; s < kBlock >> lanes_log2; ++s) {
-        sum += rows[(s << lanes_log2) + lane];
-        total += sums[(s << lanes_log2) + lane];
-    }
-    const float by = total > 0.0f ? 1.0f / total : 0.0f;
-    if (there) {
-        typedef typename Element<T>::type E;
-        typedef E Vec __attribute__((ext_vector_type(4)));
-        Vec y;
+};
+template <typename T>
+__device__ __forceinline__ void put_joined(const AttendArgs& g, int64_t at, int c, const Joined& j) {
+    const int32_t q_head = (int32_t)(at / g.t_q), token = (int32_t)(at - (int64_t)q_head * g.t_q);
+    const float by = j.total > 0.0f ? 1.0f / j.total : 0.0f;
+    typedef typename Element<T>::type E;
+    typedef E Vec __attribute__((ext_vector_type(4)));
+    Vec y;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) y[n] = (E)(sum[n] * by);
-        *reinterpret_cast<Vec*>(g.out + q_head * g.out_head + token * g.out_row + (int64_t)(4 * lane) * sizeof(E)) = y;
+    for (int n = 0; n < 4; ++n) y[n] = (E)(j.sum[n] * by);
+    *reinterpret_cast<Vec*>(g.out + q_head * g.out_head + token * g.out_row + (int64_t)c * sizeof(E)) = y;
+    if (c == 0 && g.lse) g.lse[at] = j.total > 0.0f ? (j.top + __builtin_amdgcn_logf(j.total)) * kLn2 : -__builtin_inff();
+}
+constexpr int kJoinAhead = 4;
+__device__ __forceinline__ Joined join_parts(const AttendArgs& g, int64_t at, int c, int first, int step) {
+    const f32pair* stat = g.part_stat + at * g.splits;
+    const float* part = g.part_out + at * g.splits * g.channels + c;
+    Joined j;
+    for (int s0 = first; s0 < g.splits; s0 += step * kJoinAhead) {
+        f32pair st[kJoinAhead];
+        f32x4 x[kJoinAhead];
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u) {
+            const int s = min(s0 + u * step, g.splits - 1);  // behind the last: read again, and not added
+            st[u] = stat[s];
+            x[u] = *reinterpret_cast<const f32x4*>(part + (int64_t)s * g.channels);
+        }
+#pragma unroll
+        for (int u = 0; u < kJoinAhead; ++u)
+            if (s0 + u * step < g.splits) j.add(st[u].x, st[u].y, x[u]);
     }
-    if (lane == 0 && g.lse) g.lse[at] = total > 0.0f ? (top + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff();
+    return j;
+}
+// Few parts: a lane takes them all.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void attend_join_few_kernel(AttendArgs g, uint32_t lanes, uint32_t inv_lanes, uint32_t rows) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x, row = div_by(i, lanes, inv_lanes);
+    if (row >= rows) return;
+    const int c = 4 * (int)(i - row * lanes);
+    put_joined<T>(g, row, c, join_parts(g, row, c, 0, 1));
+}
+// Many: a workgroup takes 32 channels of a row, eight lanes to a part, and joins what its lanes found.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void attend_join_many_kernel(AttendArgs g) {
+    constexpr int kLanes = 8, kSets = kBlock / kLanes;
+    const int lane = (int)threadIdx.x % kLanes, set = (int)threadIdx.x / kLanes;
+    const int c = 4 * ((int)blockIdx.y * kLanes + lane);
+    const bool there = c < g.channels;
+    Joined j;
+    if (there) j = join_parts(g, blockIdx.x, c, set, kSets);
+#pragma unroll
+    for (int m = kLanes; m < 64; m *= 2) {
+        const float top = __shfl_xor(j.top, m, 64), total = __shfl_xor(j.total, m, 64);
+        f32x4 sum;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) sum[n] = __shfl_xor(j.sum[n], m, 64);
+        j.add(top, total, sum);
+    }
+    __shared__ float tops[kBlock / 64][kLanes], totals[kBlock / 64][kLanes];
+    __shared__ f32x4 sums[kBlock / 64][kLanes];
+    const int wave = (int)threadIdx.x / 64;
+    if ((int)threadIdx.x % 64 < kLanes) {
+        tops[wave][lane] = j.top;
+        totals[wave][lane] = j.total;
+        sums[wave][lane] = j.sum;
+    }
+    __syncthreads();
+    if (threadIdx.x >= kLanes || !there) return;
+    for (int w = 1; w < kBlock / 64; ++w) j.add(tops[w][lane], totals[w][lane], sums[w][lane]);
+    put_joined<T>(g, blockIdx.x, c, j);
+}
+// Up to this many parts a lane takes them all.
+constexpr int kFewParts = 8;
+template <typename T>
+void start_join(const AttendArgs& g, hipStream_t s) {
+    const uint32_t rows = (uint32_t)(g.kv_heads * g.repeat * g.t_q), lanes = (uint32_t)(g.channels / 4);
+    if (g.splits <= kFewParts) {
+        // parts are cut from calls of 2048 waves of 16 rows or less: rows * lanes stays far inside 32 bits
+        launch(attend_join_few_kernel<T>, dim3((rows * lanes + kBlock - 1) / kBlock), dim3(kBlock), 0, s, g, lanes, reciprocal_u32(lanes), rows);
+    } else {
+        launch(attend_join_many_kernel<T>, dim3(rows, (lanes + 7) / 8), dim3(kBlock), 0, s, g);
+    }
 }
 
 template <typename T>
@@ -314,10 +360,9 @@ hipError_t launch_attend(const AttendArgs& g, const AttendForm& form, int dtype,
         start_general<In_f16>(g, s);
     }
     if (g.splits > 1) {
-        const dim3 grid((uint32_t)(g.kv_heads * g.repeat * g.t_q)), block(kBlock);
-        if (dtype == TOM_F32) launch(attend_join_kernel<In_f32>, grid, block, 0, s, g);
-        else if (dtype == TOM_BF16) launch(attend_join_kernel<In_bf16>, grid, block, 0, s, g);
-        else launch(attend_join_kernel<In_f16>, grid, block, 0, s, g);
+        if (dtype == TOM_F32) start_join<In_f32>(g, s);
+        else if (dtype == TOM_BF16) start_join<In_bf16>(g, s);
+        else start_join<In_f16>(g, s);
     }
     return hipGetLastError();
 }

@@ -40,6 +40,7 @@ struct Folded {
     static constexpr int LOADS = (PIECES + NW * 64 - 1) / (NW * 64);
     static constexpr int META = TT * NG * 8;        // bytes of K's or V's pairs in LDS
     static constexpr int STAGE = 2 * TT * STRIDE + 2 * META;
+    static constexpr int WAVES = NW == 1 ? (DP == 64 ? 4 : DP == 128 ? (NG < 4 ? 3 : 2) : 1) : MT == 1 ? (DP == 64 ? 3 : DP == 128 ? 2 : 1) : 2;  // a SIMD
     static constexpr int LDS = NW == 1 ? 4 * STAGE : 2 * STAGE;
 
     f32x4 o[MT][DP / 16];
@@ -368,18 +369,21 @@ struct Folded {
         // what lies behind the last row is read from the last row, and seen by nobody
         u32x4 kx[2][STEPS];
         Piece vx[8][VN];
+        auto load_values = [&] {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const char* p = v + (int64_t)min(t0 + 16 * (i / 4) + 4 * quarter + i % 4, tokens - 1) * r.v_row;
+#pragma unroll
+                for (int n = 0; n < VN; ++n) vx[i][n] = *reinterpret_cast<const Piece*>(p + n * GS * 2);
+            }
+        };
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const char* p = k + (int64_t)min(t0 + 16 * half + a, tokens - 1) * r.k_row;
 #pragma unroll
             for (int u = 0; u < STEPS; ++u) kx[half][u] = *reinterpret_cast<const u32x4*>(p + 16 * u);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const char* p = v + (int64_t)min(t0 + 16 * (i / 4) + 4 * quarter + i % 4, tokens - 1) * r.v_row;
-#pragma unroll
-            for (int n = 0; n < VN; ++n) vx[i][n] = *reinterpret_cast<const Piece*>(p + n * GS * 2);
-        }
+        if constexpr (MT == 1) load_values();  // in flight with the keys; with two blocks of rows there are no registers for it
         float w[MT][8];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -405,6 +409,7 @@ struct Folded {
             for (int i = 0; i < 8; ++i)
                 if (t0 + 16 * (i / 4) + 4 * quarter + i % 4 >= seen[m]) w[m][i] = -__builtin_inff();
         probabilities(w);
+        if constexpr (MT > 1) load_values();
         Operand<T> hi[MT], lo[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) split(w[m], hi[m], lo[m]);
@@ -463,7 +468,7 @@ __device__ __forceinline__ Segments segments_of(const AttendArgs& g, int32_t las
 // NW == 1: the workgroup's four waves have the same 16 MT query rows, take its tiles in turn, each staging its own, and join at
 // the end.  NW == 4: they have 16 MT rows each and share every tile.
 template <typename F>
-__global__ __launch_bounds__(kBlock) void attend_folded_kernel(AttendArgs g) {
+__global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendArgs g) {
     typedef typename F::type T;
     constexpr int MT = F::MT, NW = F::NW, TT = F::TT, DP = F::DP, NG = F::NG, STEPS = F::STEPS, VU = F::VU;
     constexpr int kJoin = NW == 1 ? 4 * (16 * MT * (DP + 4)) * 4 : 0;  // the waves' sums, at the end
@@ -684,8 +689,8 @@ template <typename T, int DP, int GS, int BITS>
 void start_folded(const AttendArgs& g, const AttendForm& form, hipStream_t s) {
     const dim3 grid((uint32_t)((int64_t)g.row_blocks * g.splits * g.kv_heads)), block(kBlock);
     if (form.rows == 16) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 1>>, grid, block, 0, s, g);
-    else if (form.rows == 64) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 4>>, grid, block, 0, s, g);
-    else launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 2, 4>>, grid, block, 0, s, g);
+    else if (DP == 256 || form.rows == 64) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 4>>, grid, block, 0, s, g);
+    else if constexpr (DP < 256) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 2, 4>>, grid, block, 0, s, g);
 }
 
 template <typename T, int BITS>

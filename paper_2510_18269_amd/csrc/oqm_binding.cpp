@@ -3,7 +3,7 @@
 // A one-frame append or a small retrieval keeps the GPU busy for 6 to 20 us, less than what
 // ctypes, torch.cuda.current_stream() and the per-tensor attribute look-ups in Python cost the
 // host around the launches (append 9.3 us, retrieval 19.9 us, the four calls of a tiny stream
-// 39 us with a launch at 3.2 us).  Here a tensor costs one data_ptr() call and the stream one
+// 39 us with a launch at 3.2 us).  Here a tensor is read as torch holds it and the stream costs one
 // call of torch's raw-stream getter.  The library is entered without the interpreter lock, as
 // ctypes enters it.
 //
@@ -11,6 +11,8 @@
 // functions with their names and defaults are in oqm.py.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+
+#include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
 #include <cstdint>
@@ -68,9 +70,27 @@ bool to_handle(PyObject* o, tom_oqm_t*& out) {
     return true;
 }
 
+// A torch tensor as torch holds it: its place and shape then cost some nanoseconds, where the same questions asked through the
+// interpreter take 0.1 to 0.2 us each (an attention has up to six tensors of three dimensions).  Anything else that
+// answers the same questions, or a tensor of a class of its own, is asked them.
+const at::Tensor* tensor_of(PyObject* o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
+
 // None, a raw device pointer, or a tensor on the device.
 bool to_ptr(PyObject* o, void*& out) {
     if (o == Py_None || PyLong_Check(o)) return to_void_p(o, out);
+    if (const at::Tensor* t = tensor_of(o)) {
+        if (!t->is_cuda()) {
+            PyErr_SetString(PyExc_AssertionError, "device tensor expected");
+            return false;
+        }
+        try {
+            out = t->data_ptr();
+        } catch (const std::exception& e) {  // a tensor without storage
+            PyErr_SetString(PyExc_RuntimeError, e.what());
+            return false;
+        }
+        return true;
+    }
     PyObject* c = PyObject_GetAttr(o, s_is_cuda);
     if (!c) return false;
     const int on_device = PyObject_IsTrue(c);
@@ -117,7 +137,9 @@ bool to_stream(PyObject* o, void*& out) {
 // Workspace tensor (or None): pointer and size in bytes.
 bool to_workspace(PyObject* o, void*& ptr, size_t& bytes) {
     bytes = 0;
-    if (o != Py_None) {
+    if (const at::Tensor* t = tensor_of(o)) {
+        bytes = (size_t)t->numel() * (size_t)t->element_size();
+    } else if (o != Py_None) {
         int64_t n, e;
         if (!method_i64(o, s_numel, n) || !method_i64(o, s_element_size, e)) return false;
         bytes = (size_t)n * (size_t)e;
@@ -327,6 +349,12 @@ constexpr int32_t kInt32 = 100, kInt64 = 101;
 
 // The dtype code of a tensor, out of the dictionary that oqm.py registered.
 bool to_dtype(PyObject* o, int32_t& out) {
+    if (const at::Tensor* t = tensor_of(o)) {
+        const at::ScalarType s = t->scalar_type();
+        out = s == at::kFloat ? TOM_F32 : s == at::kBFloat16 ? TOM_BF16 : s == at::kHalf ? TOM_F16 : s == at::kInt ? kInt32 : s == at::kLong ? kInt64 : -1;
+        if (out < 0) PyErr_SetString(PyExc_AssertionError, "tensor of another dtype expected");
+        return out >= 0;
+    }
     PyObject* t = PyObject_GetAttr(o, s_dtype);
     if (!t) return false;
     PyObject* code = PyDict_GetItemWithError(g_dtypes, t);  // borrowed
@@ -354,14 +382,20 @@ bool to_view(PyObject* o, bool rows_first, tom_oqm_view_t& v, bool& given) {
         PyErr_SetString(PyExc_AssertionError, "float32, bfloat16 or float16 tensor expected");
         return false;
     }
-    PyObject* shape = PyObject_GetAttr(o, s_shape);
-    if (!shape) return false;
-    PyObject* strides = strides_of(o);
-    bool ok = strides && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 3 && PyTuple_GET_SIZE(strides) == 3;
     int64_t n[3] = {}, s[3] = {};
-    for (int i = 0; i < 3 && ok; ++i) ok = to_i64(PyTuple_GET_ITEM(shape, i), n[i]) && to_i64(PyTuple_GET_ITEM(strides, i), s[i]);
-    Py_XDECREF(strides);
-    Py_DECREF(shape);
+    bool ok;
+    if (const at::Tensor* t = tensor_of(o)) {
+        ok = t->dim() == 3;
+        for (int i = 0; i < 3 && ok; ++i) n[i] = t->sizes()[i], s[i] = t->strides()[i];
+    } else {
+        PyObject* shape = PyObject_GetAttr(o, s_shape);
+        if (!shape) return false;
+        PyObject* strides = strides_of(o);
+        ok = strides && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 3 && PyTuple_GET_SIZE(strides) == 3;
+        for (int i = 0; i < 3 && ok; ++i) ok = to_i64(PyTuple_GET_ITEM(shape, i), n[i]) && to_i64(PyTuple_GET_ITEM(strides, i), s[i]);
+        Py_XDECREF(strides);
+        Py_DECREF(shape);
+    }
     ok = ok && fits_i32(n[0]) && fits_i32(n[1]) && fits_i32(n[2]) && (s[2] == 1 || n[2] == 1);
     if (!ok) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_AssertionError, "tensor of three dimensions with a contiguous channel axis expected");
@@ -381,12 +415,19 @@ bool to_array(PyObject* o, int64_t want, int32_t dtype, const char* what, void*&
     if (o == Py_None || PyLong_Check(o)) return true;
     int64_t n;
     int32_t own;
-    if (!method_i64(o, s_numel, n) || !to_dtype(o, own)) return false;
-    PyObject* flat = PyObject_CallMethodNoArgs(o, s_is_contiguous);
-    if (!flat) return false;
-    const int in_a_row = PyObject_IsTrue(flat);
-    Py_DECREF(flat);
-    if (in_a_row < 0) return false;
+    int in_a_row;
+    if (!to_dtype(o, own)) return false;
+    if (const at::Tensor* t = tensor_of(o)) {
+        n = t->numel();
+        in_a_row = t->is_contiguous();
+    } else {
+        if (!method_i64(o, s_numel, n)) return false;
+        PyObject* flat = PyObject_CallMethodNoArgs(o, s_is_contiguous);
+        if (!flat) return false;
+        in_a_row = PyObject_IsTrue(flat);
+        Py_DECREF(flat);
+        if (in_a_row < 0) return false;
+    }
     if (own == dtype && n >= want && in_a_row) return true;
     PyErr_Format(PyExc_AssertionError, "%s: a contiguous tensor of at least %lld elements of the right dtype expected", what, (long long)want);
     return false;

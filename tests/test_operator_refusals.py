@@ -163,11 +163,12 @@ def test_attend_refuses(oqm, store):
     refuses(oqm, "scale", lambda: call(scale=math.nan))
     refuses(oqm, "softcap", lambda: call(softcap=-1.0))
     refuses(oqm, "softcap", lambda: call(softcap=math.inf))
-    need = oqm.tom_oqm_attend_workspace_bytes(store, 3, 4 * 16 + 3)
+    need = oqm.tom_oqm_attend_workspace_bytes(store, 3, 4000 * 16 + 3)
     assert need > 0
-    refuses(oqm, f"{need} bytes needed, {need - 1} given", lambda: call(workspace=Fake((need - 1,), torch.uint8)))
-    refuses(oqm, "0 given", lambda: call(workspace=None))
-    refuses(oqm, "aligned", lambda: call(workspace=Fake((1 << 20,), torch.uint8, address=0x10008)))
+    many = dict(k_eff=4000, idx=0x10000)
+    refuses(oqm, f"{need} bytes needed, {need - 1} given", lambda: call(**many, workspace=Fake((need - 1,), torch.uint8)))
+    refuses(oqm, "0 given", lambda: call(**many, workspace=None))
+    refuses(oqm, "aligned", lambda: call(**many, workspace=Fake((need,), torch.uint8, address=0x10008)))
     refuses(oqm, "rows", lambda: call(k_eff=2 ** 27, idx=0x10000), oqm.TOM_ERR_UNSUPPORTED)
     refuses(oqm, "new tokens", lambda: call(q=Fake((6, 2 ** 20 + 1, 64)), out=Fake((6, 2 ** 20 + 1, 64))), oqm.TOM_ERR_UNSUPPORTED)
     for kw in (dict(idx=Fake((3,), torch.int32)), dict(idx=Fake((4,), torch.int64)), dict(lse=Fake((17,), torch.float32)),
