@@ -56,7 +56,7 @@ struct AttendArgs {
     int32_t t_q, repeat, kv_heads;  // repeat: query heads of a KV head
     int32_t causal, token_axis, bits, meta_bf16;
     uint32_t inv_group_tokens, inv_repeat;
-    float scale_log2;      // scale * log2(e); with a cap: scale / softcap
+    float scale_log2;      // scale * log2(e); with a cap: 2 log2(e) scale / softcap
     float cap_log2;        // softcap * log2(e), or 0
     int32_t splits, row_blocks;
 };

@@ -99,7 +99,7 @@ struct General {
             for (int i = 0; i < 4; ++i) {
                 const int j = 4 * quarter + i;
                 const float y = s[i] * g.scale_log2;
-                const float z = g.cap_log2 != 0.0f ? capped(y, g.cap_log2) : y;
+                const float z = g.cap_log2 != 0.0f ? capped_exactly(y, g.cap_log2) : y;
                 w[4 * half + i] = (there >> j & 1u) && t0 + 16 * half + j < seen ? z : -__builtin_inff();
             }
         }

@@ -129,7 +129,7 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
     a.bits = c.bits;
     a.meta_bf16 = c.meta_dtype == TOM_BF16;
     constexpr float kLog2e = 1.4426950408889634f;
-    a.scale_log2 = softcap > 0.0f ? scale / softcap : scale * kLog2e;
+    a.scale_log2 = softcap > 0.0f ? 2.0f * kLog2e * scale / softcap : scale * kLog2e;
     a.cap_log2 = softcap * kLog2e;
     a.row_blocks = (a.repeat * t_q + form.rows - 1) / form.rows;
     (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's

@@ -14,12 +14,16 @@ constexpr int kTile = 32;  // tokens
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// softcap * tanh(y) in units of log 2.  Near zero, where 1 - 2 / (1 + e^2y) cancels, the series.
-__device__ __forceinline__ float capped(float y, float cap_log2) {
-    const float z = y * y;
-    const float small = y * fmaf(z, fmaf(z, fmaf(z, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-    const float wide = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + exp2_of(2.0f * kLog2e * y)), 1.0f);
-    return cap_log2 * (z < 0.015625f ? small : wide);
+// softcap * tanh(y) in units of log 2, from z = 2 log2(e) y: tanh y = 1 - 2 / (1 + 2^z).  The difference loses what the one has over
+// tanh y: an error of 2^-22 * softcap at any y, which 16-bit results do not show.
+__device__ __forceinline__ float capped(float z, float cap_log2) {
+    return __builtin_fmaf(-2.0f * cap_log2, __builtin_amdgcn_rcpf(1.0f + exp2_of(z)), cap_log2);
+}
+// Near zero by the series, for float32.
+__device__ __forceinline__ float capped_exactly(float z, float cap_log2) {
+    const float y = z * (0.5f * kLn2), x = y * y;
+    const float small = y * fmaf(x, fmaf(x, fmaf(x, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+    return x < 0.015625f ? cap_log2 * small : capped(z, cap_log2);
 }
 
 // ---- operands: 8 consecutive k of a row of a 16 x 16 x 32 product (16-bit types), or 8 products of one k a lane (float32) ----
@@ -56,14 +60,16 @@ __device__ __forceinline__ void split(const float (&x)[8], Operand<In_bf16>& hi,
     lo.w = pack_items(In_bf16{}, r);
 }
 __device__ __forceinline__ void split(const float (&x)[8], Operand<In_f16>& hi, Operand<In_f16>& lo) {
-    f16x8 h, l;
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        h[i] = (_Float16)x[i];
-        l[i] = (_Float16)(x[i] - (float)h[i]);
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 v = {x[2 * i], x[2 * i + 1]};
+        const f16x2 h = __builtin_convertvector(v, f16x2);  // v_cvt_pk_f16_f32
+        // one instruction each, widening included
+        const f32x2 r = {__builtin_fmaf((float)h[0], -1.0f, v[0]), __builtin_fmaf((float)h[1], -1.0f, v[1])};
+        hi.w[i] = __builtin_bit_cast(uint32_t, h);
+        lo.w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(r, f16x2));
     }
-    hi.w = __builtin_bit_cast(u32x4, h);
-    lo.w = __builtin_bit_cast(u32x4, l);
 }
 __device__ __forceinline__ void split(const float (&x)[8], Operand<In_f32>& hi, Operand<In_f32>&) {
 #pragma unroll
