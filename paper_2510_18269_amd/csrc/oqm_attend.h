@@ -66,14 +66,16 @@ struct AttendForm {
     bool folded;
     int32_t rows;
 };
-// Folded: 16-bit rows of 64, 128 or 256 channels in quant-groups of 32 channels or more of one token, so that a step of the matrix
-// cores (32 channels of keys, 16 of values) lies in one group.
+// Folded: 16-bit rows of 64, 128 or 256 channels, and either quant-groups of 32 channels or more of one token, so that a step of the
+// matrix cores (32 channels of keys, 16 of values) lies in one of them, or quant-groups along 16 tokens or more, so that a tile of 32
+// tokens, which lies in one of them, is not mostly empty.
 inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
-    const bool folded = c.out_dtype != TOM_F32 && c.qaxis == TOM_QAXIS_HEAD_DIM && c.qgroup >= 32 &&
-                        (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256);
+    const bool tokens = c.qaxis == TOM_QAXIS_TOKENS;
+    const bool folded = c.out_dtype != TOM_F32 && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) &&
+                        (tokens ? c.group_tokens >= 16 : c.qgroup >= 32);
     if (!folded) return {false, 16};
     const int64_t rows = (int64_t)(c.n_q_heads / c.n_kv_heads) * t_q;
-    return {true, rows <= 16 ? 16 : rows <= 64 || c.head_dim == 256 ? 64 : 128};
+    return {true, rows <= 16 ? 16 : rows <= 64 || tokens || c.head_dim == 256 ? 64 : 128};
 }
 
 // Parts that the rows of a call are cut into, each with its own maximum and sum.  Never fewer where there are more rows: the
