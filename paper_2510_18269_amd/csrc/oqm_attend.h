@@ -84,7 +84,7 @@ inline int32_t attend_cuts(const tom_oqm_config_t& c, int32_t t_q, int64_t rows)
     const AttendForm f = attend_form(c, t_q);
     const int64_t blocks = ((int64_t)(c.n_q_heads / c.n_kv_heads) * t_q + f.rows - 1) / f.rows * c.n_kv_heads;
     int64_t target = 2048, least = 64;  // waves: two a SIMD
-    if (f.folded && f.rows == 16) target = 1024, least = 128;
+    if (f.folded && f.rows == 16) target = 768, least = 128;
     else if (f.folded) target = 512, least = 256;
     int64_t n = target / blocks;
     if (n > (rows + least - 1) / least) n = (rows + least - 1) / least;

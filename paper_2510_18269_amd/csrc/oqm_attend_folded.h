@@ -802,14 +802,14 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
 
     const int32_t stored_end = min(end, s.front_tiles + s.stored_tiles);
     if (from_in(s.front_tiles) < stored_end) {
+        char* const mine = lds + (NW == 1 ? wave * F::STAGE : 0);
+        typename F::Fetch next;
+        int32_t t = from_in(s.front_tiles);
+        F::fetch(g, head, t - s.front_tiles, next);  // the first tile is on its way while the queries are read
         typename F::Query query;
 #pragma unroll
         for (int m = 0; m < MT; ++m) F::load(g, g.q + q_head[m] * g.q_head + token[m] * g.q_row, there[m], m, query);
         f.template rescale<true>();
-        char* const mine = lds + (NW == 1 ? wave * F::STAGE : 0);
-        typename F::Fetch next;
-        int32_t t = from_in(s.front_tiles);
-        F::fetch(g, head, t - s.front_tiles, next);
         for (int buffer = 0; t < stored_end; t += kStep, buffer ^= 1) {
             char* const here = mine + (NW == 1 ? 0 : buffer * F::STAGE);
             const uint64_t valid = next.valid;

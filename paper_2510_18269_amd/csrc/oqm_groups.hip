@@ -24,11 +24,14 @@ struct GroupArgs {
 // A workgroup holds a strip of columns of a plane and walks its part of the list from the front: kAhead pieces a lane are read,
 // then written.  In place (the list ascends, so idx[i] >= i) this needs no second copy of anything: a strip belongs to one
 // workgroup, which writes slot i only after every list entry up to the end of its batch has been read, and later batches read
-// slots from their own position in the list up, which no earlier batch writes.  28 layers x 128 groups of 196 tokens, 96 of them
-// kept, 8 pieces of 16 bytes a lane.
-constexpr int kAhead = 8;
+// slots from their own position in the list up, which no earlier batch writes.  Where a lane has its column to itself nobody else
+// touches it, and the wave's own order is enough.
+// 96 of 128 groups of 196 tokens in 28 layers kept (685 MB), us: workgroups of 256 lanes with a barrier in every batch 142 (8
+// pieces), 168 (4), 198 (16); without 131; of 128 lanes 128.5; of 64 125.8 = 5.4 TB/s; the same with loads past the caches 134,
+// with stores that stay in them 141.
+constexpr int kAhead = 8, kMoveBlock = 64;
 template <typename PIECE, bool IN_PLACE>
-__global__ __launch_bounds__(kBlock) void move_groups_kernel(GroupArgs g) {
+__global__ __launch_bounds__(kMoveBlock) void move_groups_kernel(GroupArgs g) {
     uint32_t w = 0;
     if (blockIdx.x >= g.a[1].first_block) w = 1;
     if (blockIdx.x >= g.a[2].first_block) w = 2;
@@ -36,7 +39,7 @@ __global__ __launch_bounds__(kBlock) void move_groups_kernel(GroupArgs g) {
     const uint32_t block = blockIdx.x - a.first_block;
     const uint32_t plane = block / a.col_blocks, strip = block % a.col_blocks;
     const uint32_t col = (strip << a.col_log2) + (threadIdx.x & ((1u << a.col_log2) - 1u));
-    const uint32_t rows = kBlock >> a.col_log2;  // of the list at a time
+    const uint32_t rows = kMoveBlock >> a.col_log2;  // of the list at a time
     const bool there = col < a.cols;
     const char* from = a.from + plane * a.from_plane + (int64_t)col * sizeof(PIECE);
     char* to = a.to + plane * a.to_plane + (int64_t)col * sizeof(PIECE);
@@ -52,10 +55,10 @@ __global__ __launch_bounds__(kBlock) void move_groups_kernel(GroupArgs g) {
             int32_t slot = -1;
             if (there && r < end) slot = g.idx[r];
             moves[u] = slot >= 0 && slot < g.n_groups && !(IN_PLACE && slot == r);
-            if (moves[u]) piece[u] = __builtin_nontemporal_load(reinterpret_cast<const PIECE*>(from + (int64_t)slot * a.slot_bytes));
+            if (moves[u]) piece[u] = *reinterpret_cast<const PIECE*>(from + (int64_t)slot * a.slot_bytes);
         }
-        if constexpr (IN_PLACE) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what other lanes of the workgroup are about to overwrite has arrived
+        if (IN_PLACE && rows > 1) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what other lanes are about to overwrite has arrived
             __syncthreads();
         }
 #pragma unroll
@@ -97,7 +100,7 @@ hipError_t launch_move_groups(const tom_oqm_t& to, const tom_oqm_t& from, const 
         a.to_plane = (int64_t)bytes[i] * to.cfg.capacity_groups;
         if (bytes[i] / piece > 0x7fffffffu) return hipErrorInvalidConfiguration;
         a.cols = (uint32_t)(bytes[i] / piece);
-        while (a.col_log2 < 8 && (1u << a.col_log2) < a.cols) ++a.col_log2;
+        while ((1 << a.col_log2) < kMoveBlock && (1u << a.col_log2) < a.cols) ++a.col_log2;
         a.col_blocks = (a.cols + (1u << a.col_log2) - 1) >> a.col_log2;
         a.first_block = (uint32_t)blocks;
         blocks += planes * a.col_blocks;
@@ -110,7 +113,7 @@ hipError_t launch_move_groups(const tom_oqm_t& to, const tom_oqm_t& from, const 
         while (((uint32_t)n + g.rows_per_block - 1) / g.rows_per_block > 65535u) g.rows_per_block *= 2;
         parts = ((uint32_t)n + g.rows_per_block - 1) / g.rows_per_block;
     }
-    const dim3 grid((uint32_t)blocks, parts), block(kBlock);
+    const dim3 grid((uint32_t)blocks, parts), block(kMoveBlock);
     if (piece == 16) launch(move_groups_kernel<piece16, IN_PLACE>, grid, block, 0, s, g);
     else if (piece == 8) launch(move_groups_kernel<piece8, IN_PLACE>, grid, block, 0, s, g);
     else if (piece == 4) launch(move_groups_kernel<uint32_t, IN_PLACE>, grid, block, 0, s, g);

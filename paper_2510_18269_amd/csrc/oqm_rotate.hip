@@ -36,19 +36,27 @@ struct RotateArgs {
 };
 
 template <typename E, int V>
-__device__ __forceinline__ void load_elements(const char* p, float (&x)[V]) {
+struct Elements {  // as they are in memory: a load is not waited for until they are widened
     typedef E Vec __attribute__((ext_vector_type(V)));
-    const Vec r = *reinterpret_cast<const Vec*>(p);
+    Vec r;
+    template <bool PAST_CACHES>
+    __device__ __forceinline__ void load(const char* p) {
+        if constexpr (PAST_CACHES) r = __builtin_nontemporal_load(reinterpret_cast<const Vec*>(p));
+        else r = *reinterpret_cast<const Vec*>(p);
+    }
+    __device__ __forceinline__ void widen(float (&x)[V]) const {
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = (float)r[i];
-}
-template <typename E, int V>
+        for (int i = 0; i < V; ++i) x[i] = (float)r[i];
+    }
+};
+template <typename E, int V, bool PAST_CACHES>
 __device__ __forceinline__ void store_elements(char* p, const float (&x)[V]) {
     typedef E Vec __attribute__((ext_vector_type(V)));
     Vec r;
 #pragma unroll
     for (int i = 0; i < V; ++i) r[i] = (E)x[i];
-    *reinterpret_cast<Vec*>(p) = r;
+    if constexpr (PAST_CACHES) __builtin_nontemporal_store(r, reinterpret_cast<Vec*>(p));
+    else *reinterpret_cast<Vec*>(p) = r;
 }
 
 // Cosine and sine of `turn` whole turns.  The nearest quarter turn is taken off in float64, so that what remains, at most an
@@ -70,7 +78,7 @@ __device__ __forceinline__ void cos_sin_turns(double turn, float& c, float& s) {
 
 // A head is held by 2^lanes_log2 lanes of 2 V channels each: V pairs that turn (two runs of V channels half the rotary part
 // apart, or one of 2 V), or 2 V channels behind them.  WIDE: more than a wave, and the sums of a norm are joined in LDS.
-template <typename T, int V, bool PAIRS, bool WIDE>
+template <typename T, int V, bool PAIRS, bool WIDE, bool PAST_CACHES>
 __global__ __launch_bounds__(WIDE ? 1024 : kBlock) void rotate_kernel(RotateArgs g) {
     typedef typename Element<T>::type E;
     const uint32_t lanes = 1u << g.lanes_log2;
@@ -116,14 +124,18 @@ __global__ __launch_bounds__(WIDE ? 1024 : kBlock) void rotate_kernel(RotateArgs
                 w = 2;
             }
         }
-        const RotateSide& d = g.side[w];
+        const RotateSide d = w == 0 ? g.side[0] : w == 1 ? g.side[1] : g.side[2];  // selected: an index would be a load
         const char* in = d.in + head * d.in_head + token * d.in_row;
+        Elements<E, V> raw[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (has[j]) raw[j].template load<PAST_CACHES>(in + (int64_t)at[j] * sizeof(E));
         float x[2][V];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
             for (int i = 0; i < V; ++i) x[j][i] = 0.0f;
-            if (has[j]) load_elements<E, V>(in + (int64_t)at[j] * sizeof(E), x[j]);
+            if (has[j]) raw[j].widen(x[j]);
         }
         if (d.norm) {
             float sum = 0.0f;
@@ -144,10 +156,12 @@ __global__ __launch_bounds__(WIDE ? 1024 : kBlock) void rotate_kernel(RotateArgs
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 if (!has[j]) continue;
-                float weight[V];
-                load_elements<E, V>(d.norm + (int64_t)at[j] * sizeof(E), weight);
+                Elements<E, V> weight;
+                weight.template load<false>(d.norm + (int64_t)at[j] * sizeof(E));
+                float by[V];
+                weight.widen(by);
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[j][i] = x[j][i] * r * weight[i];
+                for (int i = 0; i < V; ++i) x[j][i] = x[j][i] * r * by[i];
             }
         }
         if (turns && d.turned) {
@@ -163,19 +177,24 @@ __global__ __launch_bounds__(WIDE ? 1024 : kBlock) void rotate_kernel(RotateArgs
         char* out = d.out + head * d.out_head + token * d.out_row;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            if (has[j]) store_elements<E, V>(out + (int64_t)at[j] * sizeof(E), x[j]);
+            if (has[j]) store_elements<E, V, PAST_CACHES>(out + (int64_t)at[j] * sizeof(E), x[j]);
     }
 }
 
-template <typename T, int V>
-void start_rotate(const RotateArgs& g, bool pairs, bool wide, dim3 grid, dim3 block, hipStream_t s) {
-    if (wide) {
-        if (pairs) launch(rotate_kernel<T, V, true, true>, grid, block, 0, s, g);
-        else launch(rotate_kernel<T, V, false, true>, grid, block, 0, s, g);
+template <typename T, int V, bool PAIRS>
+void start_rotate_of(const RotateArgs& g, bool wide, bool large, dim3 grid, dim3 block, hipStream_t s) {
+    if (wide) launch(rotate_kernel<T, V, PAIRS, true, false>, grid, block, 0, s, g);
+    else if constexpr (V * elem_bytes<T>::value == 16) {
+        if (large) launch(rotate_kernel<T, V, PAIRS, false, true>, grid, block, 0, s, g);
+        else launch(rotate_kernel<T, V, PAIRS, false, false>, grid, block, 0, s, g);
     } else {
-        if (pairs) launch(rotate_kernel<T, V, true, false>, grid, block, 0, s, g);
-        else launch(rotate_kernel<T, V, false, false>, grid, block, 0, s, g);
+        launch(rotate_kernel<T, V, PAIRS, false, false>, grid, block, 0, s, g);
     }
+}
+template <typename T, int V>
+void start_rotate(const RotateArgs& g, bool pairs, bool wide, bool large, dim3 grid, dim3 block, hipStream_t s) {
+    if (pairs) start_rotate_of<T, V, true>(g, wide, large, grid, block, s);
+    else start_rotate_of<T, V, false>(g, wide, large, grid, block, s);
 }
 
 static int bytes_of(int32_t dtype) { return dtype == TOM_F32 ? 4 : 2; }
@@ -310,9 +329,10 @@ tom_status_t tom_oqm_rotate(const tom_oqm_rotary_t* r, const double* turns, floa
     g.rotary_dim = r->rotary_dim;
     g.pair_slots = pair_slots;
     g.heads = (uint32_t)heads;
-    // Heads a lane takes one after the other share its cosines; small calls take one, so that every head has lanes of its own.
+    // Heads a lane takes one after the other share its cosines; small calls take one, so that every head has lanes of its own.  The
+    // same 719 MB, us at 2 / 4 / 8 / 16 heads: 126.7 / 123.2 / 135.5 / 161.
     g.heads_per_lane = 1;
-    while (g.heads_per_lane < 8 && (uint64_t)one->rows * heads * lanes / g.heads_per_lane > 512u * 1024u) g.heads_per_lane *= 2;
+    while (g.heads_per_lane < 4 && (uint64_t)one->rows * heads * lanes / g.heads_per_lane > 512u * 1024u) g.heads_per_lane *= 2;
     g.parts = (g.heads + g.heads_per_lane - 1) / g.heads_per_lane;
     g.token_fast = one->row_stride < one->head_stride;
     g.fast = g.token_fast ? (uint32_t)one->rows : g.parts;
@@ -320,22 +340,25 @@ tom_status_t tom_oqm_rotate(const tom_oqm_rotary_t* r, const double* turns, floa
     g.sets = (uint64_t)g.parts * (uint64_t)one->rows;
     const uint32_t sets_per_block = threads / lanes;
     const dim3 grid((uint32_t)((g.sets + sets_per_block - 1) / sets_per_block)), block(threads);
+    // Rows that the last-level cache (256 MB) cannot hold until somebody reads them are read and written past the caches.  28 layers x
+    // 4 heads x 12544 tokens of 128 channels (719 MB), us, through / past: 138 / 123.2 = 5.8 TB/s.
+    const bool large = (uint64_t)one->rows * (uint64_t)heads * (uint64_t)one->channels * (uint64_t)e * 2 >= (uint64_t)256 << 20;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's
     if (e == 4) {
-        if (vec == 4) start_rotate<In_f32, 4>(g, pairs, wide, grid, block, s);
-        else if (vec == 2) start_rotate<In_f32, 2>(g, pairs, wide, grid, block, s);
-        else start_rotate<In_f32, 1>(g, pairs, wide, grid, block, s);
+        if (vec == 4) start_rotate<In_f32, 4>(g, pairs, wide, large, grid, block, s);
+        else if (vec == 2) start_rotate<In_f32, 2>(g, pairs, wide, large, grid, block, s);
+        else start_rotate<In_f32, 1>(g, pairs, wide, large, grid, block, s);
     } else if (one->dtype == TOM_BF16) {
-        if (vec == 8) start_rotate<In_bf16, 8>(g, pairs, wide, grid, block, s);
-        else if (vec == 4) start_rotate<In_bf16, 4>(g, pairs, wide, grid, block, s);
-        else if (vec == 2) start_rotate<In_bf16, 2>(g, pairs, wide, grid, block, s);
-        else start_rotate<In_bf16, 1>(g, pairs, wide, grid, block, s);
+        if (vec == 8) start_rotate<In_bf16, 8>(g, pairs, wide, large, grid, block, s);
+        else if (vec == 4) start_rotate<In_bf16, 4>(g, pairs, wide, large, grid, block, s);
+        else if (vec == 2) start_rotate<In_bf16, 2>(g, pairs, wide, large, grid, block, s);
+        else start_rotate<In_bf16, 1>(g, pairs, wide, large, grid, block, s);
     } else {
-        if (vec == 8) start_rotate<In_f16, 8>(g, pairs, wide, grid, block, s);
-        else if (vec == 4) start_rotate<In_f16, 4>(g, pairs, wide, grid, block, s);
-        else if (vec == 2) start_rotate<In_f16, 2>(g, pairs, wide, grid, block, s);
-        else start_rotate<In_f16, 1>(g, pairs, wide, grid, block, s);
+        if (vec == 8) start_rotate<In_f16, 8>(g, pairs, wide, large, grid, block, s);
+        else if (vec == 4) start_rotate<In_f16, 4>(g, pairs, wide, large, grid, block, s);
+        else if (vec == 2) start_rotate<In_f16, 2>(g, pairs, wide, large, grid, block, s);
+        else start_rotate<In_f16, 1>(g, pairs, wide, large, grid, block, s);
     }
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return fail(TOM_ERR_HIP, "rotate launch: %s", hipGetErrorString(err));
