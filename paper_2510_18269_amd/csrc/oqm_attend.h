@@ -50,14 +50,17 @@ struct AttendArgs {
     char* out;
     float* lse;
     float* part_out;       // [H_q * t_q][splits][d], not normalised; NULL with one split
-    f32pair* part_stat;    // [H_q * t_q][splits]: maximum (in units of log 2) and sum
+    f32pair* part_stat;    // [H_q * t_q][splits]: maximum (a score) and sum
     int64_t q_head, q_row, out_head, out_row;            // bytes
     int32_t k_eff, n_groups, group_tokens, channels, qgroup_log2;
     int32_t t_q, repeat, kv_heads;  // repeat: query heads of a KV head
     int32_t causal, token_axis, bits, meta_bf16;
     uint32_t inv_group_tokens, inv_repeat;
-    float scale_log2;      // scale * log2(e); with a cap: 2 log2(e) scale / softcap
+    // Scores are counted in units of log 2 / score_unit: 1, but in the general form without a cap, which takes the maximum off before it
+    // multiplies, so that large scores keep their last bits.
+    float scale_log2;      // from dots to scores; with a cap: to the exponent of the tanh, 2 log2(e) scale / softcap
     float cap_log2;        // softcap * log2(e), or 0
+    float score_unit;
     int32_t splits, row_blocks;
 };
 
@@ -83,7 +86,7 @@ inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
 inline int32_t attend_cuts(const tom_oqm_config_t& c, int32_t t_q, int64_t rows) {
     const AttendForm f = attend_form(c, t_q);
     const int64_t blocks = ((int64_t)(c.n_q_heads / c.n_kv_heads) * t_q + f.rows - 1) / f.rows * c.n_kv_heads;
-    int64_t target = 2048, least = 64;  // waves: two a SIMD
+    int64_t target = 2048, least = 32;  // waves: two a SIMD
     if (f.folded && f.rows == 16) target = 768, least = 128;
     else if (f.folded) target = 512, least = 256;
     int64_t n = target / blocks;

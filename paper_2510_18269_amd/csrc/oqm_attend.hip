@@ -9,160 +9,311 @@
 
 namespace oqm {
 
-__device__ __forceinline__ f32x2 load_pair(const char* meta, int64_t i, bool bf16) {
-    if (bf16) return widen_pair(reinterpret_cast<const uint32_t*>(meta)[i]);
-    return reinterpret_cast<const f32x2*>(meta)[i];
-}
-
-// N consecutive channels from c of token `tok` of a stored head tile.
-template <int N>
-__device__ __forceinline__ void load_stored(const AttendArgs& g, const char* codes, const char* meta, uint32_t tok, int c, float* x) {
-    const int64_t first = ((int64_t)tok * g.channels + c) * g.bits / 8;
-    uint32_t w;
-    if (g.bits == 4) w = N == 8 ? *reinterpret_cast<const uint32_t*>(codes + first) : *reinterpret_cast<const uint16_t*>(codes + first);
-    else w = N == 8 ? *reinterpret_cast<const uint16_t*>(codes + first) : *reinterpret_cast<const uint8_t*>(codes + first);
-    const uint32_t mask = g.bits == 4 ? 15u : 3u;
-    if (g.token_axis) {
+// Codes and pairs of N (4 or 8) channels as they are in memory.  Branch-free whatever their widths, so that the loads of a tile are
+// on their way together: codes are read as the aligned 32 bits that hold them (an array is a multiple of 4 bytes long), bfloat16
+// pairs as the same 32 bits twice.
+template <int N, bool TOKEN_AXIS>
+struct Stored {
+    static constexpr int NP = TOKEN_AXIS ? N : 1;
+    uint32_t w, shift;
+    __device__ __forceinline__ void load(const AttendArgs& g, const char* codes, uint32_t tok, int c) {
+        const uint64_t at = reinterpret_cast<uint64_t>(codes) + ((uint64_t)tok * (uint32_t)g.channels + (uint32_t)c) * (uint32_t)g.bits / 8;
+        w = *reinterpret_cast<const uint32_t*>(at & ~uint64_t{3});
+        shift = (uint32_t)(at & 3u) * 8u;
+    }
+    __device__ __forceinline__ void values(const AttendArgs& g, const f32x2 (&pair)[NP], float* x) const {
+        const uint32_t v = w >> shift, mask = g.bits == 4 ? 15u : 3u;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const f32x2 p = load_pair(meta, c + i, g.meta_bf16 != 0);
-            x[i] = __builtin_fmaf((float)((w >> (g.bits * i)) & mask), p[0], p[1]);
+            const f32x2 p = pair[TOKEN_AXIS ? i : 0];
+            x[i] = __builtin_fmaf((float)((v >> (g.bits * i)) & mask), p[0], p[1]);
         }
-    } else {
-        const f32x2 p = load_pair(meta, ((int64_t)tok * g.channels + c) >> g.qgroup_log2, g.meta_bf16 != 0);
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = __builtin_fmaf((float)((w >> (g.bits * i)) & mask), p[0], p[1]);
     }
-}
-
-// Where a token of the groups' rows stands: its slot (-1: a hole, or no token) and its row in the group.
-__device__ __forceinline__ int32_t locate(const AttendArgs& g, int32_t token, int32_t tokens, uint32_t& tok) {
-    tok = 0;
-    if (token >= tokens) return -1;
-    const uint32_t rank = div_by((uint32_t)token, (uint32_t)g.group_tokens, g.inv_group_tokens);
-    tok = (uint32_t)token - rank * (uint32_t)g.group_tokens;
-    const int32_t slot = g.idx ? g.idx[rank] : (int32_t)rank;
-    return slot >= 0 && slot < g.n_groups ? slot : -1;
-}
+};
+struct StoredPair {
+    uint32_t first, second;
+    __device__ __forceinline__ void load(const AttendArgs& g, const char* meta, uint64_t i) {
+        const char* p = meta + (g.meta_bf16 ? 4 : 8) * i;
+        first = *reinterpret_cast<const uint32_t*>(p);
+        second = *reinterpret_cast<const uint32_t*>(p + (g.meta_bf16 ? 0 : 4));
+    }
+    // of a token that is not there: zero, whatever has been read
+    __device__ __forceinline__ f32x2 get(const AttendArgs& g, bool there) const {
+        const uint32_t s = g.meta_bf16 ? first << 16 : first, m = g.meta_bf16 ? first & 0xffff0000u : second;
+        return f32x2{__uint_as_float(there ? s : 0u), __uint_as_float(there ? m : 0u)};
+    }
+};
 
 // ---- general form ------------------------------------------------------------------------------------------------------------
 // A wave takes 16 query rows of a KV head and a run of 32-token tiles, on its own: every element is reconstructed (or widened) to
 // float32 and enters the products in two 16-bit parts where one does not hold it.  DP: channels, padded with zeros.
 //   K operand  lane (token l % 16 of a half, quarter l / 16): DP / 4 consecutive channels
 //   V operand  lane (l % 16, l / 16): of the 8 tokens whose scores it holds, VN runs of VU channels
-template <typename T, int DP>
+// Along the tokens' axis a tile lies in one group, whose pairs a lane then reads once.  Where a tile's channels are padding or a
+// token is not there, what is read instead is some valid place, and not used.
+template <typename T, int DP, bool TOKEN_AXIS>
 struct General {
     static constexpr int VU = DP / 16 < 8 ? DP / 16 : 8, VN = DP / 16 / VU, STEPS = DP / 32;
+    static constexpr bool EARLY = DP * elem_bytes<T>::value <= 256;  // the values' loads go out with the keys': there are registers for both
+    static constexpr bool LATE_PAIRS = TOKEN_AXIS && DP > 64;        // for so many pairs there are not
+    // A dot in float32 is added up in as many chains, joined by pairs: a chain of 64 products of four loses three times the last bits.
+    static constexpr int CHAINS = !__is_same(T, In_f32) ? 1 : STEPS < 4 ? STEPS : 4;
     Operand<T> q[STEPS];
     f32x4 o[DP / 16];
     float top, sum;
 
-    // STORED: a tile of the groups' rows; else of `r`.  `seen`: of the rows from the first, how many the lane's query row sees.
-    template <bool STORED>
-    __device__ __forceinline__ void tile(const AttendArgs& g, const AttendRows* r, int head, int32_t t0, int32_t tokens, int32_t seen) {
-        const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
-        const char *kc = nullptr, *km = nullptr, *vc = nullptr, *vm = nullptr;
-        if constexpr (STORED) {
-            kc = g.codes[0] + head * g.code_head;
-            vc = g.codes[1] + head * g.code_head;
-            km = g.meta[0] + head * g.meta_head;
-            vm = g.meta[1] + head * g.meta_head;
-        } else {
-            kc = r->k + head * r->k_head;
-            vc = r->v + head * r->v_head;
-        }
-        float w[8];
+    static __device__ __forceinline__ void join_chains(f32x4 (&s)[2][CHAINS]) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int32_t token = t0 + 16 * half + a;
-            uint32_t tok = 0;
-            int32_t slot = token < tokens ? token : -1;
-            if constexpr (STORED) slot = locate(g, token, tokens, tok);
-            f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int u = 0; u < STEPS; ++u) {
-                const int c = quarter * (DP / 4) + 8 * u;
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-                if (slot >= 0 && c < g.channels) {
-                    if constexpr (STORED) load_stored<8>(g, kc + slot * g.code_slot, km + slot * g.meta_slot, tok, c, x);
-                    else load_row<T, 8>(kc + slot * r->k_row + (int64_t)c * elem_bytes<T>::value, x);
-                }
-                Operand<T> hi, lo;
-                split(x, hi, lo);
-                s = product(hi, q[u], s);
-                if constexpr (STORED && !__is_same(T, In_f32)) s = product(lo, q[u], s);
-            }
-            const uint32_t there = (uint32_t)(__ballot(slot >= 0) & 0xffff);  // of the half's 16 tokens
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int j = 4 * quarter + i;
-                const float y = s[i] * g.scale_log2;
-                const float z = g.cap_log2 != 0.0f ? capped_exactly(y, g.cap_log2) : y;
-                w[4 * half + i] = (there >> j & 1u) && t0 + 16 * half + j < seen ? z : -__builtin_inff();
-            }
+            if constexpr (CHAINS == 2) s[half][0] += s[half][1];
+            if constexpr (CHAINS == 4) s[half][0] = (s[half][0] + s[half][1]) + (s[half][2] + s[half][3]);
         }
+    }
+    static __device__ __forceinline__ int32_t tiles(const AttendArgs& g) {
+        if constexpr (TOKEN_AXIS) return g.k_eff * ((g.group_tokens + kTile - 1) / kTile);
+        return (g.k_eff * g.group_tokens + kTile - 1) / kTile;
+    }
+
+    __device__ __forceinline__ void softmax(const AttendArgs& g, float (&w)[8]) {
         float high = w[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) high = fmaxf(high, w[i]);
-        high = fmaxf(high, __shfl_xor(high, 16, 64));
-        high = fmaxf(high, __shfl_xor(high, 32, 64));
         if (__any(high > top)) {
+            high = fmaxf(high, __shfl_xor(high, 16, 64));
+            high = fmaxf(high, __shfl_xor(high, 32, 64));
             const float next = fmaxf(top, high);
-            const float by = next == -__builtin_inff() ? 1.0f : exp2_of(top - next);
+            const float by = next == -__builtin_inff() ? 1.0f : exp2_of((top - next) * g.score_unit);
             top = next;
             sum *= by;
 #pragma unroll
             for (int n = 0; n < DP / 16; ++n) o[n] *= by;
         }
         const float from = top == -__builtin_inff() ? 0.0f : top;
-        float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            p[i] = exp2_of(w[i] - from);
-            sum += p[i];
+            w[i] = exp2_of((w[i] - from) * g.score_unit);
+            sum += w[i];
         }
+    }
+    __device__ __forceinline__ float score(const AttendArgs& g, float dot, bool seen) const {
+        const float y = dot * g.scale_log2;
+        const float z = g.cap_log2 != 0.0f ? capped_exactly(y, g.cap_log2) : y;
+        return seen ? z : -__builtin_inff();
+    }
+    // One block of the sums: values of the lane's 8 tokens in one channel.
+    template <bool EXACT>
+    __device__ __forceinline__ void add(f32x4& acc, const float (&y)[8], const Operand<T>& ph, const Operand<T>& pl) {
+        Operand<T> hi, lo;
+        split(y, hi, lo);
+        acc = product(hi, ph, acc);
+        if constexpr (!__is_same(T, In_f32)) {
+            acc = product(hi, pl, acc);
+            if constexpr (!EXACT) acc = product(lo, ph, acc);
+        }
+    }
+
+    __device__ __forceinline__ void stored(const AttendArgs& g, int head, int32_t t) {
+        const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
+        const char* const kc = g.codes[0] + head * g.code_head;
+        const char* const vc = g.codes[1] + head * g.code_head;
+        const char* const km = g.meta[0] + head * g.meta_head;
+        const char* const vm = g.meta[1] + head * g.meta_head;
+        // the tile's 32 tokens, one of each half a lane
+        int32_t slot[2], tok[2];
+        bool is[2];
+        if constexpr (TOKEN_AXIS) {
+            const int32_t parts = (g.group_tokens + kTile - 1) / kTile, rank = t / parts, first = (t - rank * parts) * kTile;
+            const int32_t s = g.idx ? g.idx[rank] : rank;
+            const bool there = s >= 0 && s < g.n_groups;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                slot[half] = there ? s : 0;
+                is[half] = there && first + 16 * half + a < g.group_tokens;
+                tok[half] = min(first + 16 * half + a, g.group_tokens - 1);
+            }
+        } else {
+            const int32_t tokens = g.k_eff * g.group_tokens;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int32_t token = min(t * kTile + 16 * half + a, tokens - 1);
+                const uint32_t rank = div_by((uint32_t)token, (uint32_t)g.group_tokens, g.inv_group_tokens);
+                tok[half] = token - (int32_t)(rank * (uint32_t)g.group_tokens);
+                const int32_t s = g.idx ? g.idx[rank] : (int32_t)rank;
+                is[half] = t * kTile + 16 * half + a < tokens && s >= 0 && s < g.n_groups;
+                slot[half] = s >= 0 && s < g.n_groups ? s : 0;
+            }
+        }
+        typedef Stored<8, TOKEN_AXIS> Key;
+        typedef Stored<VU, TOKEN_AXIS> Value;
+        Key kx[2][STEPS];
+        StoredPair kp[TOKEN_AXIS ? 1 : 2][LATE_PAIRS ? 1 : STEPS][Key::NP];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const int c = quarter * (DP / 4) + 8 * u, at = c < g.channels ? c : 0;
+                kx[half][u].load(g, kc + slot[half] * g.code_slot, (uint32_t)tok[half], at);
+                if constexpr (TOKEN_AXIS) {
+                    if (half == 0 && !LATE_PAIRS)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) kp[0][LATE_PAIRS ? 0 : u][i].load(g, km + slot[0] * g.meta_slot, (uint64_t)(at + i));
+                } else {
+                    kp[half][u][0].load(g, km + slot[half] * g.meta_slot, ((uint64_t)(uint32_t)tok[half] * (uint32_t)g.channels + (uint32_t)at) >> g.qgroup_log2);
+                }
+            }
+        // slots and rows of the tokens whose scores the lane holds
+        int32_t v_slot[8], v_tok[8];
+        uint32_t v_is = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v_slot[j] = __shfl(slot[j / 4], 4 * quarter + j % 4, 64);
+            v_tok[j] = __shfl(tok[j / 4], 4 * quarter + j % 4, 64);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) v_is |= (uint32_t)((__ballot(is[half]) >> (4 * quarter)) & 15u) << (4 * half);
+        Value vx[VN][8];
+        StoredPair vp[VN][TOKEN_AXIS ? 1 : 8][Value::NP];
+        auto load_values = [&] {
+#pragma unroll
+            for (int v = 0; v < VN; ++v) {
+                const int c = v * 16 * VU + a * VU, at = c < g.channels ? c : 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    vx[v][j].load(g, vc + v_slot[j] * g.code_slot, (uint32_t)v_tok[j], at);
+                    if constexpr (TOKEN_AXIS) {
+                        if (j == 0)
+#pragma unroll
+                            for (int i = 0; i < VU; ++i) vp[v][0][i].load(g, vm + v_slot[0] * g.meta_slot, (uint64_t)(at + i));
+                    } else {
+                        vp[v][j][0].load(g, vm + v_slot[j] * g.meta_slot, ((uint64_t)(uint32_t)v_tok[j] * (uint32_t)g.channels + (uint32_t)at) >> g.qgroup_log2);
+                    }
+                }
+            }
+        };
+        if constexpr (EARLY) load_values();
+        float w[8];
+        f32x4 s[2][CHAINS];
+#pragma unroll
+        for (int i = 0; i < 2 * CHAINS; ++i) s[i / CHAINS][i % CHAINS] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) {
+            const int c = quarter * (DP / 4) + 8 * u;
+            const bool inside = c < g.channels;
+            if constexpr (LATE_PAIRS) {
+                asm volatile("" ::: "memory");  // not before they are wanted
+#pragma unroll
+                for (int i = 0; i < 8; ++i) kp[0][0][i].load(g, km + slot[0] * g.meta_slot, (uint64_t)((inside ? c : 0) + i));
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f32x2 pair[Key::NP];
+#pragma unroll
+                for (int i = 0; i < Key::NP; ++i) pair[i] = kp[TOKEN_AXIS ? 0 : half][LATE_PAIRS ? 0 : u][i].get(g, is[half] && inside);
+                float x[8];
+                kx[half][u].values(g, pair, x);
+                Operand<T> hi, lo;
+                split(x, hi, lo);
+                f32x4& d = s[half][u % CHAINS];
+                d = product(hi, q[u], d);
+                if constexpr (!__is_same(T, In_f32)) d = product(lo, q[u], d);
+            }
+        }
+        join_chains(s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = score(g, s[i / 4][0][i % 4], v_is >> i & 1u);
+        softmax(g, w);
+        if constexpr (!EARLY) load_values();
         Operand<T> ph, pl;
-        split(p, ph, pl);
+        split(w, ph, pl);
 #pragma unroll
         for (int v = 0; v < VN; ++v) {
-            const int c = v * 16 * VU + a * VU;
             float x[8][VU];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
+                f32x2 pair[Value::NP];
 #pragma unroll
-                for (int i = 0; i < VU; ++i) x[j][i] = 0.0f;
-                const int32_t token = t0 + 16 * (j / 4) + 4 * quarter + j % 4;
-                uint32_t tok = 0;
-                int32_t slot = token < tokens ? token : -1;
-                if constexpr (STORED) slot = locate(g, token, tokens, tok);
-                if (slot >= 0 && c < g.channels) {
-                    if constexpr (STORED) load_stored<VU>(g, vc + slot * g.code_slot, vm + slot * g.meta_slot, tok, c, x[j]);
-                    else load_row<T, VU>(vc + slot * r->v_row + (int64_t)c * elem_bytes<T>::value, x[j]);
-                }
+                for (int i = 0; i < Value::NP; ++i) pair[i] = vp[v][TOKEN_AXIS ? 0 : j][i].get(g, v_is >> j & 1u);
+                vx[v][j].values(g, pair, x[j]);
             }
 #pragma unroll
             for (int i = 0; i < VU; ++i) {
                 float y[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = x[j][i];
-                Operand<T> hi, lo;
-                split(y, hi, lo);
-                f32x4& acc = o[v * VU + i];
-                acc = product(hi, ph, acc);
-                if constexpr (!__is_same(T, In_f32)) {
-                    acc = product(hi, pl, acc);
-                    if constexpr (STORED) acc = product(lo, ph, acc);
-                }
+                add<false>(o[v * VU + i], y, ph, pl);
             }
         }
     }
+
+    // A tile of rows as the model has them, from t0; `seen`: of the rows from the first, how many the lane's query row sees.
+    __device__ __forceinline__ void rows(const AttendArgs& g, const AttendRows& r, int head, int32_t t0, int32_t tokens, int32_t seen) {
+        const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
+        const char* const k = r.k + head * r.k_head;
+        const char* const v = r.v + head * r.v_head;
+        constexpr int E = elem_bytes<T>::value;
+        Raw8<T> kx[2][STEPS];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                const int c = quarter * (DP / 4) + 8 * u;
+                load_raw(k + min(t0 + 16 * half + a, tokens - 1) * r.k_row + (int64_t)(c < g.channels ? c : 0) * E, kx[half][u]);
+            }
+        typedef uint32_t Run __attribute__((ext_vector_type(VU * E / 4)));
+        Run vx[VN][8];
+        auto load_values = [&] {
+#pragma unroll
+            for (int n = 0; n < VN; ++n)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int c = n * 16 * VU + a * VU;
+                    const char* p = v + min(t0 + 16 * (j / 4) + 4 * quarter + j % 4, tokens - 1) * r.v_row + (int64_t)(c < g.channels ? c : 0) * E;
+                    __builtin_memcpy(&vx[n][j], __builtin_assume_aligned(p, VU * E < 16 ? VU * E : 16), sizeof(Run));
+                }
+        };
+        if constexpr (EARLY) load_values();
+        float w[8];
+        f32x4 s[2][CHAINS];
+#pragma unroll
+        for (int i = 0; i < 2 * CHAINS; ++i) s[i / CHAINS][i % CHAINS] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                float x[8];
+                widen(kx[half][u], x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = quarter * (DP / 4) + 8 * u < g.channels ? x[i] : 0.0f;
+                Operand<T> hi, lo;
+                split(x, hi, lo);
+                s[half][u % CHAINS] = product(hi, q[u], s[half][u % CHAINS]);
+            }
+        join_chains(s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = score(g, s[i / 4][0][i % 4], t0 + 16 * (i / 4) + 4 * quarter + i % 4 < seen);
+        softmax(g, w);
+        if constexpr (!EARLY) load_values();
+        Operand<T> ph, pl;
+        split(w, ph, pl);
+#pragma unroll
+        for (int n = 0; n < VN; ++n)
+#pragma unroll
+            for (int i = 0; i < VU; ++i) {
+                float y[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (E == 4) y[j] = __uint_as_float(vx[n][j][i]);
+                    else if constexpr (__is_same(T, In_bf16)) y[j] = __uint_as_float(i % 2 ? vx[n][j][i / 2] & 0xffff0000u : vx[n][j][i / 2] << 16);
+                    else y[j] = (float)__builtin_bit_cast(_Float16, (uint16_t)(vx[n][j][i / 2] >> (16 * (i % 2))));
+                }
+                add<true>(o[n * VU + i], y, ph, pl);
+            }
+    }
 };
 
-template <typename T, int DP>
-__global__ __launch_bounds__(kBlock) void attend_kernel(AttendArgs g) {
-    typedef General<T, DP> Form;
+template <typename T, int DP, bool TOKEN_AXIS>
+__global__ __launch_bounds__(kBlock, DP == 64 ? (TOKEN_AXIS ? 2 : 3) : DP == 128 ? 2 : 1) void attend_kernel(AttendArgs g) {
+    typedef General<T, DP, TOKEN_AXIS> Form;
     const uint32_t item = blockIdx.x * (kBlock / 64) + threadIdx.x / 64;
     const uint32_t block = item % (uint32_t)g.row_blocks, rest = item / (uint32_t)g.row_blocks;
     const uint32_t cut = rest % (uint32_t)g.splits;
@@ -192,20 +343,17 @@ __global__ __launch_bounds__(kBlock) void attend_kernel(AttendArgs g) {
         split(x, f.q[u], unused);
     }
 
-    const int32_t stored = g.k_eff * g.group_tokens;
     const int32_t last_token = min((int32_t)block * 16 + 15, rows - 1) / g.repeat;
     int32_t recent = g.recent.rows;  // as far as any row of the block sees
     if (g.causal) recent = max(0, min(recent, last_token + 1 + g.recent.rows - g.t_q));
-    const int32_t seen = !there ? 0 : g.causal ? token + 1 + g.recent.rows - g.t_q : g.recent.rows;
-    const int32_t front_tiles = (g.front.rows + kTile - 1) / kTile, stored_tiles = (stored + kTile - 1) / kTile;
+    const int32_t seen = !there ? 0 : g.causal ? min(recent, token + 1 + g.recent.rows - g.t_q) : recent;
+    const int32_t front_tiles = (g.front.rows + kTile - 1) / kTile, stored_tiles = Form::tiles(g);
     const int32_t tiles = front_tiles + stored_tiles + (recent + kTile - 1) / kTile;
     const int32_t begin = (int32_t)((int64_t)tiles * cut / g.splits), end = (int32_t)((int64_t)tiles * (cut + 1) / g.splits);
-    for (int32_t t = begin; t < min(end, front_tiles); ++t)
-        f.template tile<false>(g, &g.front, head, t * kTile, g.front.rows, there ? g.front.rows : 0);
-    for (int32_t t = max(begin, front_tiles); t < min(end, front_tiles + stored_tiles); ++t)
-        f.template tile<true>(g, nullptr, head, (t - front_tiles) * kTile, stored, there ? stored : 0);
+    for (int32_t t = begin; t < min(end, front_tiles); ++t) f.rows(g, g.front, head, t * kTile, g.front.rows, g.front.rows);
+    for (int32_t t = max(begin, front_tiles); t < min(end, front_tiles + stored_tiles); ++t) f.stored(g, head, t - front_tiles);
     for (int32_t t = max(begin, front_tiles + stored_tiles); t < end; ++t)
-        f.template tile<false>(g, &g.recent, head, (t - front_tiles - stored_tiles) * kTile, recent, seen);
+        f.rows(g, g.recent, head, (t - front_tiles - stored_tiles) * kTile, recent, seen);
 
     float sum = f.sum;
     sum += __shfl_xor(sum, 16, 64);
@@ -238,7 +386,7 @@ __global__ __launch_bounds__(kBlock) void attend_kernel(AttendArgs g) {
         }
     if (quarter == 0) {
         if (g.splits > 1) g.part_stat[at * g.splits + cut] = f32pair{f.top, sum};
-        else if (g.lse) g.lse[at] = sum > 0.0f ? (f.top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
+        else if (g.lse) g.lse[at] = sum > 0.0f ? (f.top * g.score_unit + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
     }
 }
 
@@ -248,9 +396,9 @@ __global__ __launch_bounds__(kBlock) void attend_kernel(AttendArgs g) {
 struct Joined {
     float top = -__builtin_inff(), total = 0.0f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    __device__ __forceinline__ void add(float their_top, float their_total, const f32x4& their_sum) {
+    __device__ __forceinline__ void add(float unit, float their_top, float their_total, const f32x4& their_sum) {
         const float next = fmaxf(top, their_top), from = next == -__builtin_inff() ? 0.0f : next;
-        const float mine = exp2_of(top - from), theirs = exp2_of(their_top - from);
+        const float mine = exp2_of((top - from) * unit), theirs = exp2_of((their_top - from) * unit);
         top = next;
         total = total * mine + their_total * theirs;
         sum = sum * mine + their_sum * theirs;
@@ -266,7 +414,7 @@ __device__ __forceinline__ void put_joined(const AttendArgs& g, int64_t at, int 
 #pragma unroll
     for (int n = 0; n < 4; ++n) y[n] = (E)(j.sum[n] * by);
     *reinterpret_cast<Vec*>(g.out + q_head * g.out_head + token * g.out_row + (int64_t)c * sizeof(E)) = y;
-    if (c == 0 && g.lse) g.lse[at] = j.total > 0.0f ? (j.top + __builtin_amdgcn_logf(j.total)) * kLn2 : -__builtin_inff();
+    if (c == 0 && g.lse) g.lse[at] = j.total > 0.0f ? (j.top * g.score_unit + __builtin_amdgcn_logf(j.total)) * kLn2 : -__builtin_inff();
 }
 constexpr int kJoinAhead = 4;
 __device__ __forceinline__ Joined join_parts(const AttendArgs& g, int64_t at, int c, int first, int step) {
@@ -284,7 +432,7 @@ __device__ __forceinline__ Joined join_parts(const AttendArgs& g, int64_t at, in
         }
 #pragma unroll
         for (int u = 0; u < kJoinAhead; ++u)
-            if (s0 + u * step < g.splits) j.add(st[u].x, st[u].y, x[u]);
+            if (s0 + u * step < g.splits) j.add(g.score_unit, st[u].x, st[u].y, x[u]);
     }
     return j;
 }
@@ -311,7 +459,7 @@ __global__ __launch_bounds__(kBlock) void attend_join_many_kernel(AttendArgs g) 
         f32x4 sum;
 #pragma unroll
         for (int n = 0; n < 4; ++n) sum[n] = __shfl_xor(j.sum[n], m, 64);
-        j.add(top, total, sum);
+        j.add(g.score_unit, top, total, sum);
     }
     __shared__ float tops[kBlock / 64][kLanes], totals[kBlock / 64][kLanes];
     __shared__ f32x4 sums[kBlock / 64][kLanes];
@@ -323,7 +471,7 @@ __global__ __launch_bounds__(kBlock) void attend_join_many_kernel(AttendArgs g) 
     }
     __syncthreads();
     if (threadIdx.x >= kLanes || !there) return;
-    for (int w = 1; w < kBlock / 64; ++w) j.add(tops[w][lane], totals[w][lane], sums[w][lane]);
+    for (int w = 1; w < kBlock / 64; ++w) j.add(g.score_unit, tops[w][lane], totals[w][lane], sums[w][lane]);
     put_joined<T>(g, blockIdx.x, c, j);
 }
 // Up to this many parts a lane takes them all.
@@ -343,9 +491,9 @@ template <typename T>
 void start_general(const AttendArgs& g, hipStream_t s) {
     const uint64_t items = (uint64_t)g.row_blocks * (uint64_t)g.splits * (uint64_t)g.kv_heads;
     const dim3 grid((uint32_t)((items + kBlock / 64 - 1) / (kBlock / 64))), block(kBlock);
-    if (g.channels <= 64) launch(attend_kernel<T, 64>, grid, block, 0, s, g);
-    else if (g.channels <= 128) launch(attend_kernel<T, 128>, grid, block, 0, s, g);
-    else launch(attend_kernel<T, 256>, grid, block, 0, s, g);
+    if (g.channels <= 64) launch(g.token_axis ? attend_kernel<T, 64, true> : attend_kernel<T, 64, false>, grid, block, 0, s, g);
+    else if (g.channels <= 128) launch(g.token_axis ? attend_kernel<T, 128, true> : attend_kernel<T, 128, false>, grid, block, 0, s, g);
+    else launch(g.token_axis ? attend_kernel<T, 256, true> : attend_kernel<T, 256, false>, grid, block, 0, s, g);
 }
 
 hipError_t launch_attend(const AttendArgs& g, const AttendForm& form, int dtype, hipStream_t s) {

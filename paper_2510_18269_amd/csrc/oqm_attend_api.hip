@@ -1,5 +1,7 @@
 // Host side of tom_oqm_attend: validation, and how the call is cut over the chip.  Nothing here allocates device memory or
 // synchronises with the GPU.
+#include <cmath>
+
 #include "oqm_attend.h"
 
 namespace oqm {
@@ -130,6 +132,11 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
     a.meta_bf16 = c.meta_dtype == TOM_BF16;
     constexpr float kLog2e = 1.4426950408889634f;
     a.scale_log2 = softcap > 0.0f ? 2.0f * kLog2e * scale / softcap : scale * kLog2e;
+    a.score_unit = 1.0f;
+    if (!form.folded && softcap == 0.0f && scale != 0.0f) {
+        a.score_unit = std::fabs(a.scale_log2);
+        a.scale_log2 = scale > 0.0f ? 1.0f : -1.0f;
+    }
     a.cap_log2 = softcap * kLog2e;
     a.row_blocks = (a.repeat * t_q + form.rows - 1) / form.rows;
     (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's

@@ -29,9 +29,9 @@ struct GroupArgs {
 // 96 of 128 groups of 196 tokens in 28 layers kept (685 MB), us: workgroups of 256 lanes with a barrier in every batch 142 (8
 // pieces), 168 (4), 198 (16); without 131; of 128 lanes 128.5; of 64 125.8 = 5.4 TB/s; the same with loads past the caches 134,
 // with stores that stay in them 141.
-constexpr int kAhead = 8, kMoveBlock = 64;
+constexpr int kAhead = 8;
 template <typename PIECE, bool IN_PLACE>
-__global__ __launch_bounds__(kMoveBlock) void move_groups_kernel(GroupArgs g) {
+__global__ __launch_bounds__(1024) void move_groups_kernel(GroupArgs g) {
     uint32_t w = 0;
     if (blockIdx.x >= g.a[1].first_block) w = 1;
     if (blockIdx.x >= g.a[2].first_block) w = 2;
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kMoveBlock) void move_groups_kernel(GroupArgs g) {
     const uint32_t block = blockIdx.x - a.first_block;
     const uint32_t plane = block / a.col_blocks, strip = block % a.col_blocks;
     const uint32_t col = (strip << a.col_log2) + (threadIdx.x & ((1u << a.col_log2) - 1u));
-    const uint32_t rows = kMoveBlock >> a.col_log2;  // of the list at a time
+    const uint32_t rows = blockDim.x >> a.col_log2;  // of the list at a time
     const bool there = col < a.cols;
     const char* from = a.from + plane * a.from_plane + (int64_t)col * sizeof(PIECE);
     char* to = a.to + plane * a.to_plane + (int64_t)col * sizeof(PIECE);
@@ -89,6 +89,17 @@ hipError_t launch_move_groups(const tom_oqm_t& to, const tom_oqm_t& from, const 
     // The widest piece that divides a slot of every array (arrays start on 16 bytes): codes of 2 bits and 8 channels leave 2 bytes.
     const uint64_t all = bytes[0] | bytes[1] | bytes[2];
     const uint32_t piece = all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : all % 4 == 0 ? 4 : 2;
+    // In place, strips that are too few to fill the chip are walked by more lanes at a time: 1024 in a workgroup, on strips as narrow as
+    // the list needs to be read in one batch, but no narrower than 16 pieces.
+    uint32_t threads = 64, widest = 6;
+    if (IN_PLACE) {
+        uint64_t waves = 0;
+        for (int i = 0; i < 3; ++i) waves += (uint64_t)c.n_layers * (i < 2 ? 2 : 1) * ((bytes[i] / piece + 63) / 64);
+        if (waves < 1024 && n > kAhead) {
+            threads = 1024;
+            while (widest > 4 && (int64_t)(1024u >> widest) * kAhead < n) --widest;
+        }
+    }
     uint64_t blocks = 0;
     for (int i = 0; i < 3; ++i) {
         GroupArray& a = g.a[i];
@@ -100,7 +111,7 @@ hipError_t launch_move_groups(const tom_oqm_t& to, const tom_oqm_t& from, const 
         a.to_plane = (int64_t)bytes[i] * to.cfg.capacity_groups;
         if (bytes[i] / piece > 0x7fffffffu) return hipErrorInvalidConfiguration;
         a.cols = (uint32_t)(bytes[i] / piece);
-        while ((1 << a.col_log2) < kMoveBlock && (1u << a.col_log2) < a.cols) ++a.col_log2;
+        while (a.col_log2 < widest && (1u << a.col_log2) < a.cols) ++a.col_log2;
         a.col_blocks = (a.cols + (1u << a.col_log2) - 1) >> a.col_log2;
         a.first_block = (uint32_t)blocks;
         blocks += planes * a.col_blocks;
@@ -113,7 +124,7 @@ hipError_t launch_move_groups(const tom_oqm_t& to, const tom_oqm_t& from, const 
         while (((uint32_t)n + g.rows_per_block - 1) / g.rows_per_block > 65535u) g.rows_per_block *= 2;
         parts = ((uint32_t)n + g.rows_per_block - 1) / g.rows_per_block;
     }
-    const dim3 grid((uint32_t)blocks, parts), block(kMoveBlock);
+    const dim3 grid((uint32_t)blocks, parts), block(threads);
     if (piece == 16) launch(move_groups_kernel<piece16, IN_PLACE>, grid, block, 0, s, g);
     else if (piece == 8) launch(move_groups_kernel<piece8, IN_PLACE>, grid, block, 0, s, g);
     else if (piece == 4) launch(move_groups_kernel<uint32_t, IN_PLACE>, grid, block, 0, s, g);
