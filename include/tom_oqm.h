@@ -409,6 +409,9 @@ size_t tom_oqm_attend_workspace_bytes(const tom_oqm_t* h, int32_t t_q, int64_t r
  *   front_k .. recent_v  [H_k][rows][d] of cfg.out_dtype, both of a pair or neither (NULL or no rows)
  *   causal     non-zero: the last t_q recent rows are the new tokens' own, and token t sees the recent rows j with
  *              j <= t + recent - t_q (so none where that is negative); otherwise every token sees all
+ *              Keys that a token does not see may hold anything.  A value that is not finite, in a row that some
+ *              of the tokens see, is unspecified for those too that see none of the row.  No row behind the last
+ *              of a view is read.
  *   softcap    0: none
  *   lse        device float32 [H_q][t_q] or NULL: the natural logarithm of the sum of exp(w_j).  Where a token sees
  *              nothing its output is 0 and its lse -inf.

@@ -56,7 +56,8 @@ struct General {
     static constexpr int VU = DP / 16 < 8 ? DP / 16 : 8, VN = DP / 16 / VU, STEPS = DP / 32;
     static constexpr bool EARLY = DP * elem_bytes<T>::value <= 256;  // the values' loads go out with the keys': there are registers for both
     static constexpr bool LATE_PAIRS = TOKEN_AXIS && DP > 64;        // for so many pairs there are not
-    // A dot in float32 is added up in as many chains, joined by pairs: a chain of 64 products of four loses three times the last bits.
+    // A dot in float32 is added up in as many chains, joined by pairs: results of 256 channels with outlier keys 2.4e-6 from 64 bits with
+    // one chain, 1.2e-6 with four.
     static constexpr int CHAINS = !__is_same(T, In_f32) ? 1 : STEPS < 4 ? STEPS : 4;
     Operand<T> q[STEPS];
     f32x4 o[DP / 16];

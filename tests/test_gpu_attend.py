@@ -221,3 +221,43 @@ def test_graph_replays(oqm):
         torch.cuda.synchronize()
         assert torch.equal(out, eager) and torch.equal(lse, eager_lse)
     oqm.tom_oqm_destroy(h)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t_q", [1, 20])
+def test_what_nobody_sees_may_be_anything(oqm, dtype, t_q):
+    """NaN behind the last row of every view, in the pairs of groups that are not listed, in slots that holes would name, in
+    keys behind a token's own; outputs stay finite and as they were."""
+    t, H_k, R, d, G, T = H.DT[dtype][1], 2, 4, 128, 40, 6
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    cfg = oqm.make_config(1, H_k, H_k * R, d, G, 64, T + 2, in_dtype=H.DT[dtype][0], out_dtype=H.DT[dtype][0])
+    h = oqm.tom_oqm_create(cfg)
+    codes = torch.randint(0, 256, (1, 2, T + 2, H_k, G, d // 2), generator=g, device="cuda", dtype=torch.uint8)
+    meta = torch.rand((1, 2, T + 2, H_k, G * 2, 2), generator=g, device="cuda")
+    oqm.tom_oqm_bind(h, codes, meta, torch.empty(16, device="cuda"))
+    oqm.tom_oqm_set_num_groups(h, T)
+    rows = [torch.randn((H_k, 64, d), generator=g, device="cuda").to(t) for _ in range(4)]
+    q = torch.randn((H_k * R, t_q, d), generator=g, device="cuda").to(t)
+    idx = torch.tensor([4, -1, 1, T, 5], dtype=torch.int32, device="cuda")
+    ws = torch.empty(oqm.tom_oqm_attend_workspace_bytes(h, t_q, 17 + 5 * G + 30), dtype=torch.uint8, device="cuda")
+    got = []
+    for spoil in (False, True):
+        if spoil:
+            for x in rows[:2]:
+                x[:, 17:] = math.nan
+            for x in rows[2:]:
+                x[:, 30:] = math.nan
+            for slot in (0, 2, 3, T, T + 1):
+                meta[:, :, slot] = math.nan
+            if t_q > 1:
+                rows[2][:, 29] = math.nan        # the last token's own key: the others do not see it
+        out = torch.zeros((H_k * R, t_q, d), dtype=t, device="cuda")
+        lse = torch.zeros((H_k * R, t_q), device="cuda")
+        oqm.tom_oqm_attend(h, 0, q, out, idx, 5, rows[0][:, :17], rows[1][:, :17], rows[2][:, :30], rows[3][:, :30], lse=lse, workspace=ws)
+        torch.cuda.synchronize()
+        got.append((out, lse))
+    seen = slice(None) if t_q == 1 else slice(0, t_q - 1)
+    assert bool(got[0][0].isfinite().all()) and bool(got[0][1].isfinite().all())
+    assert torch.equal(got[0][0][:, seen], got[1][0][:, seen]) and torch.equal(got[0][1][:, seen], got[1][1][:, seen])
+    oqm.tom_oqm_destroy(h)
