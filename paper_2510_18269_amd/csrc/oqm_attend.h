@@ -55,7 +55,7 @@ struct AttendArgs {
     int32_t k_eff, n_groups, group_tokens, channels, qgroup_log2;
     int32_t t_q, repeat, kv_heads;  // repeat: query heads of a KV head
     int32_t causal, token_axis, bits, meta_bf16;
-    uint32_t inv_group_tokens, inv_repeat;
+    uint32_t inv_group_tokens, inv_repeat, inv_splits, inv_row_blocks;  // of reciprocal_u32
     // Scores are counted in units of log 2 / score_unit: 1, but in the general form without a cap, which takes the maximum off before it
     // multiplies, so that large scores keep their last bits.
     float scale_log2;      // from dots to scores; with a cap: to the exponent of the tanh, 2 log2(e) scale / softcap

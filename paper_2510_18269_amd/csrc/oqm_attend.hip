@@ -315,15 +315,14 @@ struct General {
 template <typename T, int DP, bool TOKEN_AXIS>
 __global__ __launch_bounds__(kBlock, DP == 64 ? (TOKEN_AXIS ? 2 : 3) : DP == 128 ? 2 : 1) void attend_kernel(AttendArgs g) {
     typedef General<T, DP, TOKEN_AXIS> Form;
-    const uint32_t item = blockIdx.x * (kBlock / 64) + threadIdx.x / 64;
-    const uint32_t block = item % (uint32_t)g.row_blocks, rest = item / (uint32_t)g.row_blocks;
-    const uint32_t cut = rest % (uint32_t)g.splits;
-    const int head = (int)(rest / (uint32_t)g.splits);
+    const Item item = item_of(g, (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * (kBlock / 64) + threadIdx.x / 64)));
+    const uint32_t cut = item.cut;
+    const int head = item.head;
     if (head >= g.kv_heads) return;
     const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
     // query rows of a KV head: token-major, so that a block of them ends at about one token
     const int32_t rows = g.t_q * g.repeat;
-    const int32_t row = (int32_t)block * 16 + a;
+    const int32_t row = (int32_t)item.block * 16 + a;
     const bool there = row < rows;
     const int32_t token = there ? (int32_t)div_by((uint32_t)row, (uint32_t)g.repeat, g.inv_repeat) : 0;
     const int32_t q_head = head * g.repeat + (there ? row - token * g.repeat : 0);
@@ -344,17 +343,12 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? (TOKEN_AXIS ? 2 : 3) : DP == 128
         split(x, f.q[u], unused);
     }
 
-    const int32_t last_token = min((int32_t)block * 16 + 15, rows - 1) / g.repeat;
-    int32_t recent = g.recent.rows;  // as far as any row of the block sees
-    if (g.causal) recent = max(0, min(recent, last_token + 1 + g.recent.rows - g.t_q));
+    const Segments s = segments_of(g, min((int32_t)item.block * 16 + 15, rows - 1), cut, kTile, Form::tiles(g));
+    const int32_t recent = s.recent_rows, stored_end = s.front_tiles + s.stored_tiles;
     const int32_t seen = !there ? 0 : g.causal ? min(recent, token + 1 + g.recent.rows - g.t_q) : recent;
-    const int32_t front_tiles = (g.front.rows + kTile - 1) / kTile, stored_tiles = Form::tiles(g);
-    const int32_t tiles = front_tiles + stored_tiles + (recent + kTile - 1) / kTile;
-    const int32_t begin = (int32_t)((int64_t)tiles * cut / g.splits), end = (int32_t)((int64_t)tiles * (cut + 1) / g.splits);
-    for (int32_t t = begin; t < min(end, front_tiles); ++t) f.rows(g, g.front, head, t * kTile, g.front.rows, g.front.rows);
-    for (int32_t t = max(begin, front_tiles); t < min(end, front_tiles + stored_tiles); ++t) f.stored(g, head, t - front_tiles);
-    for (int32_t t = max(begin, front_tiles + stored_tiles); t < end; ++t)
-        f.rows(g, g.recent, head, (t - front_tiles - stored_tiles) * kTile, recent, seen);
+    for (int32_t t = s.begin; t < min(s.end, s.front_tiles); ++t) f.rows(g, g.front, head, t * kTile, g.front.rows, g.front.rows);
+    for (int32_t t = max(s.begin, s.front_tiles); t < min(s.end, stored_end); ++t) f.stored(g, head, t - s.front_tiles);
+    for (int32_t t = max(s.begin, stored_end); t < s.end; ++t) f.rows(g, g.recent, head, (t - stored_end) * kTile, recent, seen);
 
     float sum = f.sum;
     sum += __shfl_xor(sum, 16, 64);

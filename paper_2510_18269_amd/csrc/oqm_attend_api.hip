@@ -139,6 +139,8 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
     }
     a.cap_log2 = softcap * kLog2e;
     a.row_blocks = (a.repeat * t_q + form.rows - 1) / form.rows;
+    a.inv_row_blocks = reciprocal_u32((uint32_t)a.row_blocks);
+    a.inv_splits = reciprocal_u32((uint32_t)a.splits);
     (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's
     const hipError_t err = launch_attend(a, form, c.out_dtype, static_cast<hipStream_t>(hip_stream));
     if (err != hipSuccess) return fail(TOM_ERR_HIP, "attend launch: %s", hipGetErrorString(err));

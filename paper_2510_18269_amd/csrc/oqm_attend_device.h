@@ -101,4 +101,32 @@ __device__ __forceinline__ void load_row(const char* p, float* x) {
     }
 }
 
+// Which block of query rows, part and KV head a number of the grid (or of a grid's waves) stands for.
+struct Item {
+    uint32_t block, cut;
+    int head;
+};
+__device__ __forceinline__ Item item_of(const AttendArgs& g, uint32_t i) {
+    const uint32_t rest = div_by(i, (uint32_t)g.row_blocks, g.inv_row_blocks), head = div_by(rest, (uint32_t)g.splits, g.inv_splits);
+    return {i - rest * (uint32_t)g.row_blocks, rest - head * (uint32_t)g.splits, (int)head};
+}
+
+// Tiles of the three segments in one numbering, and what of them a part takes.
+struct Segments {
+    int32_t recent_rows, front_tiles, stored_tiles, begin, end;
+};
+__device__ __forceinline__ Segments segments_of(const AttendArgs& g, int32_t last_row, uint32_t cut, int tile_tokens, int32_t stored_tiles) {
+    Segments s;
+    s.recent_rows = g.recent.rows;  // as far as any row of the block sees
+    if (g.causal) s.recent_rows = max(0, min(s.recent_rows, (int32_t)div_by((uint32_t)last_row, (uint32_t)g.repeat, g.inv_repeat) + 1 + g.recent.rows - g.t_q));
+    s.front_tiles = (g.front.rows + tile_tokens - 1) / tile_tokens;
+    s.stored_tiles = stored_tiles;
+    const uint32_t tiles = (uint32_t)(s.front_tiles + s.stored_tiles + (s.recent_rows + tile_tokens - 1) / tile_tokens);
+    // equal runs, the first of them one longer where they do not divide evenly
+    const uint32_t run = div_by(tiles, (uint32_t)g.splits, g.inv_splits), longer = tiles - run * (uint32_t)g.splits;
+    s.begin = (int32_t)(cut * run + min(cut, longer));
+    s.end = s.begin + (int32_t)run + (cut < longer ? 1 : 0);
+    return s;
+}
+
 }  // namespace oqm

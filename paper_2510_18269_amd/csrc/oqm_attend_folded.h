@@ -718,23 +718,6 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
     __device__ __forceinline__ void finish() {}
 };
 
-// Tiles of the three segments in one numbering, and what of them a workgroup takes.
-struct Segments {
-    int32_t front, recent_rows, front_tiles, stored_tiles, begin, end;
-};
-__device__ __forceinline__ Segments segments_of(const AttendArgs& g, int32_t last_token, uint32_t cut, int tile_tokens, int32_t stored_tiles) {
-    Segments s;
-    s.front = g.front.rows;
-    s.recent_rows = g.recent.rows;  // as far as any row of the block sees
-    if (g.causal) s.recent_rows = max(0, min(s.recent_rows, last_token + 1 + g.recent.rows - g.t_q));
-    s.front_tiles = (s.front + tile_tokens - 1) / tile_tokens;
-    s.stored_tiles = stored_tiles;
-    const int32_t tiles = s.front_tiles + s.stored_tiles + (s.recent_rows + tile_tokens - 1) / tile_tokens;
-    s.begin = (int32_t)((int64_t)tiles * cut / g.splits);
-    s.end = (int32_t)((int64_t)tiles * (cut + 1) / g.splits);
-    return s;
-}
-
 // NW == 1: the workgroup's four waves have the same 16 MT query rows, take its tiles in turn, each staging its own, and join at
 // the end.  NW == 4: they have 16 MT rows each and share every tile.
 template <typename F>
@@ -747,12 +730,12 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
     __shared__ __align__(16) char lds[kStage > kJoin ? kStage : kJoin];
     const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
-    const uint32_t block = blockIdx.x % (uint32_t)g.row_blocks, rest = blockIdx.x / (uint32_t)g.row_blocks;
-    const uint32_t cut = rest % (uint32_t)g.splits;
-    const int head = (int)(rest / (uint32_t)g.splits);
+    const Item item = item_of(g, blockIdx.x);
+    const uint32_t cut = item.cut;
+    const int head = item.head;
     constexpr int kBlockRows = 16 * MT * NW;
     const int32_t rows = g.t_q * g.repeat;
-    const int32_t first_row = (int32_t)block * kBlockRows, wave_row = first_row + (NW == 1 ? 0 : wave * 16 * MT);
+    const int32_t first_row = (int32_t)item.block * kBlockRows, wave_row = first_row + (NW == 1 ? 0 : wave * 16 * MT);
 
     F f;
     bool there[MT];
@@ -766,9 +749,8 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
     }
     f.clear();
     const bool works = NW == 1 || wave_row < rows;  // a wave of a block's end has no rows but stages with the others
-    const int32_t last_token = (min(first_row + kBlockRows, rows) - 1) / g.repeat;
-    const int32_t wave_last = (min(wave_row + 16 * MT, rows) - 1) / g.repeat;
-    const Segments s = segments_of(g, last_token, cut, TT, F::tiles(g));
+    const int32_t wave_last = (int32_t)div_by((uint32_t)(min(wave_row + 16 * MT, rows) - 1), (uint32_t)g.repeat, g.inv_repeat);
+    const Segments s = segments_of(g, min(first_row + kBlockRows, rows) - 1, cut, TT, F::tiles(g));
     // Waves that stage for themselves take every fourth tile, so that the workgroup walks through memory, or, where a run of tiles
     // shares its queries' scales, a run each.
     constexpr int kStep = NW == 1 && F::SPREAD ? 4 : 1;
@@ -798,7 +780,7 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
     };
     auto from_in = [&](int32_t lo) { return begin >= lo ? begin : begin + (lo - begin + kStep - 1) / kStep * kStep; };
 
-    rows_of(g.front, from_in(0), min(end, s.front_tiles), 0, s.front, false);
+    rows_of(g.front, from_in(0), min(end, s.front_tiles), 0, g.front.rows, false);
 
     const int32_t stored_end = min(end, s.front_tiles + s.stored_tiles);
     if (from_in(s.front_tiles) < stored_end) {
