@@ -64,21 +64,24 @@ struct AttendArgs {
     int32_t splits, row_blocks;
 };
 
-// The kernel a call takes: `rows` query rows of a KV head a workgroup (general: a wave).
+// The kernel a call takes, and how many query rows of a KV head a workgroup of it has (general: a wave).
 struct AttendForm {
-    bool folded;
+    bool folded, shared;
     int32_t rows;
 };
 // Folded: 16-bit rows of 64, 128 or 256 channels, and either quant-groups of 32 channels or more of one token, so that a step of the
 // matrix cores (32 channels of keys, 16 of values) lies in one of them, or quant-groups along 16 tokens or more, so that a tile of 32
-// tokens, which lies in one of them, is not mostly empty.
+// tokens, which lies in one of them, is not mostly empty.  Shared: other 16-bit forms of the head_dim axis where more than 256 query
+// rows are to share a tile's reconstruction.  28 query heads on 4 of 128 channels, 64 groups of 50 tokens in quant-groups of 16, us,
+// general / shared: 16 tokens (112 rows) 31.8 / 44.9, 24 (168) 39.3 / 44.5, 64 (448) 62.1 / 52.6, 200 (1400) 149 / 79; 64 of 64
+// channels 41.2 / 35.4, of 256 channels 152 / 100.  The folded form of quant-groups of 64 and 64 tokens 39.5.
 inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
-    const bool tokens = c.qaxis == TOM_QAXIS_TOKENS;
-    const bool folded = c.out_dtype != TOM_F32 && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) &&
-                        (tokens ? c.group_tokens >= 16 : c.qgroup >= 32);
-    if (!folded) return {false, 16};
+    const bool tokens = c.qaxis == TOM_QAXIS_TOKENS, f32 = c.out_dtype == TOM_F32;
     const int64_t rows = (int64_t)(c.n_q_heads / c.n_kv_heads) * t_q;
-    return {true, rows <= 16 ? 16 : rows <= 64 || tokens || c.head_dim == 256 ? 64 : 128};
+    if (!f32 && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) && (tokens ? c.group_tokens >= 16 : c.qgroup >= 32))
+        return {true, false, rows <= 16 ? 16 : rows <= 64 || tokens || c.head_dim == 256 ? 64 : 128};
+    if (!f32 && !tokens && rows > 256) return {false, true, c.head_dim > 128 ? 128 : 256};
+    return {false, false, 16};
 }
 
 // Parts that the rows of a call are cut into, each with its own maximum and sum.  Never fewer where there are more rows: the
@@ -86,15 +89,18 @@ inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
 inline int32_t attend_cuts(const tom_oqm_config_t& c, int32_t t_q, int64_t rows) {
     const AttendForm f = attend_form(c, t_q);
     const int64_t blocks = ((int64_t)(c.n_q_heads / c.n_kv_heads) * t_q + f.rows - 1) / f.rows * c.n_kv_heads;
-    int64_t target = 2048, least = 32;  // waves: two a SIMD
-    if (f.folded && f.rows == 16) target = 768, least = 128;
+    int64_t target = 2048, least = 32;  // general: waves, two a SIMD
+    if (f.folded && f.rows == 16) target = 768, least = 128;  // one round of three workgroups a compute unit
     else if (f.folded) target = 512, least = 256;
+    else if (f.shared) target = 256, least = 256;
     int64_t n = target / blocks;
     if (n > (rows + least - 1) / least) n = (rows + least - 1) / least;
     return n < 1 ? 1 : (int32_t)n;
 }
 
 hipError_t launch_attend(const AttendArgs& a, const AttendForm& form, int dtype, hipStream_t s);
+void start_attend_shared_bf16(const AttendArgs& g, hipStream_t s);
+void start_attend_shared_f16(const AttendArgs& g, hipStream_t s);
 void start_attend_bf16_4bit(const AttendArgs& g, const AttendForm& form, hipStream_t s);
 void start_attend_bf16_2bit(const AttendArgs& g, const AttendForm& form, hipStream_t s);
 void start_attend_f16_4bit(const AttendArgs& g, const AttendForm& form, hipStream_t s);

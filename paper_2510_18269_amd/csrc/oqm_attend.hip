@@ -9,41 +9,6 @@
 
 namespace oqm {
 
-// Codes and pairs of N (4 or 8) channels as they are in memory.  Branch-free whatever their widths, so that the loads of a tile are
-// on their way together: codes are read as the aligned 32 bits that hold them (an array is a multiple of 4 bytes long), bfloat16
-// pairs as the same 32 bits twice.
-template <int N, bool TOKEN_AXIS>
-struct Stored {
-    static constexpr int NP = TOKEN_AXIS ? N : 1;
-    uint32_t w, shift;
-    __device__ __forceinline__ void load(const AttendArgs& g, const char* codes, uint32_t tok, int c) {
-        const uint64_t at = reinterpret_cast<uint64_t>(codes) + ((uint64_t)tok * (uint32_t)g.channels + (uint32_t)c) * (uint32_t)g.bits / 8;
-        w = *reinterpret_cast<const uint32_t*>(at & ~uint64_t{3});
-        shift = (uint32_t)(at & 3u) * 8u;
-    }
-    __device__ __forceinline__ void values(const AttendArgs& g, const f32x2 (&pair)[NP], float* x) const {
-        const uint32_t v = w >> shift, mask = g.bits == 4 ? 15u : 3u;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const f32x2 p = pair[TOKEN_AXIS ? i : 0];
-            x[i] = __builtin_fmaf((float)((v >> (g.bits * i)) & mask), p[0], p[1]);
-        }
-    }
-};
-struct StoredPair {
-    uint32_t first, second;
-    __device__ __forceinline__ void load(const AttendArgs& g, const char* meta, uint64_t i) {
-        const char* p = meta + (g.meta_bf16 ? 4 : 8) * i;
-        first = *reinterpret_cast<const uint32_t*>(p);
-        second = *reinterpret_cast<const uint32_t*>(p + (g.meta_bf16 ? 0 : 4));
-    }
-    // of a token that is not there: zero, whatever has been read
-    __device__ __forceinline__ f32x2 get(const AttendArgs& g, bool there) const {
-        const uint32_t s = g.meta_bf16 ? first << 16 : first, m = g.meta_bf16 ? first & 0xffff0000u : second;
-        return f32x2{__uint_as_float(there ? s : 0u), __uint_as_float(there ? m : 0u)};
-    }
-};
-
 // ---- general form ------------------------------------------------------------------------------------------------------------
 // A wave takes 16 query rows of a KV head and a run of 32-token tiles, on its own: every element is reconstructed (or widened) to
 // float32 and enters the products in two 16-bit parts where one does not hold it.  DP: channels, padded with zeros.
@@ -492,7 +457,9 @@ void start_general(const AttendArgs& g, hipStream_t s) {
 }
 
 hipError_t launch_attend(const AttendArgs& g, const AttendForm& form, int dtype, hipStream_t s) {
-    if (form.folded) {
+    if (form.shared) {
+        (dtype == TOM_BF16 ? start_attend_shared_bf16 : start_attend_shared_f16)(g, s);
+    } else if (form.folded) {
         if (dtype == TOM_BF16) (g.bits == 4 ? start_attend_bf16_4bit : start_attend_bf16_2bit)(g, form, s);
         else (g.bits == 4 ? start_attend_f16_4bit : start_attend_f16_2bit)(g, form, s);
     } else if (dtype == TOM_F32) {

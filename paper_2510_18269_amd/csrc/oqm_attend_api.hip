@@ -133,7 +133,7 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
     constexpr float kLog2e = 1.4426950408889634f;
     a.scale_log2 = softcap > 0.0f ? 2.0f * kLog2e * scale / softcap : scale * kLog2e;
     a.score_unit = 1.0f;
-    if (!form.folded && softcap == 0.0f && scale != 0.0f) {
+    if (!form.folded && !form.shared && softcap == 0.0f && scale != 0.0f) {
         a.score_unit = std::fabs(a.scale_log2);
         a.scale_log2 = scale > 0.0f ? 1.0f : -1.0f;
     }

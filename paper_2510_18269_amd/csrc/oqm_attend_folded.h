@@ -11,7 +11,7 @@
 // show (p * s as one binary16, 2^-12: 64 tokens over 128 groups 92 us against 107, 1000 over 32 291 against 335).
 #pragma once
 
-#include "oqm_attend_device.h"
+#include "oqm_attend_sums.h"
 
 namespace oqm {
 
@@ -23,149 +23,6 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 constexpr float kUp = 0x1p64f, kDown = 0x1p69f;  // 2^64 * 2^-133 = 2^-69
-constexpr float kSlack = 8.0f;                    // a maximum may lag behind by this (units of log 2) before sums are scaled anew
-
-// The sums of a wave's query rows, and the tiles of rows as the model has them.  A lane's channels of V^T: VU of each of VN runs of
-// GS channels.  NZ: sums that are scaled with the others.
-template <typename T_, int DP_, int GS_, int MT_, int NZ>
-struct Sums {
-    typedef T_ T;
-    static constexpr int DP = DP_, GS = GS_, MT = MT_;  // MT: blocks of 16 query rows of a wave
-    static constexpr int VU = GS / 16, VN = DP / GS, STEPS = DP / 32;
-    static constexpr int PARTS = __is_same(T, In_f16) ? 2 : 1;  // of a query element in bfloat16
-
-    f32x4 o[MT][DP / 16];
-    float zero[MT][NZ];
-    float top[MT], sum[MT];
-
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            top[m] = -__builtin_inff();
-            sum[m] = 0.0f;
-#pragma unroll
-            for (int n = 0; n < DP / 16; ++n) o[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int n = 0; n < NZ; ++n) zero[m][n] = 0.0f;
-        }
-    }
-    // Scores to probabilities.
-    __device__ __forceinline__ void probabilities(float (&w)[MT][8]) {
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            float high = fmaxf(fmaxf(fmaxf(w[m][0], w[m][1]), fmaxf(w[m][2], w[m][3])), fmaxf(fmaxf(w[m][4], w[m][5]), fmaxf(w[m][6], w[m][7])));
-            if (__any(high > top[m] + kSlack)) {
-                high = fmaxf(high, __shfl_xor(high, 16, 64));
-                high = fmaxf(high, __shfl_xor(high, 32, 64));
-                const float next = fmaxf(top[m], high);
-                const float by = next == -__builtin_inff() ? 1.0f : exp2_of(top[m] - next);
-                top[m] = next;
-                sum[m] *= by;
-#pragma unroll
-                for (int n = 0; n < DP / 16; ++n) o[m][n] *= by;
-#pragma unroll
-                for (int n = 0; n < NZ; ++n) zero[m][n] *= by;
-            }
-            const float from = top[m] == -__builtin_inff() ? 0.0f : top[m];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[m][i] = exp2_of(w[m][i] - from);
-                sum[m] += w[m][i];
-            }
-        }
-    }
-    static __device__ __forceinline__ void finish_scores(const AttendArgs& g, float (&w)[MT][8]) {
-        if (g.cap_log2 != 0.0f) {
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[m][i] = capped(w[m][i], g.cap_log2);
-        }
-    }
-
-    static __device__ __forceinline__ void load_query(const char* p, bool there, int quarter, Operand<T> (&q)[STEPS]) {
-#pragma unroll
-        for (int u = 0; u < STEPS; ++u) {
-            q[u].w = u32x4{0u, 0u, 0u, 0u};
-            if (there) q[u].w = *reinterpret_cast<const u32x4*>(p + (quarter * (DP / 4) + 8 * u) * 2);
-        }
-    }
-    // 32 tokens of rows as the model has them, from t0; `seen`: of the rows from the first, how many each query row sees.
-    __device__ __forceinline__ void rows(const AttendArgs& g, const AttendRows& r, int head, int32_t t0, int32_t tokens, const Operand<T> (&q)[MT][STEPS],
-                                         const int32_t (&seen)[MT]) {
-        const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
-        const char* k = r.k + head * r.k_head + quarter * (DP / 4) * 2;
-        const char* v = r.v + head * r.v_head + a * VU * 2;
-        typedef uint32_t Piece __attribute__((ext_vector_type(VU / 2)));
-        // what lies behind the last row is read from the last row, and seen by nobody
-        u32x4 kx[2][STEPS];
-        Piece vx[8][VN];
-        auto load_values = [&] {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const char* p = v + (int64_t)min(t0 + 16 * (i / 4) + 4 * quarter + i % 4, tokens - 1) * r.v_row;
-#pragma unroll
-                for (int n = 0; n < VN; ++n) vx[i][n] = *reinterpret_cast<const Piece*>(p + n * GS * 2);
-            }
-        };
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const char* p = k + (int64_t)min(t0 + 16 * half + a, tokens - 1) * r.k_row;
-#pragma unroll
-            for (int u = 0; u < STEPS; ++u) kx[half][u] = *reinterpret_cast<const u32x4*>(p + 16 * u);
-        }
-        if constexpr (MT == 1) load_values();  // in flight with the keys; with two blocks of rows there are no registers for it
-        float w[MT][8];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            f32x4 d[MT];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) d[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int u = 0; u < STEPS; ++u) {
-                Operand<T> x;
-                x.w = kx[half][u];
-#pragma unroll
-                for (int m = 0; m < MT; ++m) d[m] = product(x, q[m][u], d[m]);
-            }
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[m][4 * half + i] = d[m][i] * g.scale_log2;
-        }
-        finish_scores(g, w);
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (t0 + 16 * (i / 4) + 4 * quarter + i % 4 >= seen[m]) w[m][i] = -__builtin_inff();
-        probabilities(w);
-        if constexpr (MT > 1) load_values();
-        Operand<T> hi[MT], lo[MT];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) split(w[m], hi[m], lo[m]);
-#pragma unroll
-        for (int n = 0; n < VN; ++n)
-#pragma unroll
-            for (int u = 0; u < VU; u += 2) {
-                Operand<T> even, odd;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t x = vx[2 * i][n][u / 2], y = vx[2 * i + 1][n][u / 2];
-                    even.w[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                    odd.w[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-                }
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    f32x4 &e = o[m][n * VU + u], &f = o[m][n * VU + u + 1];
-                    e = product(even, hi[m], e);
-                    e = product(even, lo[m], e);
-                    f = product(odd, hi[m], f);
-                    f = product(odd, lo[m], f);
-                }
-            }
-    }
-};
 
 // Operands from packed codes.  In LDS a token's codes are STRIDE bytes from the next one's.
 template <int DP, int GS, int BITS>

@@ -261,3 +261,13 @@ def test_what_nobody_sees_may_be_anything(oqm, dtype, t_q):
     assert bool(got[0][0].isfinite().all()) and bool(got[0][1].isfinite().all())
     assert torch.equal(got[0][0][:, seen], got[1][0][:, seen]) and torch.equal(got[0][1][:, seen], got[1][1][:, seen])
     oqm.tom_oqm_destroy(h)
+
+
+@pytest.mark.parametrize("d,gs,bits,meta,G,dtype", [
+    (128, 16, 4, "f32", 50, "bf16"), (128, 8, 2, "bf16", 33, "bf16"), (64, 16, 2, "f32", 7, "f16"), (256, 16, 4, "bf16", 40, "bf16"), (80, 8, 4, "f32", 31, "bf16"),
+    (136, 8, 2, "f32", 64, "f16"), (8, 8, 2, "f32", 3, "bf16"), (96, 32, 4, "f32", 1, "bf16"), (128, 8, 4, "f32", 196, "f16")])
+@pytest.mark.parametrize("t_q,causal", [(97, True), (300, False)])
+def test_many_tokens_on_narrow_quant_groups(oqm, d, gs, bits, meta, G, dtype, t_q, causal):
+    """More query rows than the reconstruction of a tile is shared by: 3 * t_q, over holes, a ragged front and recent rows."""
+    check(oqm, Case(d=d, gs=gs, bits=bits, meta=meta, G=G, dtype=dtype, t_q=t_q, repeat=3, T=30, k=21, holes=3, front=45, recent=t_q + 17 if causal else 70,
+                    causal=causal, softcap=25.0 if G == 50 else 0.0, seed=t_q + d))
