@@ -617,27 +617,32 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
         if (!F::SPREAD) end = s.begin + (s.end - s.begin) * (wave + 1) / 4;
     }
 
-    auto rows_of = [&](const AttendRows& r, int32_t from, int32_t to, int32_t first, int32_t tokens, bool recent) {
-        if (from >= to || !works) return;
-        Operand<T> q[MT][STEPS];
-        int32_t seen[MT], all = tokens;
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            S::load_query(g.q + q_head[m] * g.q_head + token[m] * g.q_row, there[m], quarter, q[m]);
-            seen[m] = tokens;
-            if (recent && g.causal) seen[m] = min(tokens, token[m] + 1 + g.recent.rows - g.t_q);
-        }
-        if (recent && g.causal) all = min(tokens, wave_last + 1 + g.recent.rows - g.t_q);
-        for (int32_t t = from; t < to; t += kStep)
-#pragma unroll 1
-            for (int sub = 0; sub < TT; sub += 32) {
-                const int32_t t0 = (t - first) * TT + sub;
-                if (t0 < all) f.rows(g, r, head, t0, tokens, q, seen);
-            }
-    };
     auto from_in = [&](int32_t lo) { return begin >= lo ? begin : begin + (lo - begin + kStep - 1) / kStep * kStep; };
-
-    rows_of(g.front, from_in(0), min(end, s.front_tiles), 0, g.front.rows, false);
+    // Rows in front and recent ones by the same code, so that the sums are held across one copy of it.
+    if (works) {
+#pragma unroll 1
+        for (int segment = 0; segment < 2; ++segment) {
+            const AttendRows& r = segment == 0 ? g.front : g.recent;
+            const int32_t first = segment == 0 ? 0 : s.front_tiles + s.stored_tiles, tokens = segment == 0 ? g.front.rows : s.recent_rows;
+            const int32_t from = from_in(first), to = segment == 0 ? min(end, s.front_tiles) : end;
+            if (from >= to) continue;
+            const bool causal = segment == 1 && g.causal;
+            const int32_t all = causal ? min(tokens, wave_last + 1 + g.recent.rows - g.t_q) : tokens;
+            Operand<T> q[MT][STEPS];
+            int32_t seen[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                S::load_query(g.q + q_head[m] * g.q_head + token[m] * g.q_row, there[m], quarter, q[m]);
+                seen[m] = causal ? min(tokens, token[m] + 1 + g.recent.rows - g.t_q) : tokens;
+            }
+            for (int32_t t = from; t < to; t += kStep)
+#pragma unroll 1
+                for (int sub = 0; sub < TT; sub += 32) {
+                    const int32_t t0 = (t - first) * TT + sub;
+                    if (t0 < all) f.rows(g, r, head, t0, tokens, q, seen);
+                }
+        }
+    }
 
     const int32_t stored_end = min(end, s.front_tiles + s.stored_tiles);
     if (from_in(s.front_tiles) < stored_end) {
@@ -666,8 +671,6 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
         }
         f.template rescale<false>();
     }
-
-    rows_of(g.recent, from_in(s.front_tiles + s.stored_tiles), end, s.front_tiles + s.stored_tiles, s.recent_rows, true);
 
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
