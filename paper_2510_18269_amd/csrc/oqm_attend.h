@@ -71,17 +71,28 @@ struct AttendForm {
 };
 // Folded: 16-bit rows of 64, 128 or 256 channels, and either quant-groups of 32 channels or more of one token, so that a step of the
 // matrix cores (32 channels of keys, 16 of values) lies in one of them, or quant-groups along 16 tokens or more, so that a tile of 32
-// tokens, which lies in one of them, is not mostly empty.  Shared: other 16-bit forms of the head_dim axis where more than 256 query
-// rows are to share a tile's reconstruction.  28 query heads on 4 of 128 channels, 64 groups of 50 tokens in quant-groups of 16, us,
-// general / shared: 16 tokens (112 rows) 31.8 / 44.9, 24 (168) 39.3 / 44.5, 64 (448) 62.1 / 52.6, 200 (1400) 149 / 79; 64 of 64
-// channels 41.2 / 35.4, of 256 channels 152 / 100.  The folded form of quant-groups of 64 and 64 tokens 39.5.
+// tokens, which lies in one of them, is not mostly empty.  Its workgroups have 16 rows, which their waves share, or 16 a wave.
+// (32 a wave spare a fifth of the instructions but leave two waves a SIMD instead of three: 1000 tokens over 32 groups 332 us, 283
+// with 16; 64 over 128 groups 116 and 113.)  Shared: other 16-bit forms of the head_dim axis where more than 256 query rows are to
+// share a tile's reconstruction.  28 query heads on 4 of 128 channels, 64 groups of 50 tokens in quant-groups of 16, us, general /
+// shared: 16 tokens (112 rows) 31.8 / 44.9, 24 (168) 39.3 / 44.5, 64 (448) 62.1 / 52.6, 200 (1400) 149 / 79; 64 of 64 channels 41.2 /
+// 35.4, of 256 channels 152 / 100.  The folded form of quant-groups of 64 and 64 tokens 39.5.
 inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
     const bool tokens = c.qaxis == TOM_QAXIS_TOKENS, f32 = c.out_dtype == TOM_F32;
     const int64_t rows = (int64_t)(c.n_q_heads / c.n_kv_heads) * t_q;
     if (!f32 && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) && (tokens ? c.group_tokens >= 16 : c.qgroup >= 32))
-        return {true, false, rows <= 16 ? 16 : rows <= 64 || tokens || c.head_dim == 256 ? 64 : 128};
+        return {true, false, rows <= 16 ? 16 : 64};
     if (!f32 && !tokens && rows > 256) return {false, true, c.head_dim > 128 ? 128 : 256};
     return {false, false, 16};
+}
+
+// Waves of the folded kernels that a SIMD holds: what their registers leave, and what the kernels are bound to.  Workgroups have
+// one wave on each SIMD, so that it is also the workgroups of a compute unit.
+constexpr int attend_waves(int channels, int qgroup, bool tokens, bool f16, bool few_rows) {
+    if (channels == 256) return 1;
+    if (tokens) return channels == 64 ? 3 : 2;
+    if (channels == 64) return 4;
+    return (qgroup == 32 && (f16 || few_rows)) || (f16 && few_rows) ? 2 : 3;
 }
 
 // Parts that the rows of a call are cut into, each with its own maximum and sum.  Never fewer where there are more rows: the
@@ -90,9 +101,27 @@ inline int32_t attend_cuts(const tom_oqm_config_t& c, int32_t t_q, int64_t rows)
     const AttendForm f = attend_form(c, t_q);
     const int64_t blocks = ((int64_t)(c.n_q_heads / c.n_kv_heads) * t_q + f.rows - 1) / f.rows * c.n_kv_heads;
     int64_t target = 2048, least = 32;  // general: waves, two a SIMD
-    if (f.folded && f.rows == 16) target = 768, least = 128;  // one round of three workgroups a compute unit
-    else if (f.folded) target = 512, least = 256;
-    else if (f.shared) target = 256, least = 256;
+    if (f.folded) {
+        target = 256 * attend_waves(c.head_dim, c.qgroup, c.qaxis == TOM_QAXIS_TOKENS, c.out_dtype == TOM_F16, f.rows == 16);
+        least = f.rows == 16 ? 128 : 256;
+        if (f.rows > 16) {
+            // Rounds of the chip per part, against what they would be if all were full, and what a part of a row costs: written and read
+            // again, 1 KB at 5 TB/s, as much as 125 of its tokens.  440 blocks of 7286 rows, us at 1 / 2 / 3 / 4 / 5 / 8 / 9 parts: 394 /
+            // 339 / 309 / 283 / 287 / 289 / 373.  (As rows grow the second term falls, so that parts never become fewer.)  From two
+            // full rounds up the last one matters little, and the workspace would grow with the call.
+            if (blocks >= 2 * target) return 1;
+            int64_t best = 1;
+            double least_cost = 1e300;
+            for (int64_t n = 1; n <= 2 * target / blocks + 2 && n <= (rows + least - 1) / least; ++n) {
+                const double rounds = (double)((blocks * n + target - 1) / target) / (double)n * (double)target / (double)blocks;
+                const double cost = rounds + 125.0 * (double)n / (double)(rows > 0 ? rows : 1);
+                if (cost < least_cost) least_cost = cost, best = n;
+            }
+            return (int32_t)best;
+        }
+    } else if (f.shared) {
+        target = 256, least = 256;
+    }
     int64_t n = target / blocks;
     if (n > (rows + least - 1) / least) n = (rows + least - 1) / least;
     return n < 1 ? 1 : (int32_t)n;

@@ -125,7 +125,7 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
     static constexpr int LOADS = (PIECES + NW * 64 - 1) / (NW * 64);
     static constexpr int META = TT * NG * 8;        // bytes of K's or V's pairs in LDS
     static constexpr int STAGE = 2 * TT * STRIDE + 2 * META;
-    static constexpr int WAVES = NW == 1 ? (DP == 64 ? 4 : DP == 128 ? (NG < 4 && PARTS == 1 ? 3 : 2) : 1) : MT == 1 ? (DP == 64 ? 3 : DP == 128 ? 2 : 1) : 2;  // a SIMD
+    static constexpr int WAVES = attend_waves(DP, GS, false, __is_same(T, In_f16), NW == 1);  // a SIMD
 
     // ---- staging ----
     struct Fetch {
@@ -390,7 +390,7 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
     static constexpr int PIECES = TT * ROW / 16, LOADS = (PIECES + NW * 64 - 1) / (NW * 64);
     static constexpr int PAIRS = (2 * DP + NW * 64 - 1) / (NW * 64);  // of K and V a lane stages
     static constexpr int STAGE = 2 * TT * STRIDE + 2 * DP * 8;
-    static constexpr int WAVES = DP == 64 ? 3 : DP == 128 ? 2 : 1;
+    static constexpr int WAVES = attend_waves(DP, 0, true, __is_same(T, In_f16), NW == 1);  // a SIMD
 
     struct Fetch {
         u32x4 k[LOADS], v[LOADS];
@@ -770,8 +770,7 @@ template <typename T, int DP, int GS, int BITS>
 void start_folded(const AttendArgs& g, const AttendForm& form, hipStream_t s) {
     const dim3 grid((uint32_t)((int64_t)g.row_blocks * g.splits * g.kv_heads)), block(kBlock);
     if (form.rows == 16) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 1>>, grid, block, 0, s, g);
-    else if (DP == 256 || form.rows == 64) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 4>>, grid, block, 0, s, g);
-    else if constexpr (DP < 256) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 2, 4>>, grid, block, 0, s, g);
+    else launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 4>>, grid, block, 0, s, g);
 }
 
 template <typename T, int DP, int BITS>
