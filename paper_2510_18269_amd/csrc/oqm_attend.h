@@ -70,8 +70,9 @@ struct AttendForm {
     int32_t rows;
 };
 // Folded: 16-bit rows of 64, 128 or 256 channels, and either quant-groups of 32 channels or more of one token, so that a step of the
-// matrix cores (32 channels of keys, 16 of values) lies in one of them, or quant-groups along 16 tokens or more, so that a tile of 32
-// tokens, which lies in one of them, is not mostly empty.  Its workgroups have 16 rows, which their waves share, or 16 a wave.
+// matrix cores (32 channels of keys, 16 of values) lies in one of them, or quant-groups along the tokens, where a tile of 32 tokens
+// lies in one of them (mostly empty if they are short, and still the faster: 255 groups of 1 / 5 / 15 tokens, one new token, 135 / 44 /
+// 27 us in the general form, 13.4 / 12.9 / 13.1 folded).  Its workgroups have 16 rows, which their waves share, or 16 a wave.
 // (32 a wave spare a fifth of the instructions but leave two waves a SIMD instead of three: 1000 tokens over 32 groups 332 us, 283
 // with 16; 64 over 128 groups 116 and 113.)  Shared: other 16-bit forms of the head_dim axis where more than 256 query rows are to
 // share a tile's reconstruction.  28 query heads on 4 of 128 channels, 64 groups of 50 tokens in quant-groups of 16, us, general /
@@ -80,7 +81,7 @@ struct AttendForm {
 inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
     const bool tokens = c.qaxis == TOM_QAXIS_TOKENS, f32 = c.out_dtype == TOM_F32;
     const int64_t rows = (int64_t)(c.n_q_heads / c.n_kv_heads) * t_q;
-    if (!f32 && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) && (tokens ? c.group_tokens >= 16 : c.qgroup >= 32))
+    if (!f32 && (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) && (tokens || c.qgroup >= 32))
         return {true, false, rows <= 16 ? 16 : 64};
     if (!f32 && !tokens && rows > 256) return {false, true, c.head_dim > 128 ? 128 : 256};
     return {false, false, 16};
@@ -99,6 +100,8 @@ constexpr int attend_waves(int channels, int qgroup, bool tokens, bool f16, bool
 // workspace of the longest call serves the others.
 inline int32_t attend_cuts(const tom_oqm_config_t& c, int32_t t_q, int64_t rows) {
     const AttendForm f = attend_form(c, t_q);
+    // Along the tokens' axis a tile of 32 lies in one group, however short.
+    if (c.qaxis == TOM_QAXIS_TOKENS) rows = (rows + c.group_tokens - 1) / c.group_tokens * (((int64_t)c.group_tokens + 31) / 32 * 32);
     const int64_t blocks = ((int64_t)(c.n_q_heads / c.n_kv_heads) * t_q + f.rows - 1) / f.rows * c.n_kv_heads;
     int64_t target = 2048, least = 32;  // general: waves, two a SIMD
     if (f.folded) {

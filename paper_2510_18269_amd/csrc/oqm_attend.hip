@@ -177,11 +177,11 @@ struct General {
                 for (int i = 0; i < Key::NP; ++i) pair[i] = kp[TOKEN_AXIS ? 0 : half][LATE_PAIRS ? 0 : u][i].get(g, is[half] && inside);
                 float x[8];
                 kx[half][u].values(g, pair, x);
-                Operand<T> hi, lo;
-                split(x, hi, lo);
+                Operand<T> part[kKeyParts<T>];
+                split_key<T>(x, part);
                 f32x4& d = s[half][u % CHAINS];
-                d = product(hi, q[u], d);
-                if constexpr (!__is_same(T, In_f32)) d = product(lo, q[u], d);
+#pragma unroll
+                for (int i = 0; i < kKeyParts<T>; ++i) d = product(part[i], q[u], d);
             }
         }
         join_chains(s);

@@ -76,6 +76,29 @@ __device__ __forceinline__ void split(const float (&x)[8], Operand<In_f32>& hi, 
     for (int i = 0; i < 8; ++i) hi.x[i] = x[i];
 }
 
+// Keys that are reconstructed enter in as many parts as make them float32's: with outliers a score is a few hundred times the
+// sum's last bits, and 2^-17 of it shows in the logarithm of the sum.
+template <typename T> constexpr int kKeyParts = __is_same(T, In_f32) ? 1 : __is_same(T, In_f16) ? 2 : 3;
+template <typename T>
+__device__ __forceinline__ void split_key(const float (&x)[8], Operand<T> (&part)[kKeyParts<T>]) {
+    if constexpr (kKeyParts<T> == 1) {
+        Operand<T> none;
+        split(x, part[0], none);
+    } else if constexpr (kKeyParts<T> == 2) {
+        split(x, part[0], part[1]);
+    } else {
+        Operand<T> ignored;
+        split(x, part[0], ignored);
+        float r[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            r[2 * i] = x[2 * i] - __uint_as_float(part[0].w[i] << 16);
+            r[2 * i + 1] = x[2 * i + 1] - __uint_as_float(part[0].w[i] & 0xffff0000u);
+        }
+        split(r, part[1], part[2]);
+    }
+}
+
 // N (4 or 8) consecutive channels of a row in 32 bits.
 template <typename T, int N>
 __device__ __forceinline__ void load_row(const char* p, float* x) {

@@ -378,7 +378,7 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
 
 // Scale and zero of a channel for all tokens of a group:
 //   <q, k_t>      = <q s, code_t> + <q, m>            sum_t p_t v_t = s sum_t p_t code_t + m sum_t p_t     over a group's tokens
-// so the queries take a group's scales (in two bfloat16 parts), and the sums of a tile, which lies in one group, its values'.
+// so the queries take a group's scales (in three bfloat16 parts), and the sums of a tile, which lies in one group, its values'.
 template <typename T, int DP, int BITS, int NW_>
 struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 128 ? DP : 128), BITS> {
     typedef Sums<T, DP, (DP < 128 ? DP : 128), 1, 1> S;
@@ -463,7 +463,7 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
 
     struct Query {
         float x[DP / 4];  // as given, in the order of the operands
-        Operand<In_bf16> hi[STEPS], lo[STEPS];
+        Operand<In_bf16> part[STEPS][3];
         float plain;
         int32_t rank;
     };
@@ -504,7 +504,7 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
                 float w[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) w[j] = z[C::key_channel(step, j)] * (kUp / C::key_factor(j));
-                split(w, y.hi[n * SPG + step], y.lo[n * SPG + step]);
+                split_key<In_bf16>(w, y.part[n * SPG + step]);
             }
         }
         plain += __shfl_xor(plain, 16, 64);
@@ -528,8 +528,8 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
 #pragma unroll
                 for (int s = 0; s < SPG; ++s) {
                     const Operand<In_bf16> x = C::key_operand(words, s);
-                    d = product(x, y.hi[i * SPG + s], d);
-                    d = product(x, y.lo[i * SPG + s], d);
+#pragma unroll
+                    for (int part = 0; part < 3; ++part) d = product(x, y.part[i * SPG + s][part], d);
                 }
             }
 #pragma unroll

@@ -1,4 +1,4 @@
-// Attention of many query rows over codes of any layout: a tile of 32 tokens is reconstructed once in LDS, in two 16-bit parts, for
+// Attention of many query rows over codes of any layout: a tile of 32 tokens is reconstructed once in LDS, in 16-bit parts, for
 // all the query rows of a workgroup.
 //
 // In LDS the operands lie as the matrix cores take them, 16 bytes a lane:
@@ -19,7 +19,7 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
     typedef typename MetaPair<BF16_META>::type Pair;
     using S::GS, S::VU, S::STEPS, S::o;
     static constexpr int DP = DP_, MT = MT_, NW = NW_, THREADS = NW * 64;
-    static constexpr int KEYS = 32 * DP * 2, PART = 2 * KEYS, STAGE = 2 * PART;  // bytes: keys of a part, a part, both
+    static constexpr int KP = kKeyParts<T>, PART = 32 * DP * 2, VALUES = KP * PART, STAGE = VALUES + 2 * PART;  // bytes in LDS
     // of a thread: key units (a token's 8 channels), value units (4 tokens' 2 channels)
     static constexpr int UNITS = 4 * DP, KU = (UNITS + THREADS - 1) / THREADS;
 
@@ -172,10 +172,10 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
                 float y[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = __builtin_fmaf((float)(w >> (g.bits * j) & mask), p[0], p[1]);
-                Operand<T> hi, lo;
-                split(y, hi, lo);
-                *reinterpret_cast<u32x4*>(at) = hi.w;
-                *reinterpret_cast<u32x4*>(at + PART) = lo.w;
+                Operand<T> part[KP];
+                split_key<T>(y, part);
+#pragma unroll
+                for (int j = 0; j < KP; ++j) *reinterpret_cast<u32x4*>(at + j * PART) = part[j].w;
             } else {
                 *reinterpret_cast<u32x4*>(at) = inside ? u32x4{f.k[i][0], f.k[i][1], f.k[i][2], f.k[i][3]} : u32x4{0u, 0u, 0u, 0u};
             }
@@ -187,7 +187,7 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
             int c, half, quarter;
             value_unit(unit, c, half, quarter);
             const int rest = c % GS, n = c / GS * VU + rest % VU, a = rest / VU;
-            char* const at = lds + KEYS + ((n * 64 + quarter * 16 + a) * 8 + half * 4) * 2;
+            char* const at = lds + VALUES + ((n * 64 + quarter * 16 + a) * 8 + half * 4) * 2;
             Operand<T> hi, lo;
             if (f.stored) {
                 const uint32_t there = c < g.channels ? f.valid >> (16 * half + 4 * quarter) : 0u, up = (uint32_t)(c * g.bits) & 7u;
@@ -217,7 +217,7 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
         x.w = *reinterpret_cast<const u32x4*>(lds + (i * 64 + (int)__lane_id()) * 16);
         return x;
     }
-    // A staged tile.  two: it has second parts; valid: of its tokens; seen: of its tokens from the first, how many each query row sees.
+    // A staged tile.  two: it has more parts than one; valid: of its tokens; seen: of its tokens from the first, how many each query row sees.
     __device__ __forceinline__ void tile(const AttendArgs& g, const char* lds, const Operand<T> (&q)[MT][STEPS], bool two, uint32_t valid, const int32_t (&seen)[MT]) {
         const int quarter = (int)__lane_id() >> 4;
         f32x4 d[2][MT];
@@ -234,13 +234,12 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
         }
         if (two) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int i = 0; i < (KP - 1) * 2 * STEPS; ++i) {
+                const int half = i / STEPS % 2, u = i % STEPS;
+                const Operand<T> x = operand(lds + (1 + i / STEPS / 2) * PART, half * STEPS + u);
 #pragma unroll
-                for (int u = 0; u < STEPS; ++u) {
-                    const Operand<T> x = operand(lds + PART, half * STEPS + u);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) d[half][m] = product(x, q[m][u], d[half][m]);
-                }
+                for (int m = 0; m < MT; ++m) d[half][m] = product(x, q[m][u], d[half][m]);
+            }
         }
         float w[MT][8];
         bool all = valid == 0xffffffffu;
@@ -266,7 +265,7 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
         for (int m = 0; m < MT; ++m) split(w[m], hi[m], lo[m]);
 #pragma unroll
         for (int n = 0; n < DP / 16; ++n) {
-            const Operand<T> x = operand(lds + KEYS, n);
+            const Operand<T> x = operand(lds + VALUES, n);
 #pragma unroll
             for (int m = 0; m < MT; ++m) o[m][n] = product(x, hi[m], o[m][n]);
 #pragma unroll
@@ -275,7 +274,7 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
         if (two) {
 #pragma unroll
             for (int n = 0; n < DP / 16; ++n) {
-                const Operand<T> x = operand(lds + PART + KEYS, n);
+                const Operand<T> x = operand(lds + VALUES + PART, n);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) o[m][n] = product(x, hi[m], o[m][n]);
             }
