@@ -45,8 +45,8 @@ struct General {
 #pragma unroll
         for (int i = 1; i < 8; ++i) high = fmaxf(high, w[i]);
         if (__any(high > top)) {
-            high = fmaxf(high, __shfl_xor(high, 16, 64));
-            high = fmaxf(high, __shfl_xor(high, 32, 64));
+            high = fmaxf(high, lane_xor<16>(high));
+            high = fmaxf(high, lane_xor<32>(high));
             const float next = fmaxf(top, high);
             const float by = next == -__builtin_inff() ? 1.0f : exp2_of((top - next) * g.score_unit);
             top = next;
@@ -297,13 +297,20 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? (TOKEN_AXIS ? 2 : 3) : DP == 128
     f.sum = 0.0f;
 #pragma unroll
     for (int n = 0; n < DP / 16; ++n) f.o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // A row that is not there computes with the first one, so that nothing waits for a condition.
+    Raw8<T> raw[Form::STEPS];
+    const char* const q_row = g.q + q_head * g.q_head + token * g.q_row;
 #pragma unroll
     for (int u = 0; u < Form::STEPS; ++u) {
         const int c = quarter * (DP / 4) + 8 * u;
-        float x[8];
+        load_raw(q_row + (int64_t)(c < g.channels ? c : 0) * elem_bytes<T>::value, raw[u]);
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-        if (there && c < g.channels) load_row<T, 8>(g.q + q_head * g.q_head + token * g.q_row + (int64_t)c * elem_bytes<T>::value, x);
+    for (int u = 0; u < Form::STEPS; ++u) {
+        float x[8];
+        widen(raw[u], x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = quarter * (DP / 4) + 8 * u < g.channels ? x[i] : 0.0f;
         Operand<T> unused;
         split(x, f.q[u], unused);
     }
@@ -316,8 +323,8 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? (TOKEN_AXIS ? 2 : 3) : DP == 128
     for (int32_t t = max(s.begin, stored_end); t < s.end; ++t) f.rows(g, g.recent, head, (t - stored_end) * kTile, recent, seen);
 
     float sum = f.sum;
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
+    sum += lane_xor<16>(sum);
+    sum += lane_xor<32>(sum);
     if (!there) return;
     // the lane holds channels run(v) + VU * (4 * quarter + i) + 0 .. VU - 1 of its query row
     const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
@@ -396,6 +403,15 @@ __device__ __forceinline__ Joined join_parts(const AttendArgs& g, int64_t at, in
     }
     return j;
 }
+// What the lane N on, or back, has found.
+template <int N>
+__device__ __forceinline__ void join_across(const AttendArgs& g, Joined& j) {
+    const float top = lane_xor<N>(j.top), total = lane_xor<N>(j.total);
+    f32x4 sum;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) sum[n] = lane_xor<N>(j.sum[n]);
+    j.add(g.score_unit, top, total, sum);
+}
 // Few parts: a lane takes them all.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void attend_join_few_kernel(AttendArgs g, uint32_t lanes, uint32_t inv_lanes, uint32_t rows) {
@@ -413,14 +429,9 @@ __global__ __launch_bounds__(kBlock) void attend_join_many_kernel(AttendArgs g) 
     const bool there = c < g.channels;
     Joined j;
     if (there) j = join_parts(g, blockIdx.x, c, set, kSets);
-#pragma unroll
-    for (int m = kLanes; m < 64; m *= 2) {
-        const float top = __shfl_xor(j.top, m, 64), total = __shfl_xor(j.total, m, 64);
-        f32x4 sum;
-#pragma unroll
-        for (int n = 0; n < 4; ++n) sum[n] = __shfl_xor(j.sum[n], m, 64);
-        j.add(g.score_unit, top, total, sum);
-    }
+    join_across<8>(g, j);
+    join_across<16>(g, j);
+    join_across<32>(g, j);
     __shared__ float tops[kBlock / 64][kLanes], totals[kBlock / 64][kLanes];
     __shared__ f32x4 sums[kBlock / 64][kLanes];
     const int wave = (int)threadIdx.x / 64;

@@ -12,6 +12,21 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kTile = 32;  // tokens
 
+// The value of lane ^ N, without LDS.
+template <int N>
+__device__ __forceinline__ float lane_xor(float v) {
+    static_assert(N == 8 || N == 16 || N == 32, "lane distance");
+    if constexpr (N == 8) {
+        return dpp_f32<0x128>(v);  // row_ror:8
+    } else {
+        // both registers hold v: the first ends with the lower lanes' (even rows') in all, the second with the others'
+        uint32_t a = __float_as_uint(v), b = a;
+        if constexpr (N == 32) swap32(a, b);
+        else swap16(a, b);
+        return __uint_as_float((__lane_id() & N) ? a : b);
+    }
+}
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // softcap * tanh(y) in units of log 2, from z = 2 log2(e) y: tanh y = 1 - 2 / (1 + 2^z).  The difference loses what the one has over

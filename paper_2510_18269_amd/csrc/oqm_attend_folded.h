@@ -139,9 +139,8 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
         int32_t rank, tok, slot0, slot1;
     };
     static __device__ __forceinline__ int32_t slot_at(const AttendArgs& g, int32_t rank) {
-        if (rank >= g.k_eff) return -1;
-        const int32_t slot = g.idx ? g.idx[rank] : rank;
-        return slot >= 0 && slot < g.n_groups ? slot : -1;
+        const int32_t at = min(rank, g.k_eff - 1), slot = g.idx ? g.idx[at] : at;
+        return rank < g.k_eff && slot >= 0 && slot < g.n_groups ? slot : -1;
     }
     static __device__ __forceinline__ Place place(const AttendArgs& g, int32_t t0) {
         Place p;
@@ -150,8 +149,9 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
         p.tok = t0 - p.rank * g.group_tokens;
         p.slot0 = p.slot1 = 0;
         if (g.group_tokens >= TT) {
-            p.slot0 = __builtin_amdgcn_readfirstlane(slot_at(g, p.rank));
-            p.slot1 = __builtin_amdgcn_readfirstlane(slot_at(g, p.rank + 1));
+            const int32_t first = slot_at(g, p.rank), second = slot_at(g, p.rank + 1);  // both on their way before one is waited for
+            p.slot0 = __builtin_amdgcn_readfirstlane(first);
+            p.slot1 = __builtin_amdgcn_readfirstlane(second);
         }
         return p;
     }
@@ -235,17 +235,13 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
         Operand<In_bf16> q[MT][PARTS][STEPS];
         float sum[MT][NG];
     };
-    static __device__ __forceinline__ void load(const AttendArgs& g, const char* p, bool there, int m, Query& y) {
+    static __device__ __forceinline__ void load(const AttendArgs& g, const char* p, int m, Query& y) {
         const int quarter = (int)__lane_id() >> 4;
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
             float x[CQ], total = 0.0f;
 #pragma unroll
-            for (int c = 0; c < CQ; c += 8) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[c + i] = 0.0f;
-                if (there) load_row<T, 8>(p + (n * GS + quarter * CQ + c) * 2, x + c);
-            }
+            for (int c = 0; c < CQ; c += 8) load_row<T, 8>(p + (n * GS + quarter * CQ + c) * 2, x + c);
 #pragma unroll
             for (int c = 0; c < CQ; ++c) total += x[c];
 #pragma unroll
@@ -258,8 +254,8 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
                 y.q[m][0][n * SPG + step] = hi;
                 if constexpr (PARTS == 2) y.q[m][1][n * SPG + step] = lo;
             }
-            total += __shfl_xor(total, 16, 64);
-            total += __shfl_xor(total, 32, 64);
+            total += lane_xor<16>(total);
+            total += lane_xor<32>(total);
             y.sum[m][n] = total * g.scale_log2;
         }
     }
@@ -368,8 +364,8 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
 #pragma unroll
             for (int n = 0; n < NG; ++n) {
                 float& z = zero[m][n];
-                z += __shfl_xor(z, 16, 64);
-                z += __shfl_xor(z, 32, 64);
+                z += lane_xor<16>(z);
+                z += lane_xor<32>(z);
 #pragma unroll
                 for (int u = 0; u < VU; ++u) o[m][n * VU + u] += z;
             }
@@ -467,17 +463,13 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
         float plain;
         int32_t rank;
     };
-    static __device__ __forceinline__ void load(const AttendArgs&, const char* p, bool there, int, Query& y) {
+    static __device__ __forceinline__ void load(const AttendArgs&, const char* p, int, Query& y) {
         const int quarter = (int)__lane_id() >> 4;
 #pragma unroll
         for (int n = 0; n < VN; ++n) {
             float x[CQ];
 #pragma unroll
-            for (int c = 0; c < CQ; c += 8) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[c + i] = 0.0f;
-                if (there) load_row<T, 8>(p + (n * GS + quarter * CQ + c) * 2, x + c);
-            }
+            for (int c = 0; c < CQ; c += 8) load_row<T, 8>(p + (n * GS + quarter * CQ + c) * 2, x + c);
 #pragma unroll
             for (int c = 0; c < CQ; ++c) y.x[n * CQ + c] = x[c];
         }
@@ -507,8 +499,8 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
                 split_key<In_bf16>(w, y.part[n * SPG + step]);
             }
         }
-        plain += __shfl_xor(plain, 16, 64);
-        plain += __shfl_xor(plain, 32, 64);
+        plain += lane_xor<16>(plain);
+        plain += lane_xor<32>(plain);
         y.plain = plain * g.scale_log2;
     }
 
@@ -549,8 +541,8 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
             total += w[0][i];
             w[0][i] *= kUp;
         }
-        total += __shfl_xor(total, 16, 64);
-        total += __shfl_xor(total, 32, 64);
+        total += lane_xor<16>(total);
+        total += lane_xor<32>(total);
         Operand<In_bf16> hi, lo;
         split(w[0], hi, lo);
 #pragma unroll
@@ -600,7 +592,7 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int32_t row = wave_row + 16 * m + a;
-        there[m] = row < rows;
+        there[m] = row < rows;  // one that is not there computes with the first, so that nothing waits for a condition
         token[m] = there[m] ? (int32_t)div_by((uint32_t)row, (uint32_t)g.repeat, g.inv_repeat) : 0;
         q_head[m] = head * g.repeat + (there[m] ? row - token[m] * g.repeat : 0);
     }
@@ -632,7 +624,7 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
             int32_t seen[MT];
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                S::load_query(g.q + q_head[m] * g.q_head + token[m] * g.q_row, there[m], quarter, q[m]);
+                S::load_query(g.q + q_head[m] * g.q_head + token[m] * g.q_row, quarter, q[m]);
                 seen[m] = causal ? min(tokens, token[m] + 1 + g.recent.rows - g.t_q) : tokens;
             }
             for (int32_t t = from; t < to; t += kStep)
@@ -652,7 +644,7 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
         F::fetch(g, head, t - s.front_tiles, next);  // the first tile is on its way while the queries are read
         typename F::Query query;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) F::load(g, g.q + q_head[m] * g.q_head + token[m] * g.q_row, there[m], m, query);
+        for (int m = 0; m < MT; ++m) F::load(g, g.q + q_head[m] * g.q_head + token[m] * g.q_row, m, query);
         f.template rescale<true>();
         for (int buffer = 0; t < stored_end; t += kStep, buffer ^= 1) {
             char* const here = mine + (NW == 1 ? 0 : buffer * F::STAGE);
@@ -674,8 +666,8 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
 
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        f.sum[m] += __shfl_xor(f.sum[m], 16, 64);
-        f.sum[m] += __shfl_xor(f.sum[m], 32, 64);
+        f.sum[m] += lane_xor<16>(f.sum[m]);
+        f.sum[m] += lane_xor<32>(f.sum[m]);
     }
     f.finish();
 

@@ -310,8 +310,8 @@ __global__ __launch_bounds__(F::THREADS, 2) void attend_shared_kernel(AttendArgs
 #pragma unroll
         for (int u = 0; u < STEPS; ++u) {
             const int c = quarter * (DP / 4) + 8 * u;
-            q[m][u].w = u32x4{0u, 0u, 0u, 0u};
-            if (there[m] && c < g.channels) q[m][u].w = *reinterpret_cast<const u32x4*>(p + c * 2);
+            q[m][u].w = *reinterpret_cast<const u32x4*>(p + (c < g.channels ? c : 0) * 2);
+            if (c >= g.channels) q[m][u].w = u32x4{0u, 0u, 0u, 0u};
         }
     }
     const bool works = wave_row < rows;  // a wave of a block's end has no rows but stages with the others
@@ -352,8 +352,8 @@ __global__ __launch_bounds__(F::THREADS, 2) void attend_shared_kernel(AttendArgs
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         float sum = f.sum[m];
-        sum += __shfl_xor(sum, 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
+        sum += lane_xor<16>(sum);
+        sum += lane_xor<32>(sum);
         if (!there[m]) continue;
         typedef typename Element<T>::type E;
         const int64_t at = (int64_t)q_head[m] * g.t_q + token[m];

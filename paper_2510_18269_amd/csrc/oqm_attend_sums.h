@@ -37,8 +37,8 @@ struct Sums {
         for (int m = 0; m < MT; ++m) {
             float high = fmaxf(fmaxf(fmaxf(w[m][0], w[m][1]), fmaxf(w[m][2], w[m][3])), fmaxf(fmaxf(w[m][4], w[m][5]), fmaxf(w[m][6], w[m][7])));
             if (__any(high > top[m] + kSlack)) {
-                high = fmaxf(high, __shfl_xor(high, 16, 64));
-                high = fmaxf(high, __shfl_xor(high, 32, 64));
+                high = fmaxf(high, lane_xor<16>(high));
+                high = fmaxf(high, lane_xor<32>(high));
                 const float next = fmaxf(top[m], high);
                 const float by = next == -__builtin_inff() ? 1.0f : exp2_of(top[m] - next);
                 top[m] = next;
@@ -65,12 +65,10 @@ struct Sums {
         }
     }
 
-    static __device__ __forceinline__ void load_query(const char* p, bool there, int quarter, Operand<T> (&q)[STEPS]) {
+    static __device__ __forceinline__ void load_query(const char* p, int quarter, Operand<T> (&q)[STEPS]) {
+        asm volatile("" ::: "memory");  // read again for the codes, not kept for them: the registers are wanted
 #pragma unroll
-        for (int u = 0; u < STEPS; ++u) {
-            q[u].w = u32x4{0u, 0u, 0u, 0u};
-            if (there) q[u].w = *reinterpret_cast<const u32x4*>(p + (quarter * (DP / 4) + 8 * u) * 2);
-        }
+        for (int u = 0; u < STEPS; ++u) q[u].w = *reinterpret_cast<const u32x4*>(p + (quarter * (DP / 4) + 8 * u) * 2);
     }
     // 32 tokens of rows as the model has them, from t0; `seen`: of the rows from the first, how many each query row sees.
     __device__ __forceinline__ void rows(const AttendArgs& g, const AttendRows& r, int head, int32_t t0, int32_t tokens, const Operand<T> (&q)[MT][STEPS],
