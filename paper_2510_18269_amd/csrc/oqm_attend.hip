@@ -445,12 +445,16 @@ __global__ __launch_bounds__(kBlock) void attend_join_many_kernel(AttendArgs g) 
     for (int w = 1; w < kBlock / 64; ++w) j.add(g.score_unit, tops[w][lane], totals[w][lane], sums[w][lane]);
     put_joined<T>(g, blockIdx.x, c, j);
 }
-// Up to this many parts a lane takes them all.
-constexpr int kFewParts = 8;
+// A lane takes all parts where they are few, or where the rows alone fill the chip: eight lanes to a part then only read the
+// same bytes by more workgroups. Whole call at 128 channels, a lane takes all / workgroups: 28 rows of 4, 6, 8, 12, 24 parts 7.9,
+// 8.8, 9.4, 9.6, 12.2 / 8.2, 8.2, 9.0, 8.6, 8.7 us; 448 rows of 25 30.3 / 27.8; 896 of 48 76.3 / 71.3; 1680 of 13 28.6 / 32.9;
+// 1792 of 27 111.1 / 113.3; 5040 of 9 43.3 / 61.3; 28000 of 5 175 / 283.
+constexpr int kFewParts = 4;
+constexpr uint32_t kLanesThatFill = 48 * 1024;
 template <typename T>
 void start_join(const AttendArgs& g, hipStream_t s) {
     const uint32_t rows = (uint32_t)(g.kv_heads * g.repeat * g.t_q), lanes = (uint32_t)(g.channels / 4);
-    if (g.splits <= kFewParts) {
+    if (g.splits <= kFewParts || rows * lanes >= kLanesThatFill) {
         // parts are cut from calls of 2048 waves of 16 rows or less: rows * lanes stays far inside 32 bits
         launch(attend_join_few_kernel<T>, dim3((rows * lanes + kBlock - 1) / kBlock), dim3(kBlock), 0, s, g, lanes, reciprocal_u32(lanes), rows);
     } else {

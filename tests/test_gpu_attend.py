@@ -64,7 +64,7 @@ def expected(c, q, x, idx, rows, scale):
         h = i // c.repeat
         both = [torch.cat([rows["front"][kv][h].double(), x[kv][slots, h].reshape(-1, c.d), rows["recent"][kv][h].double()]) for kv in (0, 1)]
         dots = q[i].double() @ both[0].T * scale
-        off = (q[i].double().abs() @ both[0].abs().T * scale).amax(-1, keepdim=True) * 2.0 ** -15 if both[0].shape[0] else torch.zeros((c.t_q, 1), device="cuda")
+        off = (q[i].double().abs() @ both[0].abs().T * abs(scale)).amax(-1, keepdim=True) * 2.0 ** -15 if both[0].shape[0] else torch.zeros((c.t_q, 1), device="cuda")
         if c.softcap:
             dots, off = c.softcap * torch.tanh(dots / c.softcap), off + c.softcap * 2.0 ** -20
         if c.causal:
@@ -271,3 +271,89 @@ def test_many_tokens_on_narrow_quant_groups(oqm, d, gs, bits, meta, G, dtype, t_
     """More query rows than the reconstruction of a tile is shared by: 3 * t_q, over holes, a ragged front and recent rows."""
     check(oqm, Case(d=d, gs=gs, bits=bits, meta=meta, G=G, dtype=dtype, t_q=t_q, repeat=3, T=30, k=21, holes=3, front=45, recent=t_q + 17 if causal else 70,
                     causal=causal, softcap=25.0 if G == 50 else 0.0, seed=t_q + d))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("bits", [4, 2])
+@pytest.mark.parametrize("d,gs,axis", [(64, 32, 0), (64, 64, 0), (128, 32, 0), (128, 128, 0), (256, 32, 0), (256, 64, 0), (256, 128, 0), (64, 64, 1), (128, 64, 1), (256, 64, 1)])
+def test_blocks_of_query_rows(oqm, d, gs, axis, bits, dtype):
+    """More than 16 query rows: every compiled form, the last block ragged."""
+    check(oqm, Case(d=d, gs=gs, axis=axis, bits=bits, dtype=dtype, t_q=31, recent=40, T=20, k=17, holes=2, seed=d + gs))
+
+
+@pytest.mark.parametrize("axis", [0, 1])
+@pytest.mark.parametrize("G", [1, 5, 31, 63, 64, 65, 130])
+def test_groups_that_end_inside_a_shared_tile(oqm, G, axis):
+    check(oqm, Case(G=G, axis=axis, T=11, k=9, holes=2, t_q=12, recent=12, seed=G))
+
+
+def test_offsets_beyond_32_bits(oqm):
+    """Slots more than 4 GiB into the storage, and rows half a GiB apart."""
+    H_k, R, d, G, T = 4, 7, 128, 196, 90000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(12)
+    cfg = oqm.make_config(1, H_k, H_k * R, d, G, 64, T)
+    codes = torch.empty((2, T, H_k, G, d // 2), dtype=torch.uint8, device="cuda")
+    meta = torch.empty((2, T, H_k, G * 2, 2), device="cuda")
+    slots = [3, T // 2, T - 1]
+    for t in slots:
+        codes[:, t] = torch.randint(0, 256, codes[:, t].shape, generator=g, device="cuda", dtype=torch.uint8)
+        meta[:, t, ..., 0] = torch.rand((2, H_k, G * 2), generator=g, device="cuda") * 0.3
+        meta[:, t, ..., 1] = torch.rand((2, H_k, G * 2), generator=g, device="cuda") * 2 - 2
+    far = torch.empty((2, 9 << 28), dtype=torch.bfloat16, device="cuda")
+    front = [x.as_strided((H_k, 9, d), (d, 1 << 28, 1)) for x in far]
+    for x in front:
+        x.normal_(generator=g)
+    small = torch.stack([codes[:, t] for t in slots], 1), torch.stack([meta[:, t] for t in slots], 1)
+    for t_q in (1, 9):
+        q = torch.randn((H_k * R, t_q, d), generator=g, device="cuda").bfloat16()
+        got = []
+        for arrays, idx, rows, n in (((codes, meta), slots, front, T), (small, [0, 1, 2], [x.contiguous() for x in front], 3)):
+            h = oqm.tom_oqm_create(oqm.make_config(1, H_k, H_k * R, d, G, 64, n))
+            oqm.tom_oqm_bind(h, *arrays, torch.empty(16, device="cuda"))
+            oqm.tom_oqm_set_num_groups(h, n)
+            out, lse = torch.empty_like(q), torch.empty((H_k * R, t_q), device="cuda")
+            ws = torch.empty(oqm.tom_oqm_attend_workspace_bytes(h, t_q, 9 + 3 * G), dtype=torch.uint8, device="cuda")
+            oqm.tom_oqm_attend(h, 0, q, out, torch.tensor(idx, dtype=torch.int32, device="cuda"), 3, rows[0], rows[1], lse=lse, workspace=ws)
+            torch.cuda.synchronize()
+            oqm.tom_oqm_destroy(h)
+            got.append((out, lse))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and bool(got[0][0].isfinite().all())
+    # and moved: kept at the front, copied to the end of another
+    h = oqm.tom_oqm_create(cfg)
+    keys = torch.zeros((T, H_k, d), device="cuda")
+    oqm.tom_oqm_bind(h, codes, meta, keys)
+    oqm.tom_oqm_set_num_groups(h, T)
+    oqm.tom_oqm_keep_groups(h, torch.tensor(slots, dtype=torch.int32, device="cuda"), 3)
+    torch.cuda.synchronize()
+    assert torch.equal(codes[:, :3], small[0]) and torch.equal(meta[:, :3], small[1])
+    oqm.tom_oqm_set_num_groups(h, T - 3)
+    oqm.tom_oqm_copy_groups(h, h, torch.tensor([2, 0, 1], dtype=torch.int32, device="cuda"), 3)
+    torch.cuda.synchronize()
+    assert torch.equal(codes[:, T - 3:], small[0][:, [2, 0, 1]]) and torch.equal(meta[:, T - 3:], small[1][:, [2, 0, 1]])
+    oqm.tom_oqm_destroy(h)
+
+
+def test_negative_zero_and_other_scales(oqm):
+    """scale below zero, zero, and as given; float32 and 16 bits."""
+    for dtype in ("f32", "bf16"):
+        for scale in (-0.07, 0.0, 0.25):
+            t, H_k, R, d, G, T = H.DT[dtype][1], 1, 3, 64, 20, 4
+            g = torch.Generator(device="cuda")
+            g.manual_seed(5)
+            c = Case(dtype=dtype, d=d, heads=H_k, repeat=R, G=G, gs=32, T=T, k=T, every=True, t_q=6, front=0, recent=9, layers=1)
+            codes, meta, x = stored(c, g)
+            h = oqm.tom_oqm_create(oqm.make_config(1, H_k, H_k * R, d, G, 32, T, in_dtype=H.DT[dtype][0], out_dtype=H.DT[dtype][0]))
+            oqm.tom_oqm_bind(h, codes, meta, torch.empty(16, device="cuda"))
+            oqm.tom_oqm_set_num_groups(h, T)
+            q = torch.randn((H_k * R, 6, d), generator=g, device="cuda").to(t)
+            recent = [torch.randn((H_k, 9, d), generator=g, device="cuda").to(t) for _ in range(2)]
+            out, lse = torch.empty_like(q), torch.empty((H_k * R, 6), device="cuda")
+            ws = torch.empty(oqm.tom_oqm_attend_workspace_bytes(h, 6, T * G + 9), dtype=torch.uint8, device="cuda")
+            oqm.tom_oqm_attend(h, 0, q, out, None, T, recent_k=recent[0], recent_v=recent[1], scale=scale, lse=lse, workspace=ws)
+            torch.cuda.synchronize()
+            oqm.tom_oqm_destroy(h)
+            none = torch.zeros((H_k, 0, d), device="cuda")
+            want, want_lse, tol, lse_tol = expected(c, q, x, None, {"front": [none, none], "recent": recent}, scale)
+            assert bool(((out.double() - want).abs() <= tol + want.abs() * torch.finfo(t).eps / 2).all())
+            assert bool(((lse.double() - want_lse).abs() <= lse_tol).all())
