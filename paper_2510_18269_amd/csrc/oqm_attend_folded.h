@@ -221,10 +221,12 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
         }
         if (tid < 2 * TT) {
             f32x2* at = reinterpret_cast<f32x2*>(lds + 2 * TT * STRIDE + tid * NG * 8);
+            const float unit = tid < TT ? g.scale_log2 * kDown : kUp;  // the scales as the scores, or p * s, want them
 #pragma unroll
             for (int i = 0; i < NG; ++i) {
                 f32x2 p = {0.f, 0.f};  // a token that is not there must not bring a NaN
                 if (f.seen) p = g.meta_bf16 ? widen_pair(f.meta[i]) : f32x2{__uint_as_float(f.meta[2 * i]), __uint_as_float(f.meta[2 * i + 1])};
+                p[0] *= unit;
                 at[i] = p;
             }
         }
@@ -270,7 +272,6 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
         const f32x2* km = reinterpret_cast<const f32x2*>(lds + 2 * TT * STRIDE) + sub * NG;
         const f32x2* vm = km + TT * NG;
         float w[MT][8];
-        const float unit = g.scale_log2 * kDown;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             f32x4 d[MT][NG];
@@ -292,20 +293,17 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f32x2* pair = km + (16 * half + 4 * quarter + i) * NG;
-                float scaled[MT], plain[MT];
+                float x[MT];
 #pragma unroll
-                for (int m = 0; m < MT; ++m) scaled[m] = plain[m] = 0.0f;
+                for (int m = 0; m < MT; ++m) x[m] = 0.0f;
 #pragma unroll
                 for (int n = 0; n < NG; ++n) {
                     const f32x2 p = pair[n];
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        scaled[m] = __builtin_fmaf(p[0], d[m][n][i], scaled[m]);
-                        plain[m] = __builtin_fmaf(p[1], y.sum[m][n], plain[m]);
-                    }
+                    for (int m = 0; m < MT; ++m) x[m] = __builtin_fmaf(p[0], d[m][n][i], __builtin_fmaf(p[1], y.sum[m][n], x[m]));
                 }
 #pragma unroll
-                for (int m = 0; m < MT; ++m) w[m][4 * half + i] = __builtin_fmaf(scaled[m], unit, plain[m]);
+                for (int m = 0; m < MT; ++m) w[m][4 * half + i] = x[m];
             }
         }
         S::finish_scores(g, w);
@@ -325,10 +323,9 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const f32x2 p = vm[(16 * (i / 4) + 4 * quarter + i % 4) * NG + n];
-                const float s = p[0] * kUp;
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    scaled[m][i] = w[m][i] * s;
+                    scaled[m][i] = w[m][i] * p[0];
                     zero[m][n] = __builtin_fmaf(w[m][i], p[1], zero[m][n]);
                 }
             }
