@@ -31,14 +31,15 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 
 // softcap * tanh(y) in units of log 2, from z = 2 log2(e) y: tanh y = 1 - 2 / (1 + 2^z).  The difference loses what the one has over
 // tanh y: an error of 2^-22 * softcap at any y, which 16-bit results do not show.
-__device__ __forceinline__ float capped(float z, float cap_log2) {
-    return __builtin_fmaf(-2.0f * cap_log2, __builtin_amdgcn_rcpf(1.0f + exp2_of(z)), cap_log2);
+// high: what z = infinity gives, cap_log2 or that less what scores are counted from.
+__device__ __forceinline__ float capped(float z, float cap_log2, float high) {
+    return __builtin_fmaf(-2.0f * cap_log2, __builtin_amdgcn_rcpf(1.0f + exp2_of(z)), high);
 }
 // Near zero by the series, for float32.
 __device__ __forceinline__ float capped_exactly(float z, float cap_log2) {
     const float y = z * (0.5f * kLn2), x = y * y;
     const float small = y * fmaf(x, fmaf(x, fmaf(x, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-    return x < 0.015625f ? cap_log2 * small : capped(z, cap_log2);
+    return x < 0.015625f ? cap_log2 * small : capped(z, cap_log2, cap_log2);
 }
 
 // ---- operands: 8 consecutive k of a row of a 16 x 16 x 32 product (16-bit types), or 8 products of one k a lane (float32) ----

@@ -196,7 +196,7 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
             if (g.meta_bf16) {
                 const uint32_t* w = reinterpret_cast<const uint32_t*>(m + (int64_t)tok * NG * 4);
 #pragma unroll
-                for (int i = 0; i < NG; ++i) f.meta[i] = w[i];
+                for (int i = 0; i < NG; ++i) f.meta[i] = w[i], f.meta[NG + i] = 0;  // all of it on both sides, or it is kept in memory
             } else {
                 const u32x2* w = reinterpret_cast<const u32x2*>(m + (int64_t)tok * NG * 8);
 #pragma unroll
@@ -271,7 +271,8 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
         const char* vc = lds + (TT + sub) * STRIDE;
         const f32x2* km = reinterpret_cast<const f32x2*>(lds + 2 * TT * STRIDE) + sub * NG;
         const f32x2* vm = km + TT * NG;
-        float w[MT][8];
+        float w[MT][8], base[MT], start[MT];
+        S::bases(g, base, start);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             f32x4 d[MT][NG];
@@ -295,7 +296,7 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
                 const f32x2* pair = km + (16 * half + 4 * quarter + i) * NG;
                 float x[MT];
 #pragma unroll
-                for (int m = 0; m < MT; ++m) x[m] = 0.0f;
+                for (int m = 0; m < MT; ++m) x[m] = start[m];
 #pragma unroll
                 for (int n = 0; n < NG; ++n) {
                     const f32x2 p = pair[n];
@@ -306,7 +307,7 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
                 for (int m = 0; m < MT; ++m) w[m][4 * half + i] = x[m];
             }
         }
-        S::finish_scores(g, w);
+        S::finish_scores(g, w, base);
         if (valid != 0xffffffffu) {
             const uint32_t mine = valid >> (4 * quarter);
 #pragma unroll
@@ -315,7 +316,7 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
 #pragma unroll
                     for (int m = 0; m < MT; ++m) w[m][i] = -__builtin_inff();
         }
-        this->probabilities(w);
+        this->probabilities(w, base);
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
             Operand<In_bf16> hi[MT], lo[MT];
@@ -360,7 +361,7 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int n = 0; n < NG; ++n) {
-                float& z = zero[m][n];
+                float z = zero[m][n];
                 z += lane_xor<16>(z);
                 z += lane_xor<32>(z);
 #pragma unroll
@@ -506,7 +507,9 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
         const char* kc = lds + sub * STRIDE;
         const char* vc = lds + (TT + sub) * STRIDE;
         const f32x2* vm = reinterpret_cast<const f32x2*>(lds + 2 * TT * STRIDE) + DP;
-        float w[1][8];
+        float w[1][8], base[1], start[1];
+        S::bases(g, base, start);
+        const float plain = y.plain + start[0];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             f32x4 d = {0.f, 0.f, 0.f, 0.f};
@@ -522,16 +525,16 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[0][4 * half + i] = __builtin_fmaf(d[i], g.scale_log2 * kDown, y.plain);
+            for (int i = 0; i < 4; ++i) w[0][4 * half + i] = __builtin_fmaf(d[i], g.scale_log2 * kDown, plain);
         }
-        S::finish_scores(g, w);
+        S::finish_scores(g, w, base);
         if (valid != 0xffffffffu) {
             const uint32_t mine = valid >> (4 * quarter);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (!(mine >> (16 * (i / 4) + i % 4) & 1u)) w[0][i] = -__builtin_inff();
         }
-        this->probabilities(w);
+        this->probabilities(w, base);
         float total = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {

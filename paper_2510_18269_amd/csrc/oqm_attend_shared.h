@@ -53,6 +53,8 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
             const u32x4 x = *reinterpret_cast<const u32x4*>(k + (int64_t)min(t0 + unit % 32, tokens - 1) * r.k_row + (c < g.channels ? c : 0) * 2);
 #pragma unroll
             for (int j = 0; j < 4; ++j) f.k[i][j] = x[j];
+            f.k_shift[i] = 0;
+            if constexpr (BF16_META) f.kp[i] = 0;
         }
 #pragma unroll
         for (int i = 0; i < KU; ++i) {
@@ -60,8 +62,10 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
             value_unit((i * THREADS + tid) % UNITS, c, half, quarter);
             const char* const p = v + (c < g.channels ? c : 0) * 2;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j) {
                 f.v[i][j] = *reinterpret_cast<const uint32_t*>(p + (int64_t)min(t0 + 16 * half + 4 * quarter + j, tokens - 1) * r.v_row);
+                if constexpr (BF16_META) f.vp[i][j] = 0;  // all words of it on both sides, or some are kept in memory
+            }
         }
     }
     // Where the tile's tokens stand.  In groups of 32 tokens or more they lie in two groups at most, and the slots are the wave's.
@@ -120,6 +124,7 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
             const int c0 = (i * THREADS + tid) / 32 % (DP / 8) * 8, c = c0 < g.channels ? c0 : 0;
             const uint64_t at = reinterpret_cast<uint64_t>(kc) + (uint64_t)k_code + ((uint32_t)tok * row_bits + (uint32_t)(c * g.bits)) / 8;
             f.k[i][0] = *reinterpret_cast<const uint32_t*>(at & ~uint64_t{3});
+            f.k[i][1] = f.k[i][2] = f.k[i][3] = 0;
             f.k_shift[i] = (uint32_t)(at & 3u) * 8u;
             f.kp[i] = k_meta[((uint32_t)tok * (uint32_t)g.channels + (uint32_t)c) >> g.qgroup_log2];
         }
@@ -241,15 +246,16 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
                 for (int m = 0; m < MT; ++m) d[half][m] = product(x, q[m][u], d[half][m]);
             }
         }
-        float w[MT][8];
+        float w[MT][8], base[MT], start[MT];
+        S::bases(g, base, start);
         bool all = valid == 0xffffffffu;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             all = all && seen[m] >= 32;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[m][i] = d[i / 4][m][i % 4] * g.scale_log2;
+            for (int i = 0; i < 8; ++i) w[m][i] = __builtin_fmaf(d[i / 4][m][i % 4], g.scale_log2, start[m]);
         }
-        S::finish_scores(g, w);
+        S::finish_scores(g, w, base);
         if (!__all(all)) {
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
@@ -259,7 +265,7 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
                     if (!(mine >> (16 * (i / 4) + i % 4) & 1u)) w[m][i] = -__builtin_inff();
             }
         }
-        this->probabilities(w);
+        this->probabilities(w, base);
         Operand<T> hi[MT], lo[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) split(w[m], hi[m], lo[m]);

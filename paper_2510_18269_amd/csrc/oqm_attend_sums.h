@@ -31,15 +31,17 @@ struct Sums {
             for (int n = 0; n < NZ; ++n) zero[m][n] = 0.0f;
         }
     }
-    // Scores to probabilities.
-    __device__ __forceinline__ void probabilities(float (&w)[MT][8]) {
+    // What scores are counted from: the running maximum, or 0 before there is one.
+    __device__ __forceinline__ float from(int m) const { return top[m] == -__builtin_inff() ? 0.0f : top[m]; }
+    // Scores, counted from `base`, to probabilities.
+    __device__ __forceinline__ void probabilities(float (&w)[MT][8], const float (&base)[MT]) {
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             float high = fmaxf(fmaxf(fmaxf(w[m][0], w[m][1]), fmaxf(w[m][2], w[m][3])), fmaxf(fmaxf(w[m][4], w[m][5]), fmaxf(w[m][6], w[m][7])));
-            if (__any(high > top[m] + kSlack)) {
+            if (__any(high > (top[m] - base[m]) + kSlack)) {
                 high = fmaxf(high, lane_xor<16>(high));
                 high = fmaxf(high, lane_xor<32>(high));
-                const float next = fmaxf(top[m], high);
+                const float next = fmaxf(top[m], high + base[m]);
                 const float by = next == -__builtin_inff() ? 1.0f : exp2_of(top[m] - next);
                 top[m] = next;
                 sum[m] *= by;
@@ -47,21 +49,33 @@ struct Sums {
                 for (int n = 0; n < DP / 16; ++n) o[m][n] *= by;
 #pragma unroll
                 for (int n = 0; n < NZ; ++n) zero[m][n] *= by;
+                const float up = base[m] - from(m);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[m][i] += up;
             }
-            const float from = top[m] == -__builtin_inff() ? 0.0f : top[m];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                w[m][i] = exp2_of(w[m][i] - from);
+                w[m][i] = exp2_of(w[m][i]);
                 sum[m] += w[m][i];
             }
         }
     }
-    static __device__ __forceinline__ void finish_scores(const AttendArgs& g, float (&w)[MT][8]) {
+    // Scores are computed from `start` on, and without a cap done; with one they are counted from the maximum as it is put on.
+    __device__ __forceinline__ void bases(const AttendArgs& g, float (&base)[MT], float (&start)[MT]) const {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            base[m] = from(m);
+            start[m] = g.cap_log2 != 0.0f ? 0.0f : -base[m];
+        }
+    }
+    static __device__ __forceinline__ void finish_scores(const AttendArgs& g, float (&w)[MT][8], const float (&base)[MT]) {
         if (g.cap_log2 != 0.0f) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int m = 0; m < MT; ++m) {
+                const float high = g.cap_log2 - base[m];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[m][i] = capped(w[m][i], g.cap_log2);
+                for (int i = 0; i < 8; ++i) w[m][i] = capped(w[m][i], g.cap_log2, high);
+            }
         }
     }
 
@@ -95,7 +109,8 @@ struct Sums {
             for (int u = 0; u < STEPS; ++u) kx[half][u] = *reinterpret_cast<const u32x4*>(p + 16 * u);
         }
         if constexpr (MT == 1) load_values();  // in flight with the keys; with two blocks of rows there are no registers for it
-        float w[MT][8];
+        float w[MT][8], base[MT], start[MT];
+        bases(g, base, start);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             f32x4 d[MT];
@@ -111,15 +126,15 @@ struct Sums {
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[m][4 * half + i] = d[m][i] * g.scale_log2;
+                for (int i = 0; i < 4; ++i) w[m][4 * half + i] = __builtin_fmaf(d[m][i], g.scale_log2, start[m]);
         }
-        finish_scores(g, w);
+        finish_scores(g, w, base);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (t0 + 16 * (i / 4) + 4 * quarter + i % 4 >= seen[m]) w[m][i] = -__builtin_inff();
-        probabilities(w);
+        probabilities(w, base);
         if constexpr (MT > 1) load_values();
         Operand<T> hi[MT], lo[MT];
 #pragma unroll
