@@ -54,7 +54,7 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
 #pragma unroll
             for (int j = 0; j < 4; ++j) f.k[i][j] = x[j];
             f.k_shift[i] = 0;
-            if constexpr (BF16_META) f.kp[i] = 0;
+            if constexpr (BF16_META && DP <= 128) f.kp[i] = 0;
         }
 #pragma unroll
         for (int i = 0; i < KU; ++i) {
@@ -64,7 +64,7 @@ struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 f.v[i][j] = *reinterpret_cast<const uint32_t*>(p + (int64_t)min(t0 + 16 * half + 4 * quarter + j, tokens - 1) * r.v_row);
-                if constexpr (BF16_META) f.vp[i][j] = 0;  // all words of it on both sides, or some are kept in memory
+                if constexpr (BF16_META && DP <= 128) f.vp[i][j] = 0;  // all words of it on both sides, or some are kept in memory
             }
         }
     }
