@@ -88,12 +88,14 @@ inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
 }
 
 // Waves of the folded kernels that a SIMD holds: what their registers leave, and what the kernels are bound to.  Workgroups have
-// one wave on each SIMD, so that it is also the workgroups of a compute unit.
+// one wave on each SIMD, so that it is also the workgroups of a compute unit.  28 query heads on 4, us with one wave less / as it is:
+// 256 channels, 1000 tokens over 32 groups of 196 926 / 627, 64 over 128 191 / 133; one more spills: one binary16 token over 2000
+// groups of 256 channels 157 (166 with two), over 3600 of 128 channels in quant-groups of 32 126 (179 with three), 64 98 (101).
 constexpr int attend_waves(int channels, int qgroup, bool tokens, bool f16, bool few_rows) {
-    if (channels == 256) return 1;
+    if (channels == 256) return tokens || (f16 && few_rows) ? 1 : 2;
     if (tokens) return channels == 64 ? 3 : 2;
     if (channels == 64) return 4;
-    return (qgroup == 32 && (f16 || few_rows)) || (f16 && few_rows) ? 2 : 3;
+    return (qgroup == 32 && (f16 || few_rows)) || (qgroup == 64 && f16 && few_rows) ? 2 : 3;
 }
 
 // Parts that the rows of a call are cut into, each with its own maximum and sum.  Never fewer where there are more rows: the
