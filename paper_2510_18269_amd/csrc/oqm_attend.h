@@ -73,11 +73,12 @@ struct AttendForm {
 // matrix cores (32 channels of keys, 16 of values) lies in one of them, or quant-groups along the tokens, where a tile of 32 tokens
 // lies in one of them (mostly empty if they are short, and still the faster: 255 groups of 1 / 5 / 15 tokens, one new token, 135 / 44 /
 // 27 us in the general form, 13.4 / 12.9 / 13.1 folded).  Its workgroups have 16 rows, which their waves share, or 16 a wave.
-// (32 a wave spare a fifth of the instructions but leave two waves a SIMD instead of three: 1000 tokens over 32 groups 332 us, 283
-// with 16; 64 over 128 groups 116 and 113.)  Shared: other 16-bit forms of the head_dim axis where more than 256 query rows are to
+// (32 a wave spare a fifth of the instructions but leave two waves a SIMD instead of three: 1000 tokens over 32 groups 332 us where 16
+// took 283; 64 over 128 groups 116 and 113.)  Shared: other 16-bit forms of the head_dim axis where more than 256 query rows are to
 // share a tile's reconstruction.  28 query heads on 4 of 128 channels, 64 groups of 50 tokens in quant-groups of 16, us, general /
-// shared: 16 tokens (112 rows) 31.8 / 44.9, 24 (168) 39.3 / 44.5, 64 (448) 62.1 / 52.6, 200 (1400) 149 / 79; 64 of 64 channels 41.2 /
-// 35.4, of 256 channels 152 / 100.  The folded form of quant-groups of 64 and 64 tokens 39.5.
+// shared: 16 tokens (112 rows) 35.0 / 41.0, 24 (168) 42.3 / 47.9, 36 (252) 52.9 / 52.2, 48 (336) 60.8 / 54.8, 64 68.5 / 53.6, 200 192 /
+// 69.1; of 64 channels 36 30.7 / 35.2, 64 41.3 / 38.0; of 256 channels 36 91.1 / 89.3, 64 136 / 94.2; binary16 36 45.4 / 50.3, 64 55.2 /
+// 52.3.  The folded form of quant-groups of 64 and 64 tokens 29.3.
 inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
     const bool tokens = c.qaxis == TOM_QAXIS_TOKENS, f32 = c.out_dtype == TOM_F32;
     const int64_t rows = (int64_t)(c.n_q_heads / c.n_kv_heads) * t_q;

@@ -16,6 +16,8 @@ namespace oqm {
 //   V operand  lane (l % 16, l / 16): of the 8 tokens whose scores it holds, VN runs of VU channels
 // Along the tokens' axis a tile lies in one group, whose pairs a lane then reads once.  Where a tile's channels are padding or a
 // token is not there, what is read instead is some valid place, and not used.
+// Latency bounds it where rows are few (float32, 2 heads of 64 channels, 72 rows: 7 us), the vector unit, which takes every
+// element apart in every wave, where they are many: 64 bfloat16 tokens of 28 heads over 64 groups of 50 in quant-groups of 16 68 us.
 template <typename T, int DP, bool TOKEN_AXIS>
 struct General {
     static constexpr int VU = DP / 16 < 8 ? DP / 16 : 8, VN = DP / 16 / VU, STEPS = DP / 32;

@@ -5,8 +5,9 @@
 //   keys    [half][step][lane][8 channels]       lane = (token of the half, quarter of the channels)
 //   values  [block of channels][lane][8 tokens]  lane = (channel of the block, quarter of the tokens)
 // Eight waves of 32 rows (of 256 channels: 16) share a tile.  They walk from barrier to barrier in step, so that matrix and vector
-// unit are rarely busy at once: 1000 tokens over 32 groups with a cap in 472 us, where the folded form, whose waves pair up on two
-// workgroups a compute unit, takes 330.  It is for the layouts that the folded form does not cover.
+// unit are rarely busy at once: 1000 tokens over 32 groups of quant-groups of 64 with a cap took 472 us, where the folded form,
+// whose waves pair up on several workgroups a compute unit, takes 286.  It is for the layouts that the folded form does not cover:
+// 64 tokens over 128 groups of 196 in quant-groups of 16 134 us.
 #pragma once
 
 #include "oqm_attend_sums.h"

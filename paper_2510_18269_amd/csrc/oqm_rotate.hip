@@ -329,8 +329,10 @@ tom_status_t tom_oqm_rotate(const tom_oqm_rotary_t* r, const double* turns, floa
     g.rotary_dim = r->rotary_dim;
     g.pair_slots = pair_slots;
     g.heads = (uint32_t)heads;
-    // Heads a lane takes one after the other share its cosines; small calls take one, so that every head has lanes of its own.  The
-    // same 719 MB, us at 2 / 4 / 8 / 16 heads: 126.7 / 123.2 / 135.5 / 161.
+    // Heads a lane takes one after the other share its cosines; small calls take one, so that every head has lanes of its own.  28 layers x
+    // 4 heads x 12544 tokens of 128 channels (719 MB), us at 2 / 4 / 8 / 16 heads: 126.7 / 123.2 / 135.5 / 161.  28 + 2 * 4 heads of 128
+    // channels, us of 300 / 700 / 1333 / 3000 / 6000 tokens: from 512K lanes up 7.46 / 7.73 / 7.64 / 11.97 / 20.16, never 7.37 /
+    // 7.80 / 7.74 / 12.85 / 21.50, from 128K up 7.33 / 7.80 / 8.05 / 12.13 / 20.14.
     g.heads_per_lane = 1;
     while (g.heads_per_lane < 4 && (uint64_t)one->rows * heads * lanes / g.heads_per_lane > 512u * 1024u) g.heads_per_lane *= 2;
     g.parts = (g.heads + g.heads_per_lane - 1) / g.heads_per_lane;
@@ -340,8 +342,8 @@ tom_status_t tom_oqm_rotate(const tom_oqm_rotary_t* r, const double* turns, floa
     g.sets = (uint64_t)g.parts * (uint64_t)one->rows;
     const uint32_t sets_per_block = threads / lanes;
     const dim3 grid((uint32_t)((g.sets + sets_per_block - 1) / sets_per_block)), block(threads);
-    // Rows that the last-level cache (256 MB) cannot hold until somebody reads them are read and written past the caches.  28 layers x
-    // 4 heads x 12544 tokens of 128 channels (719 MB), us, through / past: 138 / 123.2 = 5.8 TB/s.
+    // Rows that the last-level cache (256 MB) cannot hold until somebody reads them are read and written past the caches.  The
+    // same 719 MB, us, through / past: 138 / 123.2 = 5.8 TB/s.
     const bool large = (uint64_t)one->rows * (uint64_t)heads * (uint64_t)one->channels * (uint64_t)e * 2 >= (uint64_t)256 << 20;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's
