@@ -70,7 +70,7 @@ __global__ __launch_bounds__(1024) void move_groups_kernel(GroupArgs g) {
 }
 
 typedef uint32_t piece16 __attribute__((ext_vector_type(4)));
-typedef uint32_t piece8 __attribute__((ext_vector_type(2)));
+typedef uint64_t piece8;
 
 template <bool IN_PLACE>
 hipError_t launch_move_groups(const tom_oqm_t& to, const tom_oqm_t& from, const int32_t* idx, int32_t n, int32_t first_slot, hipStream_t s) {

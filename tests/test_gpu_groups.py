@@ -31,7 +31,8 @@ def planes(mem):
 
 
 SHAPES = [dict(), dict(L=1, heads=1, d=8, G=1, gs=8, bits=2), dict(L=1, heads=1, d=8, G=1, gs=8), dict(L=3, heads=1, d=24, G=7, gs=8, bits=2, meta="bf16"),
-          dict(heads=4, d=128, G=196, gs=64), dict(L=1, heads=3, d=72, G=11, axis=1, meta="bf16"), dict(L=1, heads=1, d=16, G=3, gs=8, bits=2)]
+          dict(heads=4, d=128, G=196, gs=64), dict(L=1, heads=3, d=72, G=11, axis=1, meta="bf16"), dict(L=1, heads=1, d=16, G=3, gs=8, bits=2),
+          dict(L=2, heads=1, d=16, G=3, gs=16)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
