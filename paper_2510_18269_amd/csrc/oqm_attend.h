@@ -77,7 +77,7 @@ struct AttendForm {
 // took 283; 64 over 128 groups 116 and 113.)  Shared: other 16-bit forms of the head_dim axis where more than 256 query rows are to
 // share a tile's reconstruction.  28 query heads on 4 of 128 channels, 64 groups of 50 tokens in quant-groups of 16, us, general /
 // shared: 16 tokens (112 rows) 35.0 / 41.0, 24 (168) 42.3 / 47.9, 36 (252) 52.9 / 52.2, 48 (336) 60.8 / 54.8, 64 68.5 / 53.6, 200 192 /
-// 69.1; of 64 channels 36 30.7 / 35.2, 64 41.3 / 38.0; of 256 channels 36 91.1 / 89.3, 64 136 / 94.2; binary16 36 45.4 / 50.3, 64 55.2 /
+// 69.1; of 64 channels 36 30.7 / 35.2, 64 41.3 / 38.0; of 256 channels 36 88.9 / 89.5, 64 120 / 94.4; binary16 36 45.4 / 50.3, 64 55.2 /
 // 52.3.  The folded form of quant-groups of 64 and 64 tokens 29.3.
 inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
     const bool tokens = c.qaxis == TOM_QAXIS_TOKENS, f32 = c.out_dtype == TOM_F32;

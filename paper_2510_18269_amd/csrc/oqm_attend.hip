@@ -279,8 +279,11 @@ struct General {
     }
 };
 
+// Waves a SIMD: 192 channels, 196 tokens a group, in quant-groups of 32, with one / two: 24 bfloat16 tokens over 64 groups 172 / 136 us,
+// one over 1000 233 / 172; 64 float32 ones 480 / 382; 96 channels with two / three: 72.0 / 70.7, 88.7 / 88.9, 199 / 200.  Along the
+// tokens, of groups of 50, whose pairs want the registers, with one / two: 97 / 145, 117 / 180, 247 / 389.
 template <typename T, int DP, bool TOKEN_AXIS>
-__global__ __launch_bounds__(kBlock, DP == 64 ? (TOKEN_AXIS ? 2 : 3) : DP == 128 ? 2 : 1) void attend_kernel(AttendArgs g) {
+__global__ __launch_bounds__(kBlock, DP == 64 ? (TOKEN_AXIS ? 2 : 3) : DP == 128 || !TOKEN_AXIS ? 2 : 1) void attend_kernel(AttendArgs g) {
     typedef General<T, DP, TOKEN_AXIS> Form;
     const Item item = item_of(g, (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * (kBlock / 64) + threadIdx.x / 64)));
     const uint32_t cut = item.cut;
