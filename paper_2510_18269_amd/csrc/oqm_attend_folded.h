@@ -694,7 +694,7 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
 #pragma unroll
                     for (int u = 0; u < VU; u += 2)
                         *reinterpret_cast<f32x2*>(row + n * GS + (4 * quarter + i) * VU + u) = f32x2{f.o[m][n * VU + u][i], f.o[m][n * VU + u + 1][i]};
-            if (quarter == 0) *reinterpret_cast<f32x2*>(row + DP) = f32x2{f.top[m], f.sum[m]};
+            if (quarter == 0) *reinterpret_cast<f32x2*>(row + DP) = f32x2{f.ref[m], f.sum[m]};
         }
         __syncthreads();
         constexpr int kLanes = DP / 4;  // of a row
@@ -758,8 +758,8 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
                     }
                 }
             if (quarter == 0) {
-                if (g.splits > 1) g.part_stat[at * g.splits + cut] = f32pair{f.top[m], f.sum[m]};
-                else if (g.lse) g.lse[at] = f.sum[m] > 0.0f ? (f.top[m] + __builtin_amdgcn_logf(f.sum[m])) * kLn2 : -__builtin_inff();
+                if (g.splits > 1) g.part_stat[at * g.splits + cut] = f32pair{f.ref[m], f.sum[m]};
+                else if (g.lse) g.lse[at] = f.sum[m] > 0.0f ? (f.ref[m] + __builtin_amdgcn_logf(f.sum[m])) * kLn2 : -__builtin_inff();
             }
         }
     }

@@ -386,8 +386,8 @@ __global__ __launch_bounds__(F::THREADS, 2) void attend_shared_kernel(AttendArgs
                 }
             }
         if (quarter == 0) {
-            if (g.splits > 1) g.part_stat[at * g.splits + item.cut] = f32pair{f.top[m], sum};
-            else if (g.lse) g.lse[at] = sum > 0.0f ? (f.top[m] + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
+            if (g.splits > 1) g.part_stat[at * g.splits + item.cut] = f32pair{f.ref[m], sum};
+            else if (g.lse) g.lse[at] = sum > 0.0f ? (f.ref[m] + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
         }
     }
 }

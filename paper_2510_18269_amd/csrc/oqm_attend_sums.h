@@ -5,7 +5,7 @@
 
 namespace oqm {
 
-constexpr float kSlack = 8.0f;                    // a maximum may lag behind by this (units of log 2) before sums are scaled anew
+constexpr float kSlack = 8.0f;                    // scores may pass what they are counted from by this (units of log 2) before sums are scaled anew
 
 // The sums of a wave's query rows, and the tiles of rows as the model has them.  A lane's channels of V^T: VU of each of VN runs of
 // GS channels.  NZ: sums that are scaled with the others.
@@ -18,12 +18,12 @@ struct Sums {
 
     f32x4 o[MT][DP / 16];
     float zero[MT][NZ];
-    float top[MT], sum[MT];
+    float ref[MT], sum[MT];  // what the scores and the sums are counted from: a maximum that has been; -infinity before there is one
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            top[m] = -__builtin_inff();
+            ref[m] = -__builtin_inff();
             sum[m] = 0.0f;
 #pragma unroll
             for (int n = 0; n < DP / 16; ++n) o[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -31,27 +31,28 @@ struct Sums {
             for (int n = 0; n < NZ; ++n) zero[m][n] = 0.0f;
         }
     }
-    // What scores are counted from: the running maximum, or 0 before there is one.
-    __device__ __forceinline__ float from(int m) const { return top[m] == -__builtin_inff() ? 0.0f : top[m]; }
-    // Scores, counted from `base`, to probabilities.
+    __device__ __forceinline__ float from(int m) const { return ref[m] == -__builtin_inff() ? 0.0f : ref[m]; }
+    // Scores, counted from `base`, to probabilities.  Where a score passes the slack, the tile's are counted from the highest of them by
+    // their differences.  `ref` is rounded where scores are so large that float32 rounds them (from 2^27 on by 8 and more: 2^8 in a probability
+    // and beyond what 16 bits hold), so the next tile may count from beside it; it will then pass the slack again.
     __device__ __forceinline__ void probabilities(float (&w)[MT][8], const float (&base)[MT]) {
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             float high = fmaxf(fmaxf(fmaxf(w[m][0], w[m][1]), fmaxf(w[m][2], w[m][3])), fmaxf(fmaxf(w[m][4], w[m][5]), fmaxf(w[m][6], w[m][7])));
-            if (__any(high > (top[m] - base[m]) + kSlack)) {
+            const float level = ref[m] - base[m];  // 0, or -infinity
+            if (__any(high > level + kSlack)) {
                 high = fmaxf(high, lane_xor<16>(high));
                 high = fmaxf(high, lane_xor<32>(high));
-                const float next = fmaxf(top[m], high + base[m]);
-                const float by = next == -__builtin_inff() ? 1.0f : exp2_of(top[m] - next);
-                top[m] = next;
+                const float peak = fmaxf(high, level);
+                const float by = exp2_of(fminf(-peak, 0.0f)), down = fmaxf(peak, -__FLT_MAX__);  // sums that have not begun are zero
+                ref[m] = base[m] + peak;
                 sum[m] *= by;
 #pragma unroll
                 for (int n = 0; n < DP / 16; ++n) o[m][n] *= by;
 #pragma unroll
                 for (int n = 0; n < NZ; ++n) zero[m][n] *= by;
-                const float up = base[m] - from(m);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[m][i] += up;
+                for (int i = 0; i < 8; ++i) w[m][i] -= down;
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
