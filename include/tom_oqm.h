@@ -402,8 +402,9 @@ size_t tom_oqm_attend_workspace_bytes(const tom_oqm_t* h, int32_t t_q, int64_t r
  *   out = sum_j p_j v_j,   p = softmax_j(w_j),   w_j = scale <q, k_j>, or softcap * tanh(scale <q, k_j> / softcap)
  * over the front rows, the G rows code * s + m of each group, and the recent rows.  Query head i reads KV head
  * i / (H_q / H_k).  Codes enter the products as they are and (s, m) in float32 where quant-groups have 32 channels or
- * more (sums there stay finite for |s| below 2^54 and queries, or queries times s, below 2^63); other forms split what
- * they reconstruct into 16-bit parts.  Scores, softmax and sums are float32.
+ * more (sums there stay finite for |s| below 2^54, with binary16 2^47, and queries, or queries times s, below 2^63);
+ * other forms split what they reconstruct into 16-bit parts.  Scores, softmax and sums are float32; probabilities enter the
+ * products as two 16-bit parts, 2^-17 of each (binary16: 2^-23 of each, or 2^-39 of the largest).
  *   q, out     [H_q][t_q][d] of cfg.out_dtype, any strides that are multiples of 16 bytes
  *   idx        device int32 [k_eff]: the groups, in any order, each as often as it stands there; an index outside [0, T)
  *              is a hole that nobody sees.  NULL: the groups 0 .. k_eff - 1, k_eff <= T

@@ -26,6 +26,8 @@ struct General {
     // A dot in float32 is added up in as many chains, joined by pairs: results of 256 channels with outlier keys 2.4e-6 from 64 bits with
     // one chain, 1.2e-6 with four.
     static constexpr int CHAINS = !__is_same(T, In_f32) ? 1 : STEPS < 4 ? STEPS : 4;
+    // Probabilities of binary16 are raised by 2^15 until the sums are done: two parts of one end at 2^-25, and so would the tail of a softmax.
+    static constexpr float RAISED = __is_same(T, In_f16) ? 15.0f : 0.0f;
     Operand<T> q[STEPS];
     f32x4 o[DP / 16];
     float top, sum;
@@ -59,7 +61,8 @@ struct General {
         const float from = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            w[i] = exp2_of((w[i] - from) * g.score_unit);
+            if constexpr (RAISED != 0.0f) w[i] = exp2_of(__builtin_fmaf(w[i] - from, g.score_unit, RAISED));
+            else w[i] = exp2_of((w[i] - from) * g.score_unit);
             sum += w[i];
         }
     }
@@ -330,6 +333,11 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? (TOKEN_AXIS ? 2 : 3) : DP == 128
     float sum = f.sum;
     sum += lane_xor<16>(sum);
     sum += lane_xor<32>(sum);
+    if constexpr (Form::RAISED != 0.0f) {
+        sum *= 0x1p-15f;
+#pragma unroll
+        for (int n = 0; n < DP / 16; ++n) f.o[n] *= 0x1p-15f;
+    }
     if (!there) return;
     // the lane holds channels run(v) + VU * (4 * quarter + i) + 0 .. VU - 1 of its query row
     const float by = sum > 0.0f ? 1.0f / sum : 0.0f;

@@ -64,7 +64,8 @@ __device__ __forceinline__ f32x4 product(const Operand<In_f32>& a, const Operand
     for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i], b.x[i], c, 0, 0, 0);
     return c;
 }
-// x = hi + lo + a rest of 2^-17 of it (bfloat16) or 2^-23 (binary16); float32 has no rest in hi.
+// x = hi + lo + a rest of 2^-17 of it (bfloat16), or of 2^-23 of it but up to 2^-25 where it is small (binary16: half its last place there,
+// no more than a reconstructed element loses when it is rounded to binary16); float32 has no rest in hi.
 __device__ __forceinline__ void split(const float (&x)[8], Operand<In_bf16>& hi, Operand<In_bf16>& lo) {
     hi.w = pack_items(In_bf16{}, x);
     float r[8];

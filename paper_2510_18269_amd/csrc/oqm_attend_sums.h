@@ -5,7 +5,14 @@
 
 namespace oqm {
 
-constexpr float kSlack = 8.0f;                    // scores may pass what they are counted from by this (units of log 2) before sums are scaled anew
+// Scores are counted from RAISED below a maximum, and may pass that maximum by SLACK (units of log 2) before sums are scaled anew.  In
+// bfloat16 two parts hold a probability to 2^-17 of itself however small it is: it is the maximum itself, and the lag spares most of the
+// scaling.  Two parts of binary16 end at 2^-25: counted from the maximum, a probability below 2^-25 would be left out of the values' sums,
+// though not out of the sum that divides them.  Counted from 14 below they end at 2^-39, and reach 2^15.9, where binary16 ends at 65504.
+// 1000 binary16 tokens over 32 groups, capped / 64 over 128 groups in quant-groups of 32 / 64, us, by RAISED and SLACK: 0 and 8
+// 304 / 108.8 / 79.9, 14 and 1.9 306 / 111.2 / 80.5, 15 and 0.9 311 / 112.1 / 82.0, 15 and 0 323 / 113.5 / 85.2.
+template <typename T> constexpr float kRaised = __is_same(T, In_f16) ? 14.0f : 0.0f;
+template <typename T> constexpr float kSlack = __is_same(T, In_f16) ? 1.9f : 8.0f;
 
 // The sums of a wave's query rows, and the tiles of rows as the model has them.  A lane's channels of V^T: VU of each of VN runs of
 // GS channels.  NZ: sums that are scaled with the others.
@@ -18,7 +25,7 @@ struct Sums {
 
     f32x4 o[MT][DP / 16];
     float zero[MT][NZ];
-    float ref[MT], sum[MT];  // what the scores and the sums are counted from: a maximum that has been; -infinity before there is one
+    float ref[MT], sum[MT];  // what the scores and the sums are counted from: RAISED below a maximum that has been; -infinity before there is one
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -32,27 +39,30 @@ struct Sums {
         }
     }
     __device__ __forceinline__ float from(int m) const { return ref[m] == -__builtin_inff() ? 0.0f : ref[m]; }
-    // Scores, counted from `base`, to probabilities.  Where a score passes the slack, the tile's are counted from the highest of them by
-    // their differences.  `ref` is rounded where scores are so large that float32 rounds them (from 2^27 on by 8 and more: 2^8 in a probability
-    // and beyond what 16 bits hold), so the next tile may count from beside it; it will then pass the slack again.
+    // Scores, counted from `base`, to probabilities.  Where a score passes the slack, the tile's are counted from RAISED below the highest
+    // of them by their differences.  `ref` is rounded where scores are so large that float32 rounds them (from 2^27 on by 8 and more: 2^8
+    // in a probability and beyond what 16 bits hold), so the next tile may count from beside it; it will then pass the slack again.
     __device__ __forceinline__ void probabilities(float (&w)[MT][8], const float (&base)[MT]) {
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             float high = fmaxf(fmaxf(fmaxf(w[m][0], w[m][1]), fmaxf(w[m][2], w[m][3])), fmaxf(fmaxf(w[m][4], w[m][5]), fmaxf(w[m][6], w[m][7])));
-            const float level = ref[m] - base[m];  // 0, or -infinity
-            if (__any(high > level + kSlack)) {
+            const float level = (ref[m] - base[m]) + kRaised<T>;  // RAISED, or -infinity
+            if (__any(high > level + kSlack<T>)) {
                 high = fmaxf(high, lane_xor<16>(high));
                 high = fmaxf(high, lane_xor<32>(high));
                 const float peak = fmaxf(high, level);
-                const float by = exp2_of(fminf(-peak, 0.0f)), down = fmaxf(peak, -__FLT_MAX__);  // sums that have not begun are zero
-                ref[m] = base[m] + peak;
+                const float by = exp2_of(fminf(kRaised<T> - peak, 0.0f)), down = fmaxf(peak, -__FLT_MAX__);  // sums that have not begun are zero
+                ref[m] = base[m] + (peak - kRaised<T>);
                 sum[m] *= by;
 #pragma unroll
                 for (int n = 0; n < DP / 16; ++n) o[m][n] *= by;
 #pragma unroll
                 for (int n = 0; n < NZ; ++n) zero[m][n] *= by;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[m][i] -= down;
+                for (int i = 0; i < 8; ++i) {
+                    w[m][i] -= down;
+                    if constexpr (kRaised<T> != 0.0f) w[m][i] += kRaised<T>;
+                }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
