@@ -301,9 +301,6 @@ class Rotary:
     turns: torch.Tensor    # float64 [rotary_dim / 2]: whole turns a position
     amplitude: float
 
-    def __post_init__(self):
-        self._address = C.addressof(self.config)
-
     @staticmethod
     def create(rotary_dim: int, layout: int = TOM_ROTARY_HALF, base: float = 10000.0, scaling: int = TOM_ROTARY_PLAIN,
                factor: float = 1.0, original_length: int = 1, device="cuda") -> "Rotary":
@@ -316,8 +313,8 @@ def tom_oqm_rotate(rotary: Rotary, positions, q=None, q_out=None, k=None, k_out=
                    k_norm=None, norm_eps: float = 1e-6, stream=None) -> None:
     """Queries, keys and values [tokens][heads][channels] of any strides: q and k normed where weights are given and
     turned to `positions` (int64), v copied, each into its output (which may be the input itself)."""
-    _native.rotate(rotary._address, rotary.turns, rotary.amplitude, positions, q, q_out, k, k_out, v, v_out, q_norm, k_norm,
-                   norm_eps, stream)
+    _native.rotate(C.addressof(rotary.config), rotary.turns, rotary.amplitude, positions, q, q_out, k, k_out, v, v_out, q_norm,
+                   k_norm, norm_eps, stream)
 
 
 def tom_oqm_attend_workspace_bytes(h: int, t_q: int, rows: int) -> int:
