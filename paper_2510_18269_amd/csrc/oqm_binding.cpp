@@ -345,13 +345,13 @@ PyObject* retrieve_noalloc(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // Codes of the dtypes that are not tom_dtype_t; oqm.py registers the same.
-constexpr int32_t kInt32 = 100, kInt64 = 101;
+constexpr int32_t kInt32 = 100, kInt64 = 101, kFloat64 = 102;
 
 // The dtype code of a tensor, out of the dictionary that oqm.py registered.
 bool to_dtype(PyObject* o, int32_t& out) {
     if (const at::Tensor* t = tensor_of(o)) {
         const at::ScalarType s = t->scalar_type();
-        out = s == at::kFloat ? TOM_F32 : s == at::kBFloat16 ? TOM_BF16 : s == at::kHalf ? TOM_F16 : s == at::kInt ? kInt32 : s == at::kLong ? kInt64 : -1;
+        out = s == at::kFloat ? TOM_F32 : s == at::kBFloat16 ? TOM_BF16 : s == at::kHalf ? TOM_F16 : s == at::kInt ? kInt32 : s == at::kLong ? kInt64 : s == at::kDouble ? kFloat64 : -1;
         if (out < 0) PyErr_SetString(PyExc_AssertionError, "tensor of another dtype expected");
         return out >= 0;
     }
@@ -378,7 +378,7 @@ bool to_view(PyObject* o, bool rows_first, tom_oqm_view_t& v, bool& given) {
         return false;
     }
     if (!to_ptr(o, v.data) || !to_dtype(o, v.dtype)) return false;
-    if (v.dtype == kInt32 || v.dtype == kInt64) {
+    if (v.dtype >= kInt32) {
         PyErr_SetString(PyExc_AssertionError, "float32, bfloat16 or float16 tensor expected");
         return false;
     }
@@ -438,7 +438,8 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void *rotary, *turns, *positions, *norms[2], *stream;
     tom_oqm_view_t view[6];
     bool given[6];
-    if (!arity(n, 14) || !to_void_p(a[0], rotary) || !to_ptr(a[1], turns)) return nullptr;
+    if (!arity(n, 14) || !to_void_p(a[0], rotary) || !to_array(a[1], rotary ? static_cast<const tom_oqm_rotary_t*>(rotary)->rotary_dim / 2 : 0, kFloat64, "turns", turns))
+        return nullptr;
     const double amplitude = PyFloat_AsDouble(a[2]), eps = PyFloat_AsDouble(a[12]);
     if (PyErr_Occurred()) return nullptr;
     int32_t rows = 0;

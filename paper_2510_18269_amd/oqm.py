@@ -181,7 +181,7 @@ def _no_device(*_) -> int:
 _native.setup(_raise, _integer(C.c_int32), _integer(C.c_int64), _void_p, torch.cuda.is_initialized,
               getattr(torch._C, "_cuda_getDevice", _no_device),
               getattr(torch._C, "_cuda_getCurrentRawStream", _no_device), _first_stream,
-              {**_DTYPE_OF_TORCH, torch.int32: 100, torch.int64: 101})
+              {**_DTYPE_OF_TORCH, torch.int32: 100, torch.int64: 101, torch.float64: 102})
 
 
 def tom_oqm_query_sizes(cfg: tom_oqm_config_t) -> tom_oqm_sizes_t:
