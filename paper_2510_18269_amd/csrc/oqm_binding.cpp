@@ -16,6 +16,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <exception>
 
 #include "tom_oqm.h"
 
@@ -72,7 +73,8 @@ bool to_handle(PyObject* o, tom_oqm_t*& out) {
 
 // A torch tensor as torch holds it: its place and shape then cost some nanoseconds, where the same questions asked through the
 // interpreter take 0.1 to 0.2 us each (an attention has up to six tensors of three dimensions).  Anything else that
-// answers the same questions, or a tensor of a class of its own, is asked them.
+// answers the same questions, or a tensor of a class of its own, is asked them.  Sparse and nested tensors have no such place
+// or shape, and are refused; what else may throw when it is asked (a tensor without storage) `guarded` below makes a Python exception of.
 const at::Tensor* tensor_of(PyObject* o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
 
 // None, a raw device pointer, or a tensor on the device.
@@ -83,12 +85,11 @@ bool to_ptr(PyObject* o, void*& out) {
             PyErr_SetString(PyExc_AssertionError, "device tensor expected");
             return false;
         }
-        try {
-            out = t->data_ptr();
-        } catch (const std::exception& e) {  // a tensor without storage
-            PyErr_SetString(PyExc_RuntimeError, e.what());
+        if (t->layout() != at::kStrided || t->is_nested()) {
+            PyErr_SetString(PyExc_AssertionError, "tensor with strides expected");
             return false;
         }
+        out = t->data_ptr();
         return true;
     }
     PyObject* c = PyObject_GetAttr(o, s_is_cuda);
@@ -532,7 +533,20 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-#define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
+// No C++ exception may pass through the interpreter.  Nothing that is owned is held where one can be thrown.
+template <PyObject* (*function)(PyObject*, PyObject* const*, Py_ssize_t)>
+PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    try {
+        return function(self, a, n);
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "an unknown C++ exception");
+    }
+    return nullptr;
+}
+
+#define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(setup), FAST(set_num_groups), FAST(quantize_append), FAST(score_groups), FAST(topk),
                          FAST(dequant_gather), FAST(assemble_active), FAST(retrieve), FAST(retrieve_noalloc),
                          FAST(rotate), FAST(attend), FAST(keep_groups), FAST(copy_groups),
