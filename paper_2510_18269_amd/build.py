@@ -17,6 +17,7 @@ OBJ = os.path.join(HERE, "_build")
 BINDING = os.path.join(HERE, "_oqm_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
 # the binding reads tensors as this PyTorch lays them out; its libraries are loaded before the binding is
 TORCH = os.path.dirname(importlib.util.find_spec("torch").origin)
+
 SELFCHECK = os.path.join(HERE, "selfcheck_division.bin")
 
 SOURCES = ["oqm_api.hip", "oqm_quantize.hip", "oqm_quantize_tokens.hip", "oqm_dequant.hip", "oqm_score.hip",
@@ -41,6 +42,14 @@ COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=
 EXTRA = {"oqm_score.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
+def torch_version() -> str:
+    """torch.__version__, out of the file that holds it: PyTorch itself takes seconds to import."""
+    spec = importlib.util.spec_from_file_location("torch_version", os.path.join(TORCH, "version.py"))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module.__version__
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
 
@@ -62,7 +71,7 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     # the Python side's argument marshalling: host code only, linked against the library beside it and PyTorch's
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-I", INCLUDE,
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", f'-DTOM_TORCH_VERSION="{torch_version()}"', "-I", INCLUDE,
            "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(TORCH, "include"),
            os.path.join(CSRC, "oqm_binding.cpp"), "-o", BINDING, "-L", HERE, "-ltom_oqm", "-Wl,-rpath,$ORIGIN",
            "-L", os.path.join(TORCH, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]

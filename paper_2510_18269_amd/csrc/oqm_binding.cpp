@@ -16,6 +16,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <cstring>
 #include <exception>
 
 #include "tom_oqm.h"
@@ -551,11 +552,27 @@ PyMethodDef methods[] = {FAST(setup), FAST(set_num_groups), FAST(quantize_append
                          FAST(dequant_gather), FAST(assemble_active), FAST(retrieve), FAST(retrieve_noalloc),
                          FAST(rotate), FAST(attend), FAST(keep_groups), FAST(copy_groups),
                          {nullptr, nullptr, 0, nullptr}};
+
+// Tensors are read as the PyTorch that this file was compiled against lays them out; another one may not.
+bool same_torch() {
+    PyObject* m = PyImport_ImportModule("torch.version");
+    if (!m) return false;
+    PyObject* v = PyObject_GetAttrString(m, "__version__");
+    Py_DECREF(m);
+    if (!v) return false;
+    const char* now = PyUnicode_AsUTF8(v);
+    const bool same = now && std::strcmp(now, TOM_TORCH_VERSION) == 0;
+    if (now && !same) PyErr_Format(PyExc_ImportError, "_oqm_binding was built against PyTorch %s and cannot be used with %s: build it again", TOM_TORCH_VERSION, now);
+    Py_DECREF(v);
+    return same;
+}
+
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_oqm_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
 PyMODINIT_FUNC PyInit__oqm_binding(void) {
+    if (!same_torch()) return nullptr;
     s_is_cuda = PyUnicode_InternFromString("is_cuda");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_numel = PyUnicode_InternFromString("numel");
