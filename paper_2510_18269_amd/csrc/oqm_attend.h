@@ -33,6 +33,10 @@ inline bool elements_apart(const tom_oqm_view_t& v) {
     return (v.head_stride >= v.channels && v.row_stride >= head_span) || (v.row_stride >= v.channels && v.head_stride >= row_span);
 }
 
+// How many recent rows a token of a causal call sees, the last t_q of which are the new tokens' own: none where this is not positive.
+// (In this order, since the sum of a token's number and nearly 2^31 rows would pass 32 bits.)
+constexpr int32_t recent_seen(int32_t token, int32_t recent_rows, int32_t t_q) { return token + 1 + (recent_rows - t_q); }
+
 struct AttendRows {  // rows as the model has them: in front, or recent
     const char* k;
     const char* v;

@@ -325,7 +325,7 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? (TOKEN_AXIS ? 2 : 3) : DP == 128
 
     const Segments s = segments_of(g, min((int32_t)item.block * 16 + 15, rows - 1), cut, kTile, Form::tiles(g));
     const int32_t recent = s.recent_rows, stored_end = s.front_tiles + s.stored_tiles;
-    const int32_t seen = !there ? 0 : g.causal ? min(recent, token + 1 + g.recent.rows - g.t_q) : recent;
+    const int32_t seen = !there ? 0 : g.causal ? min(recent, recent_seen(token, g.recent.rows, g.t_q)) : recent;
     for (int32_t t = s.begin; t < min(s.end, s.front_tiles); ++t) f.rows(g, g.front, head, t * kTile, g.front.rows, g.front.rows);
     for (int32_t t = max(s.begin, s.front_tiles); t < min(s.end, stored_end); ++t) f.stored(g, head, t - s.front_tiles);
     for (int32_t t = max(s.begin, stored_end); t < s.end; ++t) f.rows(g, g.recent, head, (t - stored_end) * kTile, recent, seen);

@@ -193,7 +193,7 @@ struct Segments {
 __device__ __forceinline__ Segments segments_of(const AttendArgs& g, int32_t last_row, uint32_t cut, int tile_tokens, int32_t stored_tiles) {
     Segments s;
     s.recent_rows = g.recent.rows;  // as far as any row of the block sees
-    if (g.causal) s.recent_rows = max(0, min(s.recent_rows, (int32_t)div_by((uint32_t)last_row, (uint32_t)g.repeat, g.inv_repeat) + 1 + g.recent.rows - g.t_q));
+    if (g.causal) s.recent_rows = max(0, min(s.recent_rows, recent_seen((int32_t)div_by((uint32_t)last_row, (uint32_t)g.repeat, g.inv_repeat), g.recent.rows, g.t_q)));
     s.front_tiles = (g.front.rows + tile_tokens - 1) / tile_tokens;
     s.stored_tiles = stored_tiles;
     const uint32_t tiles = (uint32_t)(s.front_tiles + s.stored_tiles + (s.recent_rows + tile_tokens - 1) / tile_tokens);

@@ -626,13 +626,13 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
             const int32_t from = from_in(first), to = segment == 0 ? min(end, s.front_tiles) : end;
             if (from >= to) continue;
             const bool causal = segment == 1 && g.causal;
-            const int32_t all = causal ? min(tokens, wave_last + 1 + g.recent.rows - g.t_q) : tokens;
+            const int32_t all = causal ? min(tokens, recent_seen(wave_last, g.recent.rows, g.t_q)) : tokens;
             Operand<T> q[MT][STEPS];
             int32_t seen[MT];
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 S::load_query(g.q + q_head[m] * g.q_head + token[m] * g.q_row, quarter, q[m]);
-                seen[m] = causal ? min(tokens, token[m] + 1 + g.recent.rows - g.t_q) : tokens;
+                seen[m] = causal ? min(tokens, recent_seen(token[m], g.recent.rows, g.t_q)) : tokens;
             }
             for (int32_t t = from; t < to; t += kStep)
 #pragma unroll 1

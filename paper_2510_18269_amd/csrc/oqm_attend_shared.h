@@ -348,9 +348,9 @@ __global__ __launch_bounds__(F::THREADS, 2) void attend_shared_kernel(AttendArgs
         if (works) {
             int32_t seen[MT];
             const bool causal = recent && g.causal;
-            const int32_t all = stored ? 32 : (causal ? min(tokens, wave_last + 1 + g.recent.rows - g.t_q) : tokens) - t0;
+            const int32_t all = stored ? 32 : (causal ? min(tokens, recent_seen(wave_last, g.recent.rows, g.t_q)) : tokens) - t0;
 #pragma unroll
-            for (int m = 0; m < MT; ++m) seen[m] = causal ? min(tokens, token[m] + 1 + g.recent.rows - g.t_q) - t0 : all;
+            for (int m = 0; m < MT; ++m) seen[m] = causal ? min(tokens, recent_seen(token[m], g.recent.rows, g.t_q)) - t0 : all;
             if (all > 0 && valid) f.tile(g, here, q, stored, valid, seen);
         }
         if (t + 1 < s.end) F::stage(g, next, there_next);
