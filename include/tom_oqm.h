@@ -418,7 +418,8 @@ size_t tom_oqm_attend_workspace_bytes(const tom_oqm_t* h, int32_t t_q, int64_t r
  *   lse        device float32 [H_q][t_q] or NULL: the natural logarithm of the sum of exp(w_j).  Where a token sees
  *              nothing its output is 0 and its lse -inf.
  *   workspace  device, 16-byte aligned, tom_oqm_attend_workspace_bytes(h, t_q, rows) bytes
- * Errors: INVALID_ARG, NOT_BOUND, UNSUPPORTED (head_dim above 256, more than 2^20 tokens, or 2^31 - 1 rows), HIP.
+ * Errors: INVALID_ARG, NOT_BOUND, UNSUPPORTED (head_dim above 256, more than 2^20 tokens, more than 2^31 - 4097 rows, or H_q * t_q of
+ * 2^30 (2^31 in some forms, rounded up for each KV head to blocks of up to 256) and more), HIP.
  * t_q == 0 is a no-op.
  */
 tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_view_t* q, const tom_oqm_view_t* out,

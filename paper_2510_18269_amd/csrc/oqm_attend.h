@@ -137,6 +137,11 @@ inline int32_t attend_cuts(const tom_oqm_config_t& c, int32_t t_q, int64_t rows)
     return n < 1 ? 1 : (int32_t)n;
 }
 
+// Lanes of the launch of `items` blocks of query rows, each of a part and a KV head.
+constexpr uint64_t attend_lanes(const AttendForm& f, uint64_t items) {
+    return f.shared ? items * 512 : f.folded ? items * kBlock : (items + kBlock / 64 - 1) / (kBlock / 64) * kBlock;
+}
+
 hipError_t launch_attend(const AttendArgs& a, const AttendForm& form, int dtype, hipStream_t s);
 void start_attend_shared_bf16(const AttendArgs& g, hipStream_t s);
 void start_attend_shared_f16(const AttendArgs& g, hipStream_t s);

@@ -78,7 +78,6 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
     if (!is_number(softcap) || softcap < 0.0f) return fail(TOM_ERR_INVALID_ARG, "softcap must be a number >= 0");
     if (c.head_dim > 256) return fail(TOM_ERR_UNSUPPORTED, "head_dim %d: the attention covers 256 and less", c.head_dim);
     if (t_q > kMaxNewTokens) return fail(TOM_ERR_UNSUPPORTED, "%d new tokens: at most %d per call", t_q, kMaxNewTokens);
-    if ((int64_t)c.n_q_heads * t_q > 0x7fffffff) return fail(TOM_ERR_UNSUPPORTED, "n_q_heads * t_q exceeds 2^31 - 1");
     AttendArgs a{};
     if (t_q == 0) return TOM_OK;
     if (tom_status_t st = check_view(q, "q", c.n_q_heads, t_q, c, a.q_head, a.q_row)) return st;
@@ -90,6 +89,10 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
     if (rows > kMaxRows) return fail(TOM_ERR_UNSUPPORTED, "%lld rows: at most %lld per call", (long long)rows, (long long)kMaxRows);
     const AttendForm form = attend_form(c, t_q);
     a.splits = attend_cuts(c, t_q, rows);
+    const int64_t blocks = ((int64_t)(c.n_q_heads / c.n_kv_heads) * t_q + form.rows - 1) / form.rows;
+    // (so that the query rows of a KV head, rounded up to whole blocks, stay inside 32 bits too)
+    if (attend_lanes(form, (uint64_t)blocks * (uint64_t)a.splits * (uint64_t)c.n_kv_heads) > kMaxLanes)
+        return fail(TOM_ERR_UNSUPPORTED, "%d heads of %d queries need more lanes than the 2^32 - 1 of a launch", c.n_q_heads, t_q);
     const size_t need = part_bytes(c, t_q, a.splits);
     if (need > 0) {
         if (!workspace || workspace_bytes < need)
@@ -138,7 +141,7 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
         a.scale_log2 = scale > 0.0f ? 1.0f : -1.0f;
     }
     a.cap_log2 = softcap * kLog2e;
-    a.row_blocks = (a.repeat * t_q + form.rows - 1) / form.rows;
+    a.row_blocks = (int32_t)blocks;
     a.inv_row_blocks = reciprocal_u32((uint32_t)a.row_blocks);
     a.inv_splits = reciprocal_u32((uint32_t)a.splits);
     (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's

@@ -27,6 +27,9 @@ tom_status_t fail(tom_status_t st, const char* fmt, ...);
 
 constexpr int kBlock = 256;  // threads per workgroup of the streaming kernels (4 waves)
 
+// Lanes of a grid dimension: the runtime refuses more.
+constexpr uint64_t kMaxLanes = 0xffffffffu;
+
 // Launches a kernel.  The triple-chevron form takes its launch shape through a stack of the runtime, two more calls into it,
 // which cost the host 0.2 to 0.3 us of 3.9 (four calls on a store of 0.7 MB, bound by the host, 15.4 -> 14.7 us).  Errors are left
 // for hipGetLastError, as there.
