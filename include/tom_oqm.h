@@ -383,7 +383,8 @@ tom_status_t tom_oqm_rotary_turns(const tom_oqm_rotary_t* rotary, double* turns,
  *                     An output may be its own input, with the same strides; otherwise outputs overlap nothing.
  *   q_norm, k_norm    device, [channels] of the same dtype, or NULL
  * Every multiple of the element size is a valid address and stride; multiples of 16 bytes are fastest.
- * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 1 rows times heads), HIP.  No rows: a no-op.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 1 rows times heads, or more lanes than a launch holds: 2^35 elements at odd addresses,
+ * 2^37 at multiples of 16 bytes, fewer where a head does not fill a power of two of lanes), HIP.  No rows: a no-op.
  */
 tom_status_t tom_oqm_rotate(const tom_oqm_rotary_t* rotary, const double* turns_device, float amplitude,
                             const int64_t* positions_device, const tom_oqm_view_t* q, const tom_oqm_view_t* q_out,

@@ -341,7 +341,10 @@ tom_status_t tom_oqm_rotate(const tom_oqm_rotary_t* r, const double* turns, floa
     g.inv_fast = reciprocal_u32(g.fast);
     g.sets = (uint64_t)g.parts * (uint64_t)one->rows;
     const uint32_t sets_per_block = threads / lanes;
-    const dim3 grid((uint32_t)((g.sets + sets_per_block - 1) / sets_per_block)), block(threads);
+    const uint64_t blocks = (g.sets + sets_per_block - 1) / sets_per_block;
+    if (blocks * threads > kMaxLanes)
+        return fail(TOM_ERR_UNSUPPORTED, "%d rows of %lld heads need more lanes than the 2^32 - 1 of a launch: turn fewer rows per call", one->rows, (long long)heads);
+    const dim3 grid((uint32_t)blocks), block(threads);
     // Rows that the last-level cache (256 MB) cannot hold until somebody reads them are read and written past the caches.  The
     // same 719 MB, us, through / past: 138 / 123.2 = 5.8 TB/s.
     const bool large = (uint64_t)one->rows * (uint64_t)heads * (uint64_t)one->channels * (uint64_t)e * 2 >= (uint64_t)256 << 20;

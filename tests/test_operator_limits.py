@@ -32,6 +32,15 @@ def test_attend_of_more_lanes_than_a_grid(oqm, dtype, kv_heads, q_heads, t_q, d,
         oqm.tom_oqm_destroy(h)
 
 
+# a lane takes two elements at odd addresses, 16 bytes and up to four heads elsewhere; a head of 2 channels has one lane
+@pytest.mark.parametrize("rows,heads,d,n,address", [(2 ** 20, 256, 128, 128, 0x10002), (2 ** 20, 512, 128, 128, 0x10002), (2 ** 27, 1, 2048, 2048, 0x10002),
+                                                    (2 ** 23, 128, 256, 256, 0x10000), (2 ** 20, 2047, 64, 64, 0x10004)])
+def test_rotate_of_more_lanes_than_a_grid(oqm, rows, heads, d, n, address):
+    rot = oqm.Rotary(oqm.tom_oqm_rotary_t(n, 0, 0, 4096, 1e4, 1.0), 0x10000, 1.0)
+    x = Fake((rows, heads, d), address=address)
+    unsupported(oqm, "lanes", lambda: oqm.tom_oqm_rotate(rot, 0x10000, q=x, q_out=x))
+
+
 def test_attend_of_more_rows_than_an_index(oqm):
     """2^31 - 4097 rows of keys: the limit that the header gives, one more is refused."""
     most = 2 ** 31 - 4097
