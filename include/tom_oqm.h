@@ -415,7 +415,8 @@ size_t tom_oqm_attend_workspace_bytes(const tom_oqm_t* h, int32_t t_q, int64_t r
  *              Keys that a token does not see may hold anything.  A value that is not finite, in a row that some
  *              of the tokens see, is unspecified for those too that see none of the row.  No row behind the last
  *              of a view is read.
- *   softcap    0: none
+ *   scale      a number below 2^50, and below 2^50 times the cap
+ *   softcap    0: none; above 2^40 none either, below 2^-30 every score is zero
  *   lse        device float32 [H_q][t_q] or NULL: the natural logarithm of the sum of exp(w_j).  Where a token sees
  *              nothing its output is 0 and its lse -inf.
  *   workspace  device, 16-byte aligned, tom_oqm_attend_workspace_bytes(h, t_q, rows) bytes

@@ -133,6 +133,12 @@ tom_status_t tom_oqm_attend(const tom_oqm_t* h, int32_t layer, const tom_oqm_vie
     a.token_axis = c.qaxis == TOM_QAXIS_TOKENS;
     a.bits = c.bits;
     a.meta_bf16 = c.meta_dtype == TOM_BF16;
+    // Under a cap below 2^-30 all scores are zero to float32's last place beside the one of exp(0); one above 2^40 changes none of up to 2^28.
+    if (softcap > 0.0f && softcap < 0x1p-30f) scale = softcap = 0.0f;
+    if (softcap > 0x1p40f) softcap = 0.0f;
+    // what the folded form multiplies scales by stays finite
+    if (std::fabs(softcap > 0.0f ? scale / softcap : scale) >= 0x1p50f)
+        return fail(TOM_ERR_INVALID_ARG, "scale, or scale / softcap, must be below 2^50");
     constexpr float kLog2e = 1.4426950408889634f;
     a.scale_log2 = softcap > 0.0f ? 2.0f * kLog2e * scale / softcap : scale * kLog2e;
     a.score_unit = 1.0f;

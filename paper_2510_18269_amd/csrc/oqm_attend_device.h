@@ -30,12 +30,12 @@ __device__ __forceinline__ float lane_xor(float v) {
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // softcap * tanh(y) in units of log 2, from z = 2 log2(e) y: tanh y = 1 - 2 / (1 + 2^z).  The difference loses what the one has over
-// tanh y: an error of 2^-22 * softcap at any y, which 16-bit results do not show.
+// tanh y: an error of 2^-22 * softcap at any y, which 16-bit results do not show up to a cap of 64 (2^-16).
 // high: what z = infinity gives, cap_log2 or that less what scores are counted from.
 __device__ __forceinline__ float capped(float z, float cap_log2, float high) {
     return __builtin_fmaf(-2.0f * cap_log2, __builtin_amdgcn_rcpf(1.0f + exp2_of(z)), high);
 }
-// Near zero by the series, for float32.
+// Near zero by the series, for float32 and for caps above 64: there the error is 2^-22 of the score, and 2^-19 of it from an eighth of the cap on.
 __device__ __forceinline__ float capped_exactly(float z, float cap_log2) {
     const float y = z * (0.5f * kLn2), x = y * y;
     const float small = y * fmaf(x, fmaf(x, fmaf(x, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);

@@ -118,9 +118,9 @@ struct Codes {
 };
 
 // Quant-groups of GS channels of a token.
-template <typename T, int DP, int GS, int BITS, int MT, int NW_>
-struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
-    typedef Sums<T, DP, GS, MT, DP / GS> S;
+template <typename T, int DP, int GS, int BITS, int MT, int NW_, bool SERIES>
+struct Folded : Sums<T, DP, GS, MT, DP / GS, SERIES>, Codes<DP, GS, BITS> {
+    typedef Sums<T, DP, GS, MT, DP / GS, SERIES> S;
     typedef Codes<DP, GS, BITS> C;
     using S::o, S::zero, S::PARTS, S::STEPS, S::VU;
     using C::ROW, C::STRIDE, C::SPG, C::CQ, C::CQ_BYTES, C::CQ_WORDS;
@@ -132,7 +132,10 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
     static constexpr int LOADS = (PIECES + NW * 64 - 1) / (NW * 64);
     static constexpr int META = TT * NG * 8;        // bytes of K's or V's pairs in LDS
     static constexpr int STAGE = 2 * TT * STRIDE + 2 * META;
-    static constexpr int WAVES = attend_waves(DP, GS, false, __is_same(T, In_f16), NW == 1);  // a SIMD
+    static constexpr int PLAIN_WAVES = attend_waves(DP, GS, false, __is_same(T, In_f16), NW == 1);
+    // a SIMD; the series want registers where there are few left: 256 channels in quant-groups of 32, 64 tokens over 128 groups, capped at 100,
+    // with two / one 520 / 342 us (by the plain form, 194)
+    static constexpr int WAVES = SERIES && GS <= DP / 4 && PLAIN_WAVES > 1 ? PLAIN_WAVES - 1 : PLAIN_WAVES;
 
     // ---- staging ----
     struct Fetch {
@@ -380,9 +383,9 @@ struct Folded : Sums<T, DP, GS, MT, DP / GS>, Codes<DP, GS, BITS> {
 // Scale and zero of a channel for all tokens of a group:
 //   <q, k_t>      = <q s, code_t> + <q, m>            sum_t p_t v_t = s sum_t p_t code_t + m sum_t p_t     over a group's tokens
 // so the queries take a group's scales (in three bfloat16 parts), and the sums of a tile, which lies in one group, its values'.
-template <typename T, int DP, int BITS, int NW_>
-struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1>, Codes<DP, (DP < 128 ? DP : 128), BITS> {
-    typedef Sums<T, DP, (DP < 128 ? DP : 128), 1, 1> S;
+template <typename T, int DP, int BITS, int NW_, bool SERIES>
+struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1, SERIES>, Codes<DP, (DP < 128 ? DP : 128), BITS> {
+    typedef Sums<T, DP, (DP < 128 ? DP : 128), 1, 1, SERIES> S;
     typedef Codes<DP, (DP < 128 ? DP : 128), BITS> C;
     using S::o, S::STEPS, S::VU, S::VN, S::GS;
     using C::ROW, C::STRIDE, C::SPG, C::CQ, C::CQ_BYTES, C::CQ_WORDS;
@@ -765,18 +768,23 @@ __global__ __launch_bounds__(kBlock, F::WAVES) void attend_folded_kernel(AttendA
     }
 }
 
+template <typename F16, typename F64>  // of 16 and of 64 rows a workgroup
+void start_folded_form(const AttendArgs& g, const AttendForm& form, hipStream_t s) {
+    const dim3 grid((uint32_t)((int64_t)g.row_blocks * g.splits * g.kv_heads)), block(kBlock);
+    if (form.rows == 16) launch(attend_folded_kernel<F16>, grid, block, 0, s, g);
+    else launch(attend_folded_kernel<F64>, grid, block, 0, s, g);
+}
+
 template <typename T, int DP, int GS, int BITS>
 void start_folded(const AttendArgs& g, const AttendForm& form, hipStream_t s) {
-    const dim3 grid((uint32_t)((int64_t)g.row_blocks * g.splits * g.kv_heads)), block(kBlock);
-    if (form.rows == 16) launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 1>>, grid, block, 0, s, g);
-    else launch(attend_folded_kernel<Folded<T, DP, GS, BITS, 1, 4>>, grid, block, 0, s, g);
+    if (g.cap_log2 > kPlainCap) start_folded_form<Folded<T, DP, GS, BITS, 1, 1, true>, Folded<T, DP, GS, BITS, 1, 4, true>>(g, form, s);
+    else start_folded_form<Folded<T, DP, GS, BITS, 1, 1, false>, Folded<T, DP, GS, BITS, 1, 4, false>>(g, form, s);
 }
 
 template <typename T, int DP, int BITS>
 void start_folded_tokens(const AttendArgs& g, const AttendForm& form, hipStream_t s) {
-    const dim3 grid((uint32_t)((int64_t)g.row_blocks * g.splits * g.kv_heads)), block(kBlock);
-    if (form.rows == 16) launch(attend_folded_kernel<FoldedTokens<T, DP, BITS, 1>>, grid, block, 0, s, g);
-    else launch(attend_folded_kernel<FoldedTokens<T, DP, BITS, 4>>, grid, block, 0, s, g);
+    if (g.cap_log2 > kPlainCap) start_folded_form<FoldedTokens<T, DP, BITS, 1, true>, FoldedTokens<T, DP, BITS, 4, true>>(g, form, s);
+    else start_folded_form<FoldedTokens<T, DP, BITS, 1, false>, FoldedTokens<T, DP, BITS, 4, false>>(g, form, s);
 }
 
 template <typename T, int BITS>

@@ -14,9 +14,9 @@
 
 namespace oqm {
 
-template <typename T, int DP_, bool BF16_META, int NW_, int MT_>
-struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> {
-    typedef Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1> S;
+template <typename T, int DP_, bool BF16_META, int NW_, int MT_, bool SERIES>
+struct Shared : Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1, SERIES> {
+    typedef Sums<T, DP_, (DP_ < 128 ? DP_ : 128), MT_, 1, SERIES> S;
     typedef typename MetaPair<BF16_META>::type Pair;
     using S::GS, S::VU, S::STEPS, S::o;
     static constexpr int DP = DP_, MT = MT_, NW = NW_, THREADS = NW * 64;
@@ -395,8 +395,9 @@ __global__ __launch_bounds__(F::THREADS, 2) void attend_shared_kernel(AttendArgs
 template <typename T, int DP, bool BF16_META>
 void start_shared_of(const AttendArgs& g, hipStream_t s) {
     const dim3 grid((uint32_t)((int64_t)g.row_blocks * g.splits * g.kv_heads));
-    if constexpr (DP == 256) launch(attend_shared_kernel<Shared<T, DP, BF16_META, 8, 1>>, grid, dim3(512), 0, s, g);
-    else launch(attend_shared_kernel<Shared<T, DP, BF16_META, 8, 2>>, grid, dim3(512), 0, s, g);
+    constexpr int kMT = DP == 256 ? 1 : 2;
+    if (g.cap_log2 > kPlainCap) launch(attend_shared_kernel<Shared<T, DP, BF16_META, 8, kMT, true>>, grid, dim3(512), 0, s, g);
+    else launch(attend_shared_kernel<Shared<T, DP, BF16_META, 8, kMT, false>>, grid, dim3(512), 0, s, g);
 }
 
 template <typename T>

@@ -1,0 +1,85 @@
+"""Attention under caps of any size, from ones that leave nothing of the scores to ones that change nothing.
+
+Tolerance: a score differs by `off` = scale * sum_c |q_c k_c| * 2^-15 as in tests/test_gpu_attend.py.  The cap, whose slope is at most one, adds
+up to 2^-20 of itself where it is 64 or less; above that 2^-18 of the largest score: a series of five products up to an eighth of the
+cap, and from there on 2^-22 of the cap, which is 2^-19 of such a score.  The output is then off by (2 off + 2^-14) * sum_j p_j |v_j| and half a
+step of its type, the logarithm of the sum by off + 2^-20 of its size."""
+import pytest
+import torch
+
+from tests import harness as H
+from tests.test_gpu_attend import Case, stored
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def oqm():
+    from paper_2510_18269_amd import oqm as m      # raises if the library is not built
+    assert torch.cuda.is_available()
+    return m
+
+
+SHAPES = [dict(dtype="bf16", t_q=1), dict(dtype="bf16", t_q=40), dict(dtype="f16", t_q=40, gs=32), dict(dtype="bf16", t_q=3, axis=1), dict(dtype="f16", t_q=40, axis=1, d=64),
+          dict(dtype="f16", t_q=4, d=80, gs=16), dict(dtype="f32", t_q=9), dict(dtype="bf16", t_q=100, gs=16), dict(dtype="f16", t_q=100, gs=8, d=256)]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("softcap", [1e-45, 1e-38, 1e-12, 1e-6, 0.01, 8.0, 64.0, 65.0, 1e3, 1e5, 1e9, 2e12, 1e20, 3e38])
+@pytest.mark.parametrize("large", [1.0, 30.0])
+def test_caps(oqm, softcap, large, shape):
+    c = Case(T=6, k=6, every=True, front=9, recent=110, layers=1, softcap=softcap, **shape)
+    t = H.DT[c.dtype]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(c.d + c.t_q)
+    codes, meta, x = stored(c, g)
+    Hq = c.heads * c.repeat
+    q = (torch.randn((Hq, c.t_q, c.d), generator=g, device="cuda") * large).to(t[1])
+    rows = [[torch.randn((c.heads, n, c.d), generator=g, device="cuda").to(t[1]) for _ in range(2)] for n in (c.front, c.recent)]
+    h = oqm.tom_oqm_create(oqm.make_config(1, c.heads, Hq, c.d, c.G, c.gs, c.T, qaxis=c.axis, in_dtype=t[0], out_dtype=t[0]))
+    try:
+        oqm.tom_oqm_bind(h, codes, meta, torch.empty(16, device="cuda"))
+        oqm.tom_oqm_set_num_groups(h, c.T)
+        out, lse = torch.empty_like(q), torch.empty((Hq, c.t_q), device="cuda")
+        ws = torch.empty(oqm.tom_oqm_attend_workspace_bytes(h, c.t_q, c.front + c.k * c.G + c.recent), dtype=torch.uint8, device="cuda")
+        oqm.tom_oqm_attend(h, 0, q, out, None, c.k, *rows[0], *rows[1], softcap=softcap, lse=lse, workspace=ws)
+        torch.cuda.synchronize()
+    finally:
+        oqm.tom_oqm_destroy(h)
+    cap = float(torch.tensor(softcap, dtype=torch.float32))     # as the call takes it
+    for i in range(Hq):
+        n = i // c.repeat
+        k, v = (torch.cat([rows[0][kv][n].double(), x[kv][:, n].reshape(-1, c.d), rows[1][kv][n].double()]) for kv in (0, 1))
+        dots = q[i].double() @ k.T * c.d ** -0.5
+        off = (q[i].double().abs() @ k.abs().T * c.d ** -0.5).amax(-1, keepdim=True) * 2.0 ** -15
+        dots = cap * torch.tanh(dots / cap)
+        off = off + (cap * 2.0 ** -20 if cap <= 64 else dots.abs().amax(-1, keepdim=True) * 2.0 ** -18)
+        off = off.clamp(max=2 * cap)     # no score is further from another than that
+        a, j = torch.arange(c.t_q, device="cuda")[:, None], torch.arange(c.recent, device="cuda")[None]
+        dots[:, k.shape[0] - c.recent:].masked_fill_(j > a + c.recent - c.t_q, float("-inf"))
+        want_lse = torch.logsumexp(dots, -1)
+        p = torch.exp(dots - want_lse[:, None])
+        want = p @ v
+        tol = (p @ v.abs()) * (2 * off + 2.0 ** -14) + torch.finfo(t[1]).eps / 2 * want.abs() + 1e-30
+        apart = (out[i].double() - want).abs()
+        assert bool((apart <= tol).all()), f"out is off by up to {float((apart / tol).max())} times its bound"
+        apart = (lse[i].double() - want_lse).abs()
+        assert bool((apart <= off[:, 0] + 2.0 ** -20 * (1 + want_lse.abs())).all())
+
+
+def test_scales_that_the_sums_cannot_hold(oqm):
+    """Refused: from 2^50 on, of the scale or of its quotient by the cap."""
+    h = oqm.tom_oqm_create(oqm.make_config(1, 1, 1, 64, 4, 32, 8))
+    try:
+        x = torch.zeros((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+        out = torch.empty_like(x)
+        for kw in (dict(scale=2.0 ** 50), dict(scale=-3e38), dict(scale=2.0 ** 31, softcap=2.0 ** -20), dict(scale=1e30, softcap=1e-3)):
+            with pytest.raises(oqm.TomError, match="2\\^50") as e:
+                oqm.tom_oqm_attend(h, 0, x, out, recent_k=x, recent_v=x, **kw)
+            assert e.value.status == oqm.TOM_ERR_INVALID_ARG
+        for kw in (dict(scale=2.0 ** 49), dict(scale=1.0, softcap=2.0 ** -29), dict(scale=2.0 ** 49, softcap=1e-44)):
+            oqm.tom_oqm_attend(h, 0, x, out, recent_k=x, recent_v=x, **kw)
+            torch.cuda.synchronize()
+            assert bool((out == 0).all())
+    finally:
+        oqm.tom_oqm_destroy(h)
