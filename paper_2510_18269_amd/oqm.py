@@ -289,7 +289,8 @@ def tom_oqm_static_scratch_bytes() -> int:
 
 def tom_oqm_rotary_turns(rotary: tom_oqm_rotary_t) -> tuple[list[float], float]:
     """What a position turns each pair of channels by, in whole turns, and the factor on the turned channels."""
-    turns, amplitude = (C.c_double * max(1, rotary.rotary_dim // 2))(), C.c_float()
+    # a rotary_dim beyond what the library takes is refused there, before anything is written
+    turns, amplitude = (C.c_double * min(max(1, rotary.rotary_dim // 2), 1024))(), C.c_float()
     _check(lib.tom_oqm_rotary_turns(C.byref(rotary), turns, C.byref(amplitude)))
     return list(turns), amplitude.value
 

@@ -34,3 +34,14 @@ def test_turns_that_are(oqm):
             oqm.tom_oqm_rotate(rotary(oqm, turns), Fake((3,), torch.int64), q=far, q_out=far)
     with pytest.raises(oqm.TomError, match="rotary_dim"):
         oqm.tom_oqm_rotate(rotary(oqm, Fake((32,), torch.float64), -6), None)
+
+
+def test_a_rotary_that_is_refused_takes_no_memory(oqm):
+    import tracemalloc
+    for n in (2 ** 24, 2050, -2 ** 24):
+        tracemalloc.start()
+        with pytest.raises(oqm.TomError, match="rotary_dim"):
+            oqm.tom_oqm_rotary_turns(oqm.tom_oqm_rotary_t(n, 0, 0, 4096, 1e4, 1.0))
+        assert tracemalloc.get_traced_memory()[1] < 2 ** 20
+        tracemalloc.stop()
+    assert len(oqm.tom_oqm_rotary_turns(oqm.tom_oqm_rotary_t(2048, 0, 0, 4096, 1e4, 1.0))[0]) == 1024
