@@ -377,7 +377,8 @@ tom_status_t tom_oqm_rotary_turns(const tom_oqm_rotary_t* rotary, double* turns,
  * Channels from rotary_dim up are not turned (they are normed).  Angles are reduced in float64, everything else is
  * float32, rounded once to the outputs' type.
  *   turns_device      what tom_oqm_rotary_turns gave, on the device; `rotary` and `amplitude` likewise
- *   positions_device  int64, one for each row; any value
+ *   positions_device  int64, one for each row; any value.  (An angle is off by about 2^-52 of itself, 10^-10 radians at position
+ *                     10^6 and 10^-7 at 10^9; positions beyond 2^53 are rounded to float64.)
  *   q, k, v           inputs [heads][tokens][channels], each with its output of the same shape; each pair may be NULL
  *                     (v needs no position).  All of one dtype, one number of rows and of channels (rotary_dim .. 2048).
  *                     An output may be its own input, with the same strides; otherwise outputs overlap nothing.
@@ -403,10 +404,11 @@ size_t tom_oqm_attend_workspace_bytes(const tom_oqm_t* h, int32_t t_q, int64_t r
  *   out = sum_j p_j v_j,   p = softmax_j(w_j),   w_j = scale <q, k_j>, or softcap * tanh(scale <q, k_j> / softcap)
  * over the front rows, the G rows code * s + m of each group, and the recent rows.  Query head i reads KV head
  * i / (H_q / H_k).  Codes enter the products as they are and (s, m) in float32 where quant-groups have 32 channels or
- * more (sums there stay finite for |s| below 2^54, with binary16 2^47, and queries, or queries times s, below 2^63);
+ * more (sums there stay finite for |s| and |s scale|, with a cap |s scale / softcap|, below 2^54, with binary16 2^47, and
+ * queries, or queries times s, below 2^63; outputs below 2^-57 lose their last places);
  * other forms split what they reconstruct into 16-bit parts.  Scores, softmax and sums are float32; probabilities enter the
  * products as two 16-bit parts, 2^-17 of each (binary16: 2^-23 of each, or 2^-39 of the largest).
- *   q, out     [H_q][t_q][d] of cfg.out_dtype, any strides that are multiples of 16 bytes
+ *   q, out     [H_q][t_q][d] of cfg.out_dtype, any strides that are multiples of 16 bytes; out overlaps nothing that is read
  *   idx        device int32 [k_eff]: the groups, in any order, each as often as it stands there; an index outside [0, T)
  *              is a hole that nobody sees.  NULL: the groups 0 .. k_eff - 1, k_eff <= T
  *   front_k .. recent_v  [H_k][rows][d] of cfg.out_dtype, both of a pair or neither (NULL or no rows)

@@ -76,13 +76,24 @@ struct AttendForm {
 // Folded: 16-bit rows of 64, 128 or 256 channels, and either quant-groups of 32 channels or more of one token, so that a step of the
 // matrix cores (32 channels of keys, 16 of values) lies in one of them, or quant-groups along the tokens, where a tile of 32 tokens
 // lies in one of them (mostly empty if they are short, and still the faster: 255 groups of 1 / 5 / 15 tokens, one new token, 135 / 44 /
-// 27 us in the general form, 13.4 / 12.9 / 13.1 folded).  Its workgroups have 16 rows, which their waves share, or 16 a wave.
-// (32 a wave spare a fifth of the instructions but leave two waves a SIMD instead of three: 1000 tokens over 32 groups 332 us where 16
-// took 283; 64 over 128 groups 116 and 113.)  Shared: other 16-bit forms of the head_dim axis where more than 256 query rows are to
-// share a tile's reconstruction.  28 query heads on 4 of 128 channels, 64 groups of 50 tokens in quant-groups of 16, us, general /
-// shared: 16 tokens (112 rows) 35.0 / 41.0, 24 (168) 42.3 / 47.9, 36 (252) 52.9 / 52.2, 48 (336) 60.8 / 54.8, 64 68.5 / 53.6, 200 192 /
-// 69.1; of 64 channels 36 30.7 / 35.2, 64 41.3 / 38.0; of 256 channels 36 88.9 / 89.5, 64 120 / 94.4; binary16 36 45.4 / 50.3, 64 55.2 /
-// 52.3.  The folded form of quant-groups of 64 and 64 tokens 29.3.
+// 27 us in the general form, 13.4 / 12.9 / 13.1 folded).  Its workgroups have 16 rows, which their waves share, or 16 a wave: 4 heads of
+// 128 channels, us of 16 / 64 rows a workgroup, over 64 groups of 196 and over 1024:
+//      rows of a head     8           16          17          32          48          64          100
+//      64 groups          11.0 / 15.2 11.9 / 15.7 14.6 / 16.4 16.1 / 17.6 17.4 / 19.1 19.2 / 20.8 23.4 / 24.9
+//      1024 groups        31.4 / 46.6 32.6 / 47.3 52.8 / 57.5 53.5 / 59.0 76.4 / 72.6 99.1 / 74.9 168 / 131
+// so that 17 to 32 rows lose a tenth by the rule, and more of them in short memories.  (32 rows a wave spare a fifth of the instructions but
+// leave two waves a SIMD instead of three: 1000 tokens over 32 groups 287 us and 306, 64 over 128 in quant-groups of 32 95 and 105.)
+// Shared: other 16-bit forms of the head_dim axis where more than 256 query rows of a head share a tile's reconstruction.  28 query heads on 4,
+// quant-groups of 16, us, general / shared:
+//      tokens (rows)                   12 (84)     24 (168)    36 (252)    48 (336)    64 (448)
+//      64 channels, 64 groups of 50    20.8 / 31.1 26.8 / 33.0 30.2 / 34.8 36.5 / 36.4 41.4 / 37.4
+//      128                             33.0 / 38.7 42.2 / 46.5 52.6 / 50.9 60.5 / 53.5 68.3 / 52.2
+//      256                             54.7 / 71.2 73.0 / 89.3 87.7 / 87.8 102 / 90.3  118 / 93.1
+//      64 channels, 128 groups of 196  56.8 / 48.1 92.5 / 53.8 125 / 58.1  163 / 94.1  212 / 95.0
+//      128                             101 / 62.5  172 / 73.7  235 / 79.0  307 / 131   402 / 132
+//      256                             173 / 134   289 / 248   399 / 247   519 / 363   676 / 470
+// The rule goes by rows alone, where short memories tie.  In long ones the shared form is the faster from 84 rows on, so that they lose up to
+// a factor of 3 below 257 rows (with 1 KV head 69 / 53 at 252 rows, with 8 451 / 133).
 inline AttendForm attend_form(const tom_oqm_config_t& c, int32_t t_q) {
     const bool tokens = c.qaxis == TOM_QAXIS_TOKENS, f32 = c.out_dtype == TOM_F32;
     const int64_t rows = (int64_t)(c.n_q_heads / c.n_kv_heads) * t_q;

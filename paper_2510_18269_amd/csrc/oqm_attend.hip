@@ -17,7 +17,7 @@ namespace oqm {
 // Along the tokens' axis a tile lies in one group, whose pairs a lane then reads once.  Where a tile's channels are padding or a
 // token is not there, what is read instead is some valid place, and not used.
 // Latency bounds it where rows are few (float32, 2 heads of 64 channels, 72 rows: 7 us), the vector unit, which takes every
-// element apart in every wave, where they are many: 64 bfloat16 tokens of 28 heads over 64 groups of 50 in quant-groups of 16 68 us.
+// element apart in every wave, where they are many: 36 bfloat16 tokens of 28 heads over 64 groups of 50 in quant-groups of 16 53 us.
 template <typename T, int DP, bool TOKEN_AXIS>
 struct General {
     static constexpr int VU = DP / 16 < 8 ? DP / 16 : 8, VN = DP / 16 / VU, STEPS = DP / 32;
@@ -468,7 +468,7 @@ template <typename T>
 void start_join(const AttendArgs& g, hipStream_t s) {
     const uint32_t rows = (uint32_t)(g.kv_heads * g.repeat * g.t_q), lanes = (uint32_t)(g.channels / 4);
     if (g.splits <= kFewParts || rows * lanes >= kLanesThatFill) {
-        // parts are cut from calls of 2048 waves of 16 rows or less: rows * lanes stays far inside 32 bits
+        // calls that are cut into parts have at most 2047 workgroups of 64 rows: rows * lanes stays below 2^23
         launch(attend_join_few_kernel<T>, dim3((rows * lanes + kBlock - 1) / kBlock), dim3(kBlock), 0, s, g, lanes, reciprocal_u32(lanes), rows);
     } else {
         launch(attend_join_many_kernel<T>, dim3(rows, (lanes + 7) / 8), dim3(kBlock), 0, s, g);

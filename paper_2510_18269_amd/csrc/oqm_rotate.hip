@@ -59,9 +59,9 @@ __device__ __forceinline__ void store_elements(char* p, const float (&x)[V]) {
     else *reinterpret_cast<Vec*>(p) = r;
 }
 
-// Cosine and sine of `turn` whole turns.  The nearest quarter turn is taken off in float64, so that what remains, at most an
-// eighth, is exact to a part in 2^24 of itself at any position; then the Taylor series of both (x = 2 pi r <= pi / 4: the terms
-// left out are below 2^-28).
+// Cosine and sine of `turn` whole turns.  The nearest quarter turn is taken off in float64, exactly, and what remains, at most an
+// eighth, rounded to float32; then the Taylor series of both (x = 2 pi r <= pi / 4: the terms left out are below 2^-28).  `turn` itself is a rounded
+// product of float64: off by 2^-52 of the turns or so, which passes float32's last place of the cosine from position 10^9 on.
 __device__ __forceinline__ void cos_sin_turns(double turn, float& c, float& s) {
     const double quarters = rint(turn * 4.0);
     const float r = (float)fma(quarters, -0.25, turn);
