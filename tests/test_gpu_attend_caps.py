@@ -20,13 +20,14 @@ def oqm():
     return m
 
 
-SHAPES = [dict(dtype="bf16", t_q=1), dict(dtype="bf16", t_q=40), dict(dtype="f16", t_q=40, gs=32), dict(dtype="bf16", t_q=3, axis=1), dict(dtype="f16", t_q=40, axis=1, d=64),
-          dict(dtype="f16", t_q=4, d=80, gs=16), dict(dtype="f32", t_q=9), dict(dtype="bf16", t_q=100, gs=16), dict(dtype="f16", t_q=100, gs=8, d=256)]
+# with what the queries are multiplied by: scores of a few units, or of a hundred
+SHAPES = [(dict(dtype="bf16", t_q=1), 30.0), (dict(dtype="bf16", t_q=40), 1.0), (dict(dtype="f16", t_q=40, gs=32), 30.0), (dict(dtype="bf16", t_q=3, axis=1), 30.0),
+          (dict(dtype="f16", t_q=40, axis=1, d=64), 1.0), (dict(dtype="f16", t_q=4, d=80, gs=16), 30.0), (dict(dtype="f32", t_q=9), 1.0), (dict(dtype="f32", t_q=30, d=64, gs=32), 30.0),
+          (dict(dtype="bf16", t_q=100, gs=16), 1.0), (dict(dtype="f16", t_q=100, gs=8, d=256), 30.0)]
 
 
-@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("shape,large", SHAPES)
 @pytest.mark.parametrize("softcap", [1e-45, 1e-38, 1e-12, 1e-6, 0.01, 8.0, 64.0, 65.0, 1e3, 1e5, 1e9, 2e12, 1e20, 3e38])
-@pytest.mark.parametrize("large", [1.0, 30.0])
 def test_caps(oqm, softcap, large, shape):
     c = Case(T=6, k=6, every=True, front=9, recent=110, layers=1, softcap=softcap, **shape)
     t = H.DT[c.dtype]

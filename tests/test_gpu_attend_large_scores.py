@@ -39,8 +39,7 @@ ROWS = [dict(d=128, gs=64, t_q=1, repeat=7), dict(d=64, gs=32, t_q=1, repeat=3),
 
 
 @pytest.mark.parametrize("shape", ROWS)
-@pytest.mark.parametrize("dtype,size", [(t, s) for t in ("f16", "bf16", "f32") for s in (1500.0, 6000.0, 8000.0, 12000.0, 16000.0, 3e5, 1e8)
-                                        if t != "f16" or 4 * s < 65504])
+@pytest.mark.parametrize("dtype,size", [("f16", 1500.0), ("f16", 8000.0), ("f16", 16000.0), ("bf16", 16000.0), ("bf16", 3e5), ("bf16", 1e8), ("f32", 1e8)])
 def test_scores_that_float32_rounds(oqm, dtype, size, shape):
     """Scores of 2^21 to 2^55.  The general, the folded and the shared form; 16 rows of queries and more."""
     n = 200

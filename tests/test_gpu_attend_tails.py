@@ -20,6 +20,9 @@ def oqm():
     return m
 
 
+LEVELS = [("f16", 12.0), ("f16", 17.5), ("f16", 20.0), ("bf16", 20.0), ("f32", 20.0)]
+
+
 def compare(c, got, q, x, rows):
     want, want_lse, tol, lse_tol = expected(c, q, x, None, rows, c.d ** -0.5)
     t = H.DT[c.dtype][1]
@@ -42,8 +45,7 @@ def sinks(c, above):
 
 
 @pytest.mark.parametrize("shape", ROWS)
-@pytest.mark.parametrize("above", [12.0, 17.5, 20.0])
-@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("dtype,above", LEVELS)
 def test_rows_below_sinks(oqm, dtype, above, shape):
     n = 2048
     c = Case(dtype=dtype, heads=2, G=50, T=1, k=0, every=True, front=n, recent=0, causal=False, layers=1, **shape)
@@ -68,8 +70,7 @@ STORED = [dict(d=128, gs=64, t_q=1, repeat=7), dict(d=128, gs=32, t_q=60, repeat
 
 
 @pytest.mark.parametrize("shape", STORED)
-@pytest.mark.parametrize("above", [12.0, 17.5, 20.0])
-@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("dtype,above", LEVELS)
 def test_groups_below_sinks(oqm, dtype, above, shape):
     """A sink's key has the codes 15 in the first quant-group's channels, where all others have 0, and its value the codes 0."""
     G, T = 64, 16
