@@ -11,11 +11,12 @@
 // show (p * s as one binary16, 2^-12, would spare a seventh of the time).
 //
 // What bounds it, 28 query heads on 4 of 128 channels in groups of 196 tokens, 4 bits.  One new token: memory, 3600 groups (451 MB) in
-// 80 us = 5.6 TB/s; few groups, latency: 64 in 7.4 us.  Many tokens: the vector unit, which for every tile takes codes apart and
+// 80 us = 5.6 TB/s; few groups, latency: 64 in 7.8 us.  Many tokens: mostly the vector unit, which for every tile takes codes apart and
 // multiplies scores and probabilities by scales in every wave: 1000 tokens over 32 groups in quant-groups of 64 with a cap (97 GFLOP) 286
-// us, 64 over 128 groups in quant-groups of 32 (23 GFLOP) 96 us, where the matrix cores alone want 58 and 14.  For 32 tokens of 16
-// rows in quant-groups of 64 a wave issues 24 matrix instructions (384 cycles), 235 of the vector unit (940) and, with a cap, 24
-// transcendental ones (384).  What p * s leaves by one v_dot2 each, instead of a shift and a difference: 301 us against 289.
+// us, of which it is busy for 213 and the matrix cores for 58, 64 over 128 groups in quant-groups of 32 (23 GFLOP) 96 us, 61 and 14.  For 32
+// tokens of 16 rows in quant-groups of 64 a wave issues 24 matrix instructions (384 cycles), 235 of the vector unit (940) and, with a cap, 24
+// transcendental ones (384).  About 96 of the 235 take codes apart, alike in the four waves of a workgroup, and 8 a quant-group add the keys' zeros.
+// What p * s leaves by one v_dot2 each, instead of a shift and a difference: 301 us against 289.
 #pragma once
 
 #include "oqm_attend_sums.h"
