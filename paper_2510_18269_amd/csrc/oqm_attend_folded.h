@@ -10,6 +10,14 @@
 // enter in two bfloat16 parts (exactly), p * s too (2^-17): code * s and m often cancel, so that the rounding of one part would
 // show (p * s as one binary16, 2^-12, would spare a seventh of the time).
 //
+// What this costs in exactness.  The matrix cores align products by the exponents of their operands, and a sub-normal's is that of the
+// highest place it could have, so that a product's last places are cut off: measured over 64 tokens, up to 2^-15 of the scale for codes in
+// the lowest bits of a byte, 2^-19 for those four bits higher.  With the 2^-17 of p * s that is what a value is off by where code * s and m
+// cancel; sums over many rows hardly show it (705600 rows: 1.0 % of bfloat16 outputs are rounded to the other side, in plain float32 0.2 %,
+// of binary16 7.5 % and 1.3 %; their distance from 64 bits is the same to two digits).  Zeros as quotients by the scales, which the matrix
+// cores add up over the same parts of p * s, took 4 to 11 % more time and did not show less.  Along the tokens, where the zeros go with p itself,
+// the same costs nothing, and is done: 0.8 % of binary16 outputs over 3600 groups of 50 instead of 2.6 %.
+//
 // What bounds it, 28 query heads on 4 of 128 channels in groups of 196 tokens, 4 bits.  One new token: memory, 3600 groups (451 MB) in
 // 80 us = 5.6 TB/s; few groups, latency: 64 in 7.8 us.  Many tokens: mostly the vector unit, which for every tile takes codes apart and
 // multiplies scores and probabilities by scales in every wave: 1000 tokens over 32 groups in quant-groups of 64 with a cap (97 GFLOP) 286
@@ -546,16 +554,14 @@ struct FoldedTokens : Sums<T, DP, (DP < 128 ? DP : 128), 1, 1, SERIES>, Codes<DP
                 if (!(mine >> (16 * (i / 4) + i % 4) & 1u)) w[0][i] = -__builtin_inff();
         }
         this->probabilities(w, base);
-        float total = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            total += w[0][i];
-            w[0][i] *= kUp;
-        }
-        total += lane_xor<16>(total);
-        total += lane_xor<32>(total);
-        Operand<In_bf16> hi, lo;
+        for (int i = 0; i < 8; ++i) w[0][i] *= kUp;
+        Operand<In_bf16> hi, lo, ones;
         split(w[0], hi, lo);
+        // the zeros go with the sum of the same two parts as the codes: what the parts leave of a probability does not show where
+        // the two cancel
+        ones.w = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        const float total = product(ones, lo, product(ones, hi, f32x4{0.f, 0.f, 0.f, 0.f}))[0] * (1.0f / kUp);
 #pragma unroll
         for (int n = 0; n < VN; ++n) {
             typename C::ValueWords v;
