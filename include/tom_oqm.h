@@ -408,7 +408,7 @@ size_t tom_oqm_attend_workspace_bytes(const tom_oqm_t* h, int32_t t_q, int64_t r
  * queries, or queries times s, below 2^63; outputs below 2^-57 lose their last places);
  * other forms split what they reconstruct into 16-bit parts.  Scores, softmax and sums are float32; probabilities enter the
  * products as two 16-bit parts, 2^-17 of each (binary16: 2^-23 of each, or 2^-39 of the largest), and codes as sub-normal
- * numbers: where code * s and m cancel, an output may be off by 2^-15 of s.
+ * numbers: where code * s and m cancel, an output may be off by 2^-13 of s.
  *   q, out     [H_q][t_q][d] of cfg.out_dtype, any strides that are multiples of 16 bytes; out overlaps nothing that is read
  *   idx        device int32 [k_eff]: the groups, in any order, each as often as it stands there; an index outside [0, T)
  *              is a hole that nobody sees.  NULL: the groups 0 .. k_eff - 1, k_eff <= T

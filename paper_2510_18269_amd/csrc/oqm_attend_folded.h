@@ -12,8 +12,8 @@
 //
 // What this costs in exactness.  The matrix cores align products by the exponents of their operands, and a sub-normal's is that of the
 // highest place it could have, so that a product's last places are cut off: measured over 64 tokens, up to 2^-15 of the scale for codes in
-// the lowest bits of a byte, 2^-19 for those four bits higher.  With the 2^-17 of p * s that is what a value is off by where code * s and m
-// cancel; sums over many rows hardly show it (705600 rows: 1.0 % of bfloat16 outputs are rounded to the other side, in plain float32 0.2 %,
+// the lowest bits of a byte, 2^-19 for those four bits higher.  With the 2^-17 of p * s (2^-13 of the scale for a code of 15) that is what a value is off by where
+// code * s and m cancel; sums over many rows hardly show it (705600 rows: 1.0 % of bfloat16 outputs are rounded to the other side, in plain float32 0.2 %,
 // of binary16 7.5 % and 1.3 %; their distance from 64 bits is the same to two digits).  Zeros as quotients by the scales, which the matrix
 // cores add up over the same parts of p * s, took 4 to 11 % more time and did not show less.  Along the tokens, where the zeros go with p itself,
 // the same costs nothing, and is done: 0.8 % of binary16 outputs over 3600 groups of 50 instead of 2.6 %.
