@@ -453,6 +453,111 @@ tom_status_t tom_oqm_keep_groups(tom_oqm_t* h, const int32_t* idx_device, int32_
 tom_status_t tom_oqm_copy_groups(tom_oqm_t* to, const tom_oqm_t* from, const int32_t* idx_device, int32_t n,
                                  void* hip_stream);
 
+/* ---- answers of several sequences, drafted: rows in pages ------------------- */
+
+/* Rows of several sequences in pages of one pool, and what a call adds to them.  Element c of row i of page p, head h, layer l:
+ * at l * layer_stride + p * page_stride + h * head_stride + i * row_stride + c, the same in K and in V, channels contiguous.  Row r
+ * of sequence s is row r % page_rows of page table[s][r / page_rows].  An entry outside [0, n_pages), like a row at or behind
+ * table_pages * page_rows, is not there: nothing is read or written for it, and nobody sees it.
+ * What is on the device is read when the work runs, so a captured graph can be replayed with other rows, starts and tables.
+ * Numbers there are never trusted with an address: rows count as 0 where they are negative, starts are cut to the call's tokens,
+ * and what sequences with overlapping starts get is unspecified. */
+typedef struct {
+    void *k, *v;         /* device                                                                      */
+    int64_t layer_stride, page_stride, head_stride, row_stride; /* elements, >= 0, multiples of 16 bytes  */
+    int32_t n_layers, n_pages, heads, page_rows, channels;      /* channels: 8 .. 256, a multiple of 8    */
+    int32_t dtype;       /* tom_dtype_t                                                                  */
+    const int32_t* table; /* device [sequences][table_pages]; a page may stand in several tables         */
+    const int32_t* rows;  /* device [sequences]: rows that a sequence has before the call's tokens        */
+    const int32_t* starts; /* device [sequences + 1], ascending: the call's tokens starts[s] .. starts[s + 1] - 1 are
+                              sequence s's, in order, and go to (or stand in) its rows rows[s], rows[s] + 1, ...  Tokens in
+                              front of the first and behind the last are nobody's: their outputs are left as they are.
+                              NULL: one token each                                                       */
+    int32_t sequences, table_pages;
+} tom_oqm_pages_t;
+
+/*
+ * The tree of drafted tokens: from each token's parent the mask of the tokens that it sees (itself, its parent, and so on
+ * up) and its position, once for all layers of a step.
+ *   parents    device int32 [tokens]: the parent's number within the sequence's tokens of this call.  A parent must come before
+ *              its children; -1, and any number outside [0, own number), makes the token a root.
+ *   starts     device int32 [sequences + 1], or NULL: one token each.  As in tom_oqm_pages_t.
+ *   mask       device int64 [tokens][words], 1 <= words <= 64: bit j of word w is 1 where the token sees token 64 w + j of its
+ *              sequence.  There are no bits for tokens from number 64 * words on.
+ *   first      device int64 [sequences] or NULL (zeros): the position of a root
+ *   positions  device int64 [tokens] or NULL: first + the number of tokens above
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 sequences or 2^24 tokens), HIP.  No tokens: a no-op.
+ */
+tom_status_t tom_oqm_draft_tree(const int32_t* parents_device, const int32_t* starts_device, int32_t sequences, int32_t tokens,
+                                int64_t* mask_device, int32_t words, const int64_t* first_device, int64_t* positions_device,
+                                void* hip_stream);
+
+/*
+ * tom_oqm_rotate whose keys and values go to the pages: new token j of sequence s to row rows[s] + j of `layer`.
+ *   q, q_out   [H_q][tokens][channels], both or neither
+ *   k, v       [heads][tokens][channels] of the pages' dtype, heads and channels
+ * Inputs and q_out may have any strides and addresses that are multiples of the element size (16 bytes are fastest); q_out may
+ * be q itself, with the same strides, and otherwise outputs overlap nothing that is read.  Sequences that are appended to share no
+ * page that is written.  Other arguments, arithmetic and errors as there; UNSUPPORTED also where a layer's pages span 2^36 bytes
+ * and more, and beyond 2^20 sequences.
+ */
+tom_status_t tom_oqm_append_rows(const tom_oqm_pages_t* pages, int32_t layer, const tom_oqm_rotary_t* rotary,
+                                 const double* turns_device, float amplitude, const int64_t* positions_device,
+                                 const tom_oqm_view_t* q, const tom_oqm_view_t* q_out, const tom_oqm_view_t* k,
+                                 const tom_oqm_view_t* v, const void* q_norm_device, const void* k_norm_device, float norm_eps,
+                                 void* hip_stream);
+
+/* Bytes of device workspace tom_oqm_attend_pages needs for `tokens` new tokens of n_q_heads query heads on these pages.  It goes by
+ * their sizes, not by what stands in rows or starts, and grows with the tokens and with the table.  0: none is needed, or arguments that call would refuse. */
+size_t tom_oqm_attend_pages_workspace_bytes(const tom_oqm_pages_t* pages, int32_t tokens, int32_t n_q_heads);
+
+/*
+ * Attention of new tokens over the rows of their sequences in pages (in which the call's own rows stand already), joined with a part that
+ * another call has given for the same tokens:
+ *   out = sum_j p_j v_j,   p = softmax_j(w_j),   w_j = scale <q, k_j>, or softcap * tanh(scale <q, k_j> / softcap)
+ * over the rows that a token sees: the rows[s] that were there, and of the call's tokens of its sequence
+ *   with a mask       those whose bit is 1 (a tree's ancestors, as tom_oqm_draft_tree makes them, or any other bits),
+ *   else if causal    those up to itself,
+ *   else              all.
+ * Query head i reads head i / (H_q / heads).  Scores, softmax and sums are float32.  Probabilities enter the products with 16-bit values as
+ * two 16-bit parts (2^-17 of each; binary16 2^-23 of each, or 2^-39 of the largest) where a sequence has few query rows, and as one (2^-8;
+ * binary16 2^-11 of each, or 2^-39 of the largest) where it has many.
+ *   q, out     [H_q][tokens][channels] of the pages' dtype, any strides that are multiples of 16 bytes; out overlaps nothing
+ *              that is read, but may be prior_out itself, with the same strides
+ *   mask       device int64 [tokens][words] or NULL, words >= 1; tokens from number 64 * words on are seen by nobody
+ *   scale      a number below 2^50, and below 2^50 times the cap
+ *   softcap    0: none; above 2^40 none either, below 2^-30 every score is zero
+ *   prior_out, prior_lse   [H_q][tokens][channels] and [H_q][tokens][1], both or neither: softmax-weighted values over other rows, as
+ *              tom_oqm_attend gives them over stored groups, and the natural logarithm of their sum of exponentials (-inf: nothing,
+ *              and prior_out is not looked at).  The result is then the attention over all of them:
+ *              (e^lse out + e^prior_lse prior_out) / (e^lse + e^prior_lse)
+ *   lse        [H_q][tokens][1] of float32 or NULL: the natural logarithm of the sum of exp(w_j), the prior's included.  Where a token
+ *              sees nothing its output is 0 and its lse -inf.  lse may be prior_lse itself.
+ *   workspace  device, 16-byte aligned, tom_oqm_attend_pages_workspace_bytes(...) bytes; calls that may overlap need separate ones
+ * A row that a token does not see has no part in what it gets, whatever the row holds; a token that sees a value that is not finite gets
+ * unspecified channels there.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 tokens or sequences, table_pages * page_rows above 2^31 - 4097, H_q * tokens of 2^30 and
+ * more, a layer's pages that span 2^36 bytes and more), HIP.  No tokens: a no-op.
+ */
+tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, const tom_oqm_view_t* q, const tom_oqm_view_t* out,
+                                  const int64_t* mask_device, int32_t words, int32_t causal, float scale, float softcap,
+                                  const tom_oqm_view_t* prior_out, const tom_oqm_view_t* prior_lse, const tom_oqm_view_t* lse,
+                                  void* workspace_device, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Keeps accepted tokens of a draft and drops the others: row rows[s] + idx[s][i] moves to row rows[s] + i, i < counts[s], K and V of all
+ * layers, in place.  The sequence then has rows_out[s] = rows[s] + counts[s] rows.
+ *   idx       device int32 [sequences][width], strictly ascending as far as counts[s]: numbers of the sequence's tokens in the call that
+ *             appended them.  An index outside [i, the sequence's tokens) leaves row i as it is (any order that is not ascending leaves
+ *             unspecified rows).
+ *   counts    device int32 [sequences], cut to [0, width]
+ *   rows_out  device int32 [sequences]; may be pages->rows itself (a second launch then writes it)
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 sequences, or more 16-byte columns, sequences * layers * heads * 2 * channels / 8, than the
+ * 2^32 - 1 lanes of a launch), HIP.  No sequences: a no-op.
+ */
+tom_status_t tom_oqm_keep_rows(const tom_oqm_pages_t* pages, const int32_t* idx_device, int32_t width, const int32_t* counts_device,
+                               int32_t* rows_out_device, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

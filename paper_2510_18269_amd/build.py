@@ -23,7 +23,9 @@ SELFCHECK = os.path.join(HERE, "selfcheck_division.bin")
 SOURCES = ["oqm_api.hip", "oqm_quantize.hip", "oqm_quantize_tokens.hip", "oqm_dequant.hip", "oqm_score.hip",
            "oqm_topk.hip", "oqm_rotate.hip", "oqm_attend_api.hip", "oqm_attend.hip", "oqm_groups.hip",
            "oqm_attend_bf16_4bit.hip", "oqm_attend_bf16_2bit.hip", "oqm_attend_f16_4bit.hip", "oqm_attend_f16_2bit.hip",
-           "oqm_attend_shared_bf16.hip", "oqm_attend_shared_f16.hip"]
+           "oqm_attend_shared_bf16.hip", "oqm_attend_shared_f16.hip",
+           "oqm_append_rows.hip", "oqm_draft.hip", "oqm_attend_pages_api.hip", "oqm_attend_pages_f32.hip", "oqm_attend_pages_bf16.hip",
+           "oqm_attend_pages_f16.hip"]
 # benchmark-only helpers (stream probes, timing events): a shared object of their own that only
 # bench.py loads; nothing of it is in the library or in its ABI header
 BENCH_LIB = os.path.join(HERE, "libtom_bench_probe.so")

@@ -1,0 +1,269 @@
+// What the kernels of the attention over pages share: which part of which block of query rows a workgroup has, what a token sees, and how
+// a row's result is written.
+#pragma once
+
+#include "oqm_attend_device.h"
+#include "oqm_attend_pages.h"
+
+namespace oqm {
+
+// Lies where a row of a sequence does not: what is not there is read as zero.
+static __device__ const u32x4 kZeroRow[64] = {};
+
+struct Block {  // a block of query rows of a sequence, and a part of its rows
+    int32_t sequence, first_token, tokens, rows;  // rows: without the call's
+    int32_t tile;                                 // which block of the sequence
+    int32_t begin, end;                           // rows of the part
+    uint32_t first_item, parts;
+};
+
+// Of x items, in LDS: the sequence whose item it is and that one's first, and the length of a part.
+struct FoundItem {
+    uint32_t x_in_sequence, base, parts;
+    int32_t sequence, chunk;
+    uint64_t totals[16];
+    uint32_t counts[16];
+};
+
+template <int QT>
+__device__ __forceinline__ uint32_t tiles_of(const PagesArgs& g, int32_t tokens) {
+    return ((uint32_t)tokens * (uint32_t)g.repeat + QT - 1) / QT;  // H_q * tokens is below 2^30
+}
+
+// The same in every lane of the workgroup; false: there is nothing for it.
+// All workgroups look at all sequences: a sum over them says how long a part is (so that a long sequence among short ones is cut and they are not), a second
+// one where each one's items begin.  48 sequences cost two passes of one load a lane; the host knows none of the lengths.
+template <int QT, int KT, int LEAST, int THREADS>
+__device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundItem& found, Block& b) {
+    const int32_t sequences = g.p.sequences;
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint32_t in_sequence, base;
+    int32_t s, chunk = 0x7fffffff;
+    auto part_length = [&](uint64_t total) {  // whole tiles, above total / extra
+        return (int32_t)min(max((total / g.extra + KT) / KT * KT, (uint64_t)LEAST), (uint64_t)0x7fffffff);
+    };
+    if (sequences == 1) {
+        s = 0;
+        in_sequence = x;
+        base = 0;
+        if (g.extra) {
+            const int32_t n = max(start_of(g.p, 1) - start_of(g.p, 0), 0);
+            const uint64_t total = (uint64_t)tiles_of<QT>(g, n) * (uint64_t)min((int64_t)rows_of(g.p, 0) + n, (int64_t)g.p.capacity);
+            chunk = part_length(total);
+        }
+    } else if (!g.p.starts && g.extra == 0) {
+        const uint32_t tiles = tiles_of<QT>(g, 1);
+        s = (int32_t)(x / tiles);
+        in_sequence = x - (uint32_t)s * tiles;
+        base = (uint32_t)s * tiles;
+    } else {
+        const int32_t per = (sequences + THREADS - 1) / THREADS, from = min(tid * per, sequences), to = min(from + per, sequences);
+        auto shape = [&](int32_t i, uint32_t& tiles, uint32_t& rows) {
+            const int32_t n = max(start_of(g.p, i + 1) - start_of(g.p, i), 0);
+            tiles = tiles_of<QT>(g, n);
+            rows = (uint32_t)min((int64_t)rows_of(g.p, i) + n, (int64_t)g.p.capacity);
+        };
+        if (g.extra) {
+            uint64_t total = 0;
+            for (int32_t i = from; i < to; ++i) {
+                uint32_t tiles, rows;
+                shape(i, tiles, rows);
+                total += (uint64_t)tiles * rows;
+            }
+            for (int m = 32; m > 0; m /= 2) total += __shfl_xor(total, m, 64);
+            if (lane == 0) found.totals[wave] = total;
+            __syncthreads();
+            total = 0;
+            for (int w = 0; w < THREADS / 64; ++w) total += found.totals[w];
+            chunk = part_length(total);
+        }
+        auto items = [&](int32_t i) {
+            uint32_t tiles, rows;
+            shape(i, tiles, rows);
+            return tiles * max((rows + (uint32_t)chunk - 1u) / (uint32_t)chunk, 1u);
+        };
+        uint32_t mine = 0;
+        for (int32_t i = from; i < to; ++i) mine += items(i);
+        uint32_t before = mine;
+        for (int m = 1; m < 64; m *= 2) {
+            const uint32_t other = __shfl_up(before, m, 64);
+            if (lane >= m) before += other;
+        }
+        if (lane == 63) found.counts[wave] = before;
+        if (tid == 0) found.sequence = -1;
+        before -= mine;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) before += found.counts[w];
+        if (x >= before && x < before + mine) {
+            int32_t i = from;
+            uint32_t at = before, n = items(i);
+            while (x >= at + n) {
+                at += n;
+                n = items(++i);
+            }
+            found.sequence = i;
+            found.base = at;
+        }
+        __syncthreads();
+        s = found.sequence;
+        if (s < 0) return false;
+        base = found.base;
+        in_sequence = x - base;
+    }
+    s = __builtin_amdgcn_readfirstlane(s);
+    b.sequence = s;
+    b.first_token = start_of(g.p, s);
+    b.tokens = max(start_of(g.p, s + 1) - b.first_token, 0);
+    b.rows = rows_of(g.p, s);
+    const int32_t all = (int32_t)min((int64_t)b.rows + b.tokens, (int64_t)g.p.capacity);
+    b.parts = g.extra ? max(((uint32_t)all + (uint32_t)chunk - 1u) / (uint32_t)chunk, 1u) : 1u;
+    b.tile = (int32_t)(in_sequence / b.parts);
+    const uint32_t part = in_sequence - (uint32_t)b.tile * b.parts;
+    if ((uint32_t)b.tile >= tiles_of<QT>(g, b.tokens)) return false;
+    b.first_item = base + (uint32_t)b.tile * b.parts;
+    b.begin = 0;
+    b.end = all;
+    if (b.parts > 1) {
+        b.begin = (int32_t)part * chunk;
+        b.end = (int32_t)min((uint32_t)all, (uint32_t)b.begin + (uint32_t)chunk);
+    }
+    if (g.causal && !g.mask) {
+        // the block's last token sees nothing behind itself
+        const int32_t last_row = min((b.tile + 1) * QT, b.tokens * g.repeat) - 1;
+        const int32_t last = (int32_t)div_by((uint32_t)last_row, (uint32_t)g.repeat, g.inv_repeat);
+        b.end = (int32_t)min((int64_t)b.end, (int64_t)b.rows + last + 1);
+    }
+    return true;
+}
+// Where a block's first item and its parts stand: unique, and below the units that the host counts.  (A sequence with tokens has as many in front of
+// it as it has predecessors with some, at most.)
+template <int QT>
+__device__ __forceinline__ uint32_t unit_of(const PagesArgs& g, int32_t s, int32_t first_token, int32_t tile) {
+    if (!g.p.starts) return (uint32_t)s * tiles_of<QT>(g, 1) + (uint32_t)tile;
+    return (uint32_t)first_token * (uint32_t)g.repeat / QT + (uint32_t)min(s, first_token) + (uint32_t)tile;
+}
+
+// Of the N rows (32 or 64) from t0 those that token `own` of a sequence sees, as bits; what lies behind the sequence's rows is left to the caller.
+template <int N>
+__device__ __forceinline__ uint64_t seen_from(const PagesArgs& g, int32_t t0, int32_t rows, int32_t own, const uint64_t* mask) {
+    const int32_t at = t0 - rows;  // of the call's tokens; |t0|, |rows| < 2^31
+    if (at <= -N) return ~uint64_t{0};
+    if (mask) {
+        if (at < 0) return mask[0] << -at | ((uint64_t{1} << -at) - 1);
+        const int32_t w = at >> 6, up = at & 63;
+        uint64_t bits = w < g.words ? mask[w] >> up : 0;
+        if (up && w + 1 < g.words) bits |= mask[w + 1] << (64 - up);
+        return bits;
+    }
+    if (!g.causal) return ~uint64_t{0};
+    const int32_t count = own + 1 - at;  // (at > -64, own < 2^20)
+    return count >= 64 ? ~uint64_t{0} : count <= 0 ? 0 : (uint64_t{1} << count) - 1;
+}
+
+// Values that are not finite (an exponent of all ones), by their bits: the build assumes that arithmetic meets no NaN.  Of a word, in one of its halves
+// or (float32) in all of it.
+template <typename T>
+__device__ __forceinline__ bool any_odd(uint32_t w) {
+    constexpr uint32_t m = __is_same(T, In_f32) ? 0x7f800000u : __is_same(T, In_bf16) ? 0x7f80u : 0x7c00u;
+    if constexpr (__is_same(T, In_f32)) return (w & m) == m;
+    else return (w & m) == m || (w & m << 16) == m << 16;
+}
+// Puts zeros in their places, and ones into `is`.
+template <typename T>
+__device__ __forceinline__ void take_odd(Operand<T>& x, Operand<T>& is) {
+    if constexpr (__is_same(T, In_f32)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t w = __float_as_uint(x.x[i]);
+            asm("" : "+v"(w));  // a number of its own: of a float's bits the compiler would ask for infinity alone
+            const bool odd = any_odd<T>(w);
+            is.x[i] = odd ? 1.0f : 0.0f;
+            x.x[i] = __uint_as_float(odd ? 0u : w);
+        }
+    } else {
+        constexpr uint32_t m = __is_same(T, In_bf16) ? 0x7f80u : 0x7c00u, one = __is_same(T, In_bf16) ? 0x3f80u : 0x3c00u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = x.w[i];
+            const bool low = (w & m) == m, high = (w & m << 16) == m << 16;
+            is.w[i] = (low ? one : 0u) | (high ? one << 16 : 0u);
+            x.w[i] = w & ((low ? 0u : 0xffffu) | (high ? 0u : 0xffff0000u));
+        }
+    }
+}
+
+// The result of four channels of a row out of its sums, the prior taken in: sums are counted from `from` (units of log 2).
+template <typename T>
+__device__ __forceinline__ void put_row(const PagesArgs& g, int32_t q_head, int32_t token, int c, float from, float total, f32x4 sum) {
+    typedef typename Element<T>::type E;
+    typedef E Vec __attribute__((ext_vector_type(4)));
+    if (g.prior_lse) {
+        const float before = g.prior_lse[q_head * g.prior_lse_head + token * g.prior_lse_row] * kLog2e;
+        if (before > -__builtin_inff()) {
+            const float top = fmaxf(from, before), mine = exp2_of(from - top), theirs = exp2_of(before - top);
+            const Vec x = *reinterpret_cast<const Vec*>(g.prior_out + q_head * g.prior_head + token * g.prior_row + (int64_t)c * sizeof(E));
+            from = top;
+            total = total > 0.0f ? total * mine + theirs : theirs;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = sum[i] * mine + theirs * (float)x[i];
+        }
+    }
+    const float by = total > 0.0f ? 1.0f / total : 0.0f;
+    Vec y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (E)(sum[i] * by);
+    *reinterpret_cast<Vec*>(g.out + q_head * g.out_head + token * g.out_row + (int64_t)c * sizeof(E)) = y;
+    if (c == 0 && g.lse) g.lse[q_head * g.lse_head + token * g.lse_row] = total > 0.0f ? (from + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff();
+}
+
+// Parts joined, four channels of a row a lane.  A row's lanes are of one wave: they have read the prior's sum when the first of them
+// writes the row's, so that both may be one array.
+template <typename T, int QT>
+__global__ __launch_bounds__(kBlock) void join_pages_kernel(PagesArgs g, uint32_t lanes, uint32_t lanes_log2, uint32_t rows, uint32_t inv_heads_all) {
+    const uint32_t i = blockIdx.x * kBlock + threadIdx.x, row = i >> lanes_log2;
+    const int c = 4 * (int)(i & (lanes - 1));
+    if (row >= rows || c >= g.channels) return;
+    const uint32_t heads = (uint32_t)(g.kv_heads * g.repeat), token = div_by(row, heads, inv_heads_all), q_head = row - token * heads;
+    const int32_t s = sequence_of(g.p, (int32_t)token);
+    if (s < 0) return;
+    const int32_t first_token = start_of(g.p, s);
+    const uint32_t head = div_by(q_head, (uint32_t)g.repeat, g.inv_repeat);
+    const uint32_t at = (token - (uint32_t)first_token) * (uint32_t)g.repeat + (q_head - head * (uint32_t)g.repeat);
+    const uint32_t* const unit = g.unit_first + 2 * (size_t)unit_of<QT>(g, s, first_token, (int32_t)(at / QT));
+    const uint32_t first = unit[0], parts = min(unit[1], first < g.items ? g.items - first : 0u);  // (starts that overlap leave units that nobody has written)
+    if (parts <= 1) return;
+    const size_t step = (size_t)g.kv_heads * QT;
+    const size_t slot = ((size_t)first * g.kv_heads + head) * QT + at % QT;
+    const f32pair* const stat = g.part_stat + slot;
+    const float* const part = g.part_out + slot * g.channels + c;
+    constexpr int kAhead = 4;
+    float from = -__builtin_inff(), total = 0.0f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (uint32_t p0 = 0; p0 < parts; p0 += kAhead) {
+        f32pair st[kAhead];
+        f32x4 x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const size_t n = min(p0 + u, parts - 1) * step;  // behind the last: read again, and not added
+            st[u] = stat[n];
+            x[u] = *reinterpret_cast<const f32x4*>(part + n * g.channels);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (p0 + u >= parts || st[u].x == -__builtin_inff()) continue;
+            const float top = fmaxf(from, st[u].x), mine = exp2_of(from - top), theirs = exp2_of(st[u].x - top);
+            from = top;
+            total = total * mine + st[u].y * theirs;
+            sum = sum * mine + x[u] * theirs;
+        }
+    }
+    put_row<T>(g, (int32_t)q_head, (int32_t)token, c, from, total, sum);
+}
+template <typename T, int QT>
+void start_join_pages(const PagesArgs& g, hipStream_t s) {
+    const uint32_t rows = (uint32_t)(g.kv_heads * g.repeat) * (uint32_t)g.p.tokens, lanes_log2 = g.channels <= 64 ? 4 : g.channels <= 128 ? 5 : 6;
+    launch(join_pages_kernel<T, QT>, dim3((uint32_t)((((uint64_t)rows << lanes_log2) + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, g, 1u << lanes_log2, lanes_log2,
+           rows, reciprocal_u32((uint32_t)(g.kv_heads * g.repeat)));
+}
+
+}  // namespace oqm

@@ -1,0 +1,248 @@
+// Attention over pages for few query rows a sequence (one token, a short draft), and for float32.
+//
+// Memory bounds it: K and V are read once, straight into the operands of the matrix cores, no LDS and no barrier on the way.  S^T = K Q^T leaves a lane, for
+// one query row, the scores of the very rows whose values it feeds to O^T = V^T P^T.  A workgroup has 16 query rows of a KV head; its four waves take the part's tiles of
+// 32 rows in turn, each with sums of its own, and join them in LDS.
+#pragma once
+
+#include "oqm_attend_pages_device.h"
+#include "oqm_attend_sums.h"
+
+namespace oqm {
+
+template <typename T_, int DP_, bool SERIES>
+struct PagedRows : Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> {
+    typedef T_ T;
+    typedef Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> S;
+    using S::GS, S::VU, S::VN, S::STEPS, S::o;
+    static constexpr int DP = DP_, E = elem_bytes<T>::value, KW = 8 * E / 16;  // KW: loads of 16 bytes of 8 channels
+    static constexpr int VW = VU * E / 4;                                      // words of a value piece
+    typedef uint32_t Piece __attribute__((ext_vector_type(VW)));
+
+    // Channel c of what begins at p, or zeros where the head has no such channel.
+    static __device__ __forceinline__ const char* channel(const PagesArgs& g, const char* p, int c) {
+        return c < g.channels ? p + c * E : reinterpret_cast<const char*>(kZeroRow);
+    }
+    static __device__ __forceinline__ void load8(const char* p, Operand<T>& x) {
+        if constexpr (E == 2) {
+            x.w = *reinterpret_cast<const u32x4*>(p);
+        } else {
+            const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.x[i] = a[i], x.x[4 + i] = b[i];
+        }
+    }
+    // A tile of 32 rows; place: of row (lane & 31); there: the rows that are; see: of these the lane's query row's.
+    __device__ __forceinline__ void tile(const PagesArgs& g, const char* k, const char* v, uint32_t place, const Operand<T> (&q)[1][STEPS], uint32_t there, uint32_t see) {
+        const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
+        auto row = [&](const char* base, int i) {
+            const uint32_t at = (uint32_t)__shfl((int)place, i, 64);
+            return at == kNoPlace ? reinterpret_cast<const char*>(kZeroRow) : base + (int64_t)at * 16;
+        };
+        Operand<T> kx[2][STEPS];
+        Piece vx[8][VN];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const char* const p = row(k, 16 * half + a);
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) load8(channel(g, p, quarter * (DP / 4) + 8 * u), kx[half][u]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const char* const p = row(v, 16 * (i / 4) + 4 * quarter + i % 4);
+#pragma unroll
+            for (int n = 0; n < VN; ++n) vx[i][n] = *reinterpret_cast<const Piece*>(channel(g, p, n * GS + a * VU));
+        }
+        float w[1][8], base[1], start[1];
+        S::bases(g, base, start);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) d = product(kx[half][u], q[0][u], d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[0][4 * half + i] = __builtin_fmaf(d[i], g.scale_log2, start[0]);
+        }
+        S::finish_scores(g, w, base);
+        const uint32_t mine = see >> (4 * quarter);
+        auto seen = [&](int i) { return (mine >> (16 * (i / 4) + i % 4) & 1u) != 0; };
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!seen(i)) w[0][i] = -__builtin_inff();
+        this->probabilities(w, base);
+        Operand<T> hi, lo;
+        split(w[0], hi, lo);
+        // Where a row is not for all, a probability of zero times what is not finite there would reach those who do not see it.
+        bool odd = false;
+        if (__any(see != there)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int n = 0; n < VN; ++n)
+#pragma unroll
+                    for (int u = 0; u < VW; ++u) odd = odd || any_odd<T>(vx[i][n][u]);
+        }
+        if (__any(odd)) {
+            Operand<T> ones;
+            float one[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) one[i] = seen(i) ? 1.0f : 0.0f;
+            Operand<T> none;
+            split(one, ones, none);
+            values<true>(vx, hi, lo, ones);
+        } else {
+            values<false>(vx, hi, lo, hi);
+        }
+    }
+    template <bool ODD>
+    __device__ __forceinline__ void add(Operand<T> x, const Operand<T>& hi, const Operand<T>& lo, const Operand<T>& ones, f32x4& sum) {
+        if constexpr (ODD) {
+            Operand<T> is;
+            take_odd(x, is);
+            const f32x4 count = product(is, ones, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (count[i] > 0.0f) sum[i] = __builtin_inff();
+        }
+        sum = product(x, hi, sum);
+        if constexpr (E == 2) sum = product(x, lo, sum);
+    }
+    template <bool ODD>
+    __device__ __forceinline__ void values(const Piece (&vx)[8][VN], const Operand<T>& hi, const Operand<T>& lo, const Operand<T>& ones) {
+#pragma unroll
+        for (int n = 0; n < VN; ++n) {
+            if constexpr (E == 2) {
+#pragma unroll
+                for (int u = 0; u < VU; u += 2) {
+                    Operand<T> even, odd;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t x = vx[2 * i][n][u / 2], y = vx[2 * i + 1][n][u / 2];
+                        even.w[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                        odd.w[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                    }
+                    add<ODD>(even, hi, lo, ones, o[0][n * VU + u]);
+                    add<ODD>(odd, hi, lo, ones, o[0][n * VU + u + 1]);
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < VU; ++u) {
+                    Operand<T> x;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x.x[i] = __uint_as_float(vx[i][n][u]);
+                    add<ODD>(x, hi, lo, ones, o[0][n * VU + u]);
+                }
+            }
+        }
+    }
+};
+
+constexpr int kPagedRows = 16, kPagedTile = 32, kPagedLeast = 128;
+
+template <typename F>
+__global__ __launch_bounds__(kBlock) void attend_pages_few_kernel(PagesArgs g) {
+    typedef typename F::T T;
+    constexpr int DP = F::DP, STEPS = F::STEPS, VU = F::VU, VN = F::VN, GS = F::GS, NW = kBlock / 64;
+    __shared__ FoundItem found;
+    __shared__ __align__(16) float sums[NW][kPagedRows][DP + 4];
+    __shared__ f32pair stats[NW][kPagedRows];
+    const uint32_t x = div_by(blockIdx.x, (uint32_t)g.kv_heads, g.inv_kv_heads);
+    const int head = (int)(blockIdx.x - x * (uint32_t)g.kv_heads);
+    Block b;
+    if (!block_of<kPagedRows, kPagedTile, kPagedLeast, kBlock>(g, x, found, b)) return;
+    const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
+    if (b.parts > 1 && head == 0 && x == b.first_item && threadIdx.x == 0) {
+        uint32_t* const unit = g.unit_first + 2 * (size_t)unit_of<kPagedRows>(g, b.sequence, b.first_token, b.tile);
+        unit[0] = b.first_item;
+        unit[1] = b.parts;
+    }
+    if (b.parts == 1 && g.extra && head == 0 && threadIdx.x == 0)
+        g.unit_first[2 * (size_t)unit_of<kPagedRows>(g, b.sequence, b.first_token, b.tile) + 1] = 1;
+
+    const int32_t rows = b.tokens * g.repeat, row = b.tile * kPagedRows + a;
+    const int32_t mine = row < rows ? row : rows - 1;
+    const int32_t own = (int32_t)div_by((uint32_t)mine, (uint32_t)g.repeat, g.inv_repeat), token = b.first_token + own;
+    const int32_t q_head = head * g.repeat + (mine - own * g.repeat);
+    Operand<T> q[1][STEPS];
+    {
+        const char* const p = g.q + q_head * g.q_head + token * g.q_row;
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) F::load8(F::channel(g, p, quarter * (DP / 4) + 8 * u), q[0][u]);
+    }
+    const uint64_t* const mask = g.mask ? g.mask + (int64_t)token * g.words : nullptr;
+    const int32_t* const table = g.p.table + (int64_t)b.sequence * g.p.table_pages;
+    const char* const k = g.k + head * g.p.head_bytes;
+    const char* const v = g.v + head * g.p.head_bytes;
+    F f;
+    f.clear();
+    uint32_t next = kNoPlace;
+    int32_t t0 = b.begin + wave * kPagedTile;
+    if (t0 < b.end) next = place_of(g.p, table, (uint32_t)(t0 + (lane & 31)), (uint32_t)b.end);
+    for (; t0 < b.end; t0 += NW * kPagedTile) {
+        const uint32_t place = next;
+        if (t0 + NW * kPagedTile < b.end) next = place_of(g.p, table, (uint32_t)(t0 + NW * kPagedTile + (lane & 31)), (uint32_t)b.end);
+        const uint32_t there = (uint32_t)__ballot(place != kNoPlace);
+        if (!there) continue;
+        f.tile(g, k, v, place, q, there, there & (uint32_t)seen_from<kPagedTile>(g, t0, b.rows, own, mask));
+    }
+    float sum = f.sum[0];
+    sum += lane_xor<16>(sum);
+    sum += lane_xor<32>(sum);
+    if (quarter == 0) stats[wave][a] = f32pair{f.ref[0], sum};
+#pragma unroll
+    for (int n = 0; n < VN; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            typedef float Vec __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int u = 0; u < VU; u += 4) {
+                Vec y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = f.o[0][n * VU + u + j][i];
+                *reinterpret_cast<Vec*>(&sums[wave][a][n * GS + (4 * quarter + i) * VU + u]) = y;
+            }
+        }
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < kPagedRows * DP / 4; i += kBlock) {
+        const int r = i / (DP / 4), c = i % (DP / 4) * 4;
+        const int32_t row_at = b.tile * kPagedRows + r;
+        if (row_at >= rows || c >= g.channels) continue;
+        float from = -__builtin_inff(), total = 0.0f;
+        f32x4 all = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const f32pair st = stats[w][r];
+            if (st.x == -__builtin_inff()) continue;
+            const float top = fmaxf(from, st.x), old = exp2_of(from - top), new_ = exp2_of(st.x - top);
+            from = top;
+            total = total * old + st.y * new_;
+            all = all * old + *reinterpret_cast<const f32x4*>(&sums[w][r][c]) * new_;
+        }
+        if (b.parts > 1) {
+            const size_t slot = ((size_t)x * g.kv_heads + head) * kPagedRows + r;
+            *reinterpret_cast<f32x4*>(g.part_out + slot * g.channels + c) = all;
+            if (c == 0) g.part_stat[slot] = f32pair{from, total};
+        } else {
+            const int32_t t = (int32_t)div_by((uint32_t)row_at, (uint32_t)g.repeat, g.inv_repeat);
+            put_row<T>(g, head * g.repeat + (row_at - t * g.repeat), b.first_token + t, c, from, total, all);
+        }
+    }
+}
+
+template <typename T, int DP>
+void start_pages_few_of(const PagesArgs& g, hipStream_t s) {
+    const dim3 grid(g.items * (uint32_t)g.kv_heads), block(kBlock);
+    // (float32 takes the tanh by its series under any cap)
+    if (g.cap_log2 > (__is_same(T, In_f32) ? 0.0f : kPlainCap)) launch(attend_pages_few_kernel<PagedRows<T, DP, true>>, grid, block, 0, s, g);
+    else launch(attend_pages_few_kernel<PagedRows<T, DP, false>>, grid, block, 0, s, g);
+}
+template <typename T>
+void start_pages_few(const PagesArgs& g, hipStream_t s) {
+    if (g.channels <= 64) start_pages_few_of<T, 64>(g, s);
+    else if (g.channels <= 128) start_pages_few_of<T, 128>(g, s);
+    else start_pages_few_of<T, 256>(g, s);
+    if (g.extra) start_join_pages<T, kPagedRows>(g, s);
+}
+
+}  // namespace oqm

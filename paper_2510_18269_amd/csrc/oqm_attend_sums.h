@@ -77,14 +77,16 @@ struct Sums {
         }
     }
     // Scores are computed from `start` on, and without a cap done; with one they are counted from the maximum as it is put on.
-    __device__ __forceinline__ void bases(const AttendArgs& g, float (&base)[MT], float (&start)[MT]) const {
+    template <typename ARGS>
+    __device__ __forceinline__ void bases(const ARGS& g, float (&base)[MT], float (&start)[MT]) const {
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             base[m] = from(m);
             start[m] = g.cap_log2 != 0.0f ? 0.0f : -base[m];
         }
     }
-    static __device__ __forceinline__ void finish_scores(const AttendArgs& g, float (&w)[MT][8], const float (&base)[MT]) {
+    template <typename ARGS>
+    static __device__ __forceinline__ void finish_scores(const ARGS& g, float (&w)[MT][8], const float (&base)[MT]) {
         if constexpr (SERIES) {
 #pragma unroll
             for (int m = 0; m < MT; ++m)

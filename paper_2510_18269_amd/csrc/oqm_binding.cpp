@@ -522,6 +522,161 @@ PyObject* copy_groups(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return finish_none(st);
 }
 
+// A tensor [heads][rows] of float32 on the device, of any strides, as a view of one channel; `given` is false for None.
+bool to_row_view(PyObject* o, const char* what, tom_oqm_view_t& v, bool& given) {
+    given = o != Py_None;
+    v = tom_oqm_view_t{};
+    if (!given) return true;
+    if (PyLong_Check(o)) {
+        PyErr_SetString(PyExc_AssertionError, "device tensor expected");
+        return false;
+    }
+    if (!to_ptr(o, v.data) || !to_dtype(o, v.dtype)) return false;
+    int64_t n[2] = {}, s[2] = {};
+    bool ok = v.dtype == TOM_F32;
+    if (const at::Tensor* t = tensor_of(o)) {
+        ok = ok && t->dim() == 2;
+        for (int i = 0; i < 2 && ok; ++i) n[i] = t->sizes()[i], s[i] = t->strides()[i];
+    } else {
+        PyObject* shape = PyObject_GetAttr(o, s_shape);
+        if (!shape) return false;
+        PyObject* strides = strides_of(o);
+        ok = ok && strides && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 2 && PyTuple_GET_SIZE(strides) == 2;
+        for (int i = 0; i < 2 && ok; ++i) ok = to_i64(PyTuple_GET_ITEM(shape, i), n[i]) && to_i64(PyTuple_GET_ITEM(strides, i), s[i]);
+        Py_XDECREF(strides);
+        Py_DECREF(shape);
+    }
+    if (!ok || !fits_i32(n[0]) || !fits_i32(n[1])) {
+        if (!PyErr_Occurred()) PyErr_Format(PyExc_AssertionError, "%s: a float32 tensor of [heads][tokens] expected", what);
+        return false;
+    }
+    v.heads = (int32_t)n[0];
+    v.rows = (int32_t)n[1];
+    v.channels = 1;
+    v.head_stride = s[0];
+    v.row_stride = s[1];
+    return true;
+}
+
+// A mask: None, or a contiguous int64 tensor [tokens][words]; its words.
+bool to_mask(PyObject* o, int64_t tokens, void*& out, int32_t& words) {
+    words = 0;
+    if (o == Py_None) {
+        out = nullptr;
+        return true;
+    }
+    int64_t n[2] = {-1, -1};
+    if (PyLong_Check(o) || !to_array(o, 0, kInt64, "mask", out)) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_AssertionError, "device tensor expected");
+        return false;
+    }
+    if (const at::Tensor* t = tensor_of(o)) {
+        if (t->dim() == 2) n[0] = t->sizes()[0], n[1] = t->sizes()[1];
+    } else {
+        PyObject* shape = PyObject_GetAttr(o, s_shape);
+        if (!shape) return false;
+        const bool two = PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 2;
+        const bool ok = !two || (to_i64(PyTuple_GET_ITEM(shape, 0), n[0]) && to_i64(PyTuple_GET_ITEM(shape, 1), n[1]));
+        Py_DECREF(shape);
+        if (!ok) return false;
+    }
+    if (n[0] != tokens || !fits_i32(n[1])) {
+        PyErr_SetString(PyExc_AssertionError, "mask: a tensor of [tokens][words] expected");
+        return false;
+    }
+    words = (int32_t)n[1];
+    return true;
+}
+
+// parents, tokens, starts, sequences, mask, first, positions, stream
+PyObject* draft_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    int32_t tokens, sequences, words;
+    void *parents, *starts, *mask, *first, *positions, *stream;
+    if (!arity(n, 8) || !to_i32(a[1], tokens) || !to_array(a[0], tokens, kInt32, "parents", parents) || !to_i32(a[3], sequences) ||
+        !to_array(a[2], (int64_t)sequences + 1, kInt32, "starts", starts) || !to_mask(a[4], tokens, mask, words) || !to_array(a[5], sequences, kInt64, "first", first) ||
+        !to_array(a[6], tokens, kInt64, "positions", positions) || !to_stream(a[7], stream))
+        return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = tom_oqm_draft_tree(static_cast<const int32_t*>(parents), static_cast<const int32_t*>(starts), sequences, tokens, static_cast<int64_t*>(mask), words,
+                            static_cast<const int64_t*>(first), static_cast<int64_t*>(positions), stream);
+    Py_END_ALLOW_THREADS
+    return finish_none(st);
+}
+
+// pages (address of a tom_oqm_pages_t), layer, rotary (of a tom_oqm_rotary_t), turns, amplitude, positions, q, q_out, k, v, q_norm, k_norm, norm_eps, stream
+PyObject* append_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void *pages, *rotary, *turns, *positions, *norms[2], *stream;
+    int32_t layer;
+    tom_oqm_view_t view[4];
+    bool given[4];
+    if (!arity(n, 14) || !to_void_p(a[0], pages) || !to_i32(a[1], layer) || !to_void_p(a[2], rotary) ||
+        !to_array(a[3], rotary ? static_cast<const tom_oqm_rotary_t*>(rotary)->rotary_dim / 2 : 0, kFloat64, "turns", turns))
+        return nullptr;
+    const double amplitude = PyFloat_AsDouble(a[4]), eps = PyFloat_AsDouble(a[12]);
+    if (PyErr_Occurred()) return nullptr;
+    for (int i = 0; i < 4; ++i)
+        if (!to_view(a[6 + i], true, view[i], given[i])) return nullptr;
+    if (!to_array(a[5], view[2].rows, kInt64, "positions", positions)) return nullptr;
+    for (int i = 0; i < 2; ++i)
+        if (!to_array(a[10 + i], view[2 * i].channels, view[2 * i].dtype, "norm weights", norms[i])) return nullptr;
+    if (!to_stream(a[13], stream)) return nullptr;
+    const tom_oqm_view_t* p[4];
+    for (int i = 0; i < 4; ++i) p[i] = given[i] ? &view[i] : nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = tom_oqm_append_rows(static_cast<const tom_oqm_pages_t*>(pages), layer, static_cast<const tom_oqm_rotary_t*>(rotary), static_cast<const double*>(turns),
+                             (float)amplitude, static_cast<const int64_t*>(positions), p[0], p[1], p[2], p[3], norms[0], norms[1], (float)eps, stream);
+    Py_END_ALLOW_THREADS
+    return finish_none(st);
+}
+
+// pages, layer, q, out, mask, causal, scale (None: channels^-0.5), softcap, prior_out, prior_lse, lse, workspace, stream
+PyObject* attend_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void *pages, *mask, *ws, *stream;
+    int32_t layer, words;
+    size_t ws_bytes;
+    tom_oqm_view_t view[3], lines[2];  // q, out, prior_out; prior_lse, lse
+    bool given[3], lines_given[2];
+    static const int at[3] = {2, 3, 8};
+    if (!arity(n, 13) || !to_void_p(a[0], pages) || !to_i32(a[1], layer)) return nullptr;
+    for (int i = 0; i < 3; ++i)
+        if (!to_view(a[at[i]], false, view[i], given[i])) return nullptr;
+    for (int i = 0; i < 2; ++i)
+        if (!to_row_view(a[9 + i], i == 0 ? "prior_lse" : "lse", lines[i], lines_given[i])) return nullptr;
+    if (!to_mask(a[4], view[0].rows, mask, words)) return nullptr;
+    const int causal = PyObject_IsTrue(a[5]);
+    if (causal < 0) return nullptr;
+    double scale = 0.0;
+    if (a[6] != Py_None) scale = PyFloat_AsDouble(a[6]);
+    else if (given[0] && view[0].channels > 0) scale = 1.0 / std::sqrt((double)view[0].channels);
+    const double softcap = PyFloat_AsDouble(a[7]);
+    if (PyErr_Occurred() || !to_workspace(a[11], ws, ws_bytes) || !to_stream(a[12], stream)) return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = tom_oqm_attend_pages(static_cast<const tom_oqm_pages_t*>(pages), layer, given[0] ? &view[0] : nullptr, given[1] ? &view[1] : nullptr,
+                              static_cast<const int64_t*>(mask), words, causal, (float)scale, (float)softcap, given[2] ? &view[2] : nullptr,
+                              lines_given[0] ? &lines[0] : nullptr, lines_given[1] ? &lines[1] : nullptr, ws, ws_bytes, stream);
+    Py_END_ALLOW_THREADS
+    return finish_none(st);
+}
+
+// pages, sequences, idx, width, counts, rows_out, stream
+PyObject* keep_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void *pages, *idx, *counts, *rows_out, *stream;
+    int32_t sequences, width;
+    if (!arity(n, 7) || !to_void_p(a[0], pages) || !to_i32(a[1], sequences) || !to_i32(a[3], width) ||
+        !to_array(a[2], (int64_t)sequences * width, kInt32, "idx", idx) || !to_array(a[4], sequences, kInt32, "counts", counts) ||
+        !to_array(a[5], sequences, kInt32, "rows_out", rows_out) || !to_stream(a[6], stream))
+        return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = tom_oqm_keep_rows(static_cast<const tom_oqm_pages_t*>(pages), static_cast<const int32_t*>(idx), width, static_cast<const int32_t*>(counts),
+                           static_cast<int32_t*>(rows_out), stream);
+    Py_END_ALLOW_THREADS
+    return finish_none(st);
+}
+
 // The Python callables that the functions above need, in the order of the globals, and the dictionary of dtypes.
 PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!arity(n, 9)) return nullptr;
@@ -551,6 +706,7 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {FAST(setup), FAST(set_num_groups), FAST(quantize_append), FAST(score_groups), FAST(topk),
                          FAST(dequant_gather), FAST(assemble_active), FAST(retrieve), FAST(retrieve_noalloc),
                          FAST(rotate), FAST(attend), FAST(keep_groups), FAST(copy_groups),
+                         FAST(draft_tree), FAST(append_rows), FAST(attend_pages), FAST(keep_rows),
                          {nullptr, nullptr, 0, nullptr}};
 
 // Tensors are read as the PyTorch that this file was compiled against lays them out; another one may not.

@@ -1,0 +1,182 @@
+// What a draft needs around the attention: the tree's masks and positions before it, the accepted rows' move after it.
+#include "oqm_pages.h"
+
+namespace oqm {
+
+struct TreeArgs {
+    const int32_t* parents;
+    PagePlaces seq;  // starts, sequences and tokens alone
+    int64_t* mask;
+    const int64_t* first;
+    int64_t* positions;
+    int32_t words;
+};
+
+// A lane takes a token and walks up to its root, numbers falling as it goes, so that the bits of a word are complete when the walk leaves it: no
+// array, and no other lane's result.  The walk is a chain of dependent reads, a step each: from LDS where the parents lie (the first kStaged of a sequence; a
+// parent's number is below its child's, so a workgroup needs none behind its own tokens).
+constexpr int kTreeBlock = 64, kStaged = 4096;
+__global__ __launch_bounds__(kTreeBlock) void draft_tree_kernel(TreeArgs g) {
+    __shared__ int32_t staged[kStaged];
+    const int32_t s = (int32_t)blockIdx.x;
+    const int32_t begin = start_of(g.seq, s), count = start_of(g.seq, s + 1) - begin;
+    for (int32_t first = (int32_t)blockIdx.y * kTreeBlock; first < count; first += (int32_t)gridDim.y * kTreeBlock) {
+        const int32_t* const parents = g.parents + begin;
+        const int32_t end = min(first + kTreeBlock, count);
+        __syncthreads();
+        for (int32_t i = (int32_t)threadIdx.x; i < min(end, kStaged); i += kTreeBlock) staged[i] = parents[i];
+        __syncthreads();
+        const int32_t own = first + (int32_t)threadIdx.x;
+        if (own >= count) continue;
+        const int64_t token = begin + own;
+        uint64_t* const mask = reinterpret_cast<uint64_t*>(g.mask) + token * g.words;
+        int32_t word = g.words - 1, at = own, above = 0;
+        uint64_t bits = 0;
+        while (true) {
+            for (; word > at / 64; --word) {
+                mask[word] = bits;
+                bits = 0;
+            }
+            if (at / 64 == word) bits |= uint64_t{1} << (at % 64);
+            const int32_t p = at < kStaged ? staged[at] : parents[at];
+            if (p < 0 || p >= at) break;
+            at = p;
+            ++above;
+        }
+        for (; word >= 0; --word) {
+            mask[word] = bits;
+            bits = 0;
+        }
+        if (g.positions) g.positions[token] = (g.first ? g.first[s] : 0) + above;
+    }
+}
+
+struct KeepArgs {
+    char *k, *v;
+    PagePlaces p;
+    int64_t layer_bytes;
+    const int32_t* idx;
+    const int32_t* counts;
+    int32_t* rows_out;  // NULL: a launch of its own writes them
+    int32_t width, heads;
+    uint32_t cols, inv_cols, planes;  // 16 bytes of a row; layers * heads * 2
+    uint32_t blocks_per_sequence, inv_blocks;
+    uint32_t inv_heads;
+};
+
+// A lane has 16 bytes of a row of one layer, head and of K or V, and walks the list from the front: kAhead pieces are read, then written.  The list
+// ascends, so idx[i] >= i, and what a batch writes lies in front of all that later batches read: in place without a second copy, and no lane touches
+// another's column.
+constexpr int kAhead = 8;
+__global__ __launch_bounds__(kBlock) void keep_rows_kernel(KeepArgs g) {
+    const uint32_t s = div_by(blockIdx.x, g.blocks_per_sequence, g.inv_blocks), block = blockIdx.x - s * g.blocks_per_sequence;
+    const uint32_t i = block * kBlock + threadIdx.x, plane = div_by(i, g.cols, g.inv_cols), col = i - plane * g.cols;
+    const int32_t rows = rows_of(g.p, (int32_t)s), count = min(max(g.counts[s], 0), g.width);
+    if (g.rows_out && i == 0) g.rows_out[s] = rows + count;
+    if (plane >= g.planes) return;
+    const int32_t own = start_of(g.p, (int32_t)s + 1) - start_of(g.p, (int32_t)s);
+    const uint32_t layer_head = plane >> 1, layer = div_by(layer_head, (uint32_t)g.heads, g.inv_heads), head = layer_head - layer * (uint32_t)g.heads;
+    char* const base = ((plane & 1) ? g.v : g.k) + layer * g.layer_bytes + head * g.p.head_bytes + (int64_t)col * 16;
+    const int32_t* const table = g.p.table + (int64_t)s * g.p.table_pages;
+    const int32_t* const idx = g.idx + (int64_t)s * g.width;
+    for (int32_t first = 0; first < count; first += kAhead) {
+        u32x4 piece[kAhead];
+        uint32_t to[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            to[u] = kNoPlace;
+            const int32_t at = first + u;
+            if (at >= count) continue;
+            const int32_t from = idx[at];
+            if (from <= at || from >= own || from >= g.p.capacity - rows) continue;  // (its own place, nothing to move, or not there)
+            const uint32_t source = place_of(g.p, table, (uint32_t)(rows + from), (uint32_t)g.p.capacity);
+            if (source == kNoPlace) continue;
+            to[u] = place_of(g.p, table, (uint32_t)(rows + at), (uint32_t)g.p.capacity);
+            piece[u] = *reinterpret_cast<const u32x4*>(base + (int64_t)source * 16);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (to[u] != kNoPlace) *reinterpret_cast<u32x4*>(base + (int64_t)to[u] * 16) = piece[u];
+    }
+}
+__global__ __launch_bounds__(kBlock) void kept_rows_kernel(KeepArgs g, int32_t* rows_out) {
+    const uint32_t s = blockIdx.x * kBlock + threadIdx.x;
+    if (s < (uint32_t)g.p.sequences) rows_out[s] = rows_of(g.p, (int32_t)s) + min(max(g.counts[s], 0), g.width);
+}
+
+}  // namespace oqm
+
+using namespace oqm;
+
+extern "C" {
+
+tom_status_t tom_oqm_draft_tree(const int32_t* parents, const int32_t* starts, int32_t sequences, int32_t tokens, int64_t* mask, int32_t words,
+                                const int64_t* first, int64_t* positions, void* hip_stream) {
+    if (sequences < 0 || tokens < 0) return fail(TOM_ERR_INVALID_ARG, "sequences or tokens is negative");
+    if (words < 1 || words > 64) return fail(TOM_ERR_INVALID_ARG, "words = %d must be in [1, 64]", words);
+    if (!starts && tokens != sequences) return fail(TOM_ERR_INVALID_ARG, "%d tokens of %d sequences: without starts each has one", tokens, sequences);
+    if (sequences > kMaxSequences || tokens > (1 << 24)) return fail(TOM_ERR_UNSUPPORTED, "%d sequences of %d tokens: at most 2^20 and 2^24 per call", sequences, tokens);
+    if (sequences == 0 || tokens == 0) return TOM_OK;
+    if (!parents || !mask) return fail(TOM_ERR_INVALID_ARG, "parents and mask must be non-NULL");
+    if ((reinterpret_cast<uintptr_t>(parents) | reinterpret_cast<uintptr_t>(starts)) & 3u) return fail(TOM_ERR_INVALID_ARG, "parents and starts must be 4-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(mask) | reinterpret_cast<uintptr_t>(first) | reinterpret_cast<uintptr_t>(positions)) & 7u)
+        return fail(TOM_ERR_INVALID_ARG, "mask, first and positions must be 8-byte aligned");
+    TreeArgs g{};
+    g.parents = parents;
+    g.seq.starts = starts;
+    g.seq.sequences = sequences;
+    g.seq.tokens = tokens;
+    g.mask = mask;
+    g.first = first;
+    g.positions = positions;
+    g.words = words;
+    // workgroups of a sequence: as many as the longest may need, few where there are many sequences (they then take several blocks of tokens)
+    const int32_t most = (tokens + kTreeBlock - 1) / kTreeBlock, want = 4096 / sequences + 1;
+    (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's
+    launch(draft_tree_kernel, dim3((uint32_t)sequences, (uint32_t)(most < want ? most : want)), dim3(kTreeBlock), 0, static_cast<hipStream_t>(hip_stream), g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(TOM_ERR_HIP, "draft_tree launch: %s", hipGetErrorString(e));
+    return TOM_OK;
+}
+
+tom_status_t tom_oqm_keep_rows(const tom_oqm_pages_t* pages, const int32_t* idx, int32_t width, const int32_t* counts, int32_t* rows_out, void* hip_stream) {
+    KeepArgs g{};
+    if (tom_status_t st = check_pages(pages, g.p)) return st;
+    if (width < 0) return fail(TOM_ERR_INVALID_ARG, "width < 0");
+    if (pages->sequences == 0) return TOM_OK;
+    if ((!idx && width > 0) || !counts || !rows_out) return fail(TOM_ERR_INVALID_ARG, "idx, counts and rows_out must be non-NULL");
+    if ((reinterpret_cast<uintptr_t>(idx) | reinterpret_cast<uintptr_t>(counts) | reinterpret_cast<uintptr_t>(rows_out)) & 3u)
+        return fail(TOM_ERR_INVALID_ARG, "idx, counts and rows_out must be 4-byte aligned");
+    const uint64_t cols = (uint64_t)pages->channels * bytes_of_dtype(pages->dtype) / 16;
+    const __int128 pieces = (__int128)pages->n_layers * pages->heads * 2 * cols;
+    if (pieces > 0x7fffffff) return fail(TOM_ERR_UNSUPPORTED, "layers and heads of more than 2^31 - 1 pieces of 16 bytes a row");
+    const uint64_t blocks = ((uint64_t)pieces + kBlock - 1) / kBlock;
+    if (blocks * (uint64_t)pages->sequences * kBlock > kMaxLanes)
+        return fail(TOM_ERR_UNSUPPORTED, "%d sequences need more lanes than the 2^32 - 1 of a launch: keep fewer per call", pages->sequences);
+    g.k = static_cast<char*>(pages->k);
+    g.v = static_cast<char*>(pages->v);
+    g.layer_bytes = pages->n_layers > 1 ? layer_bytes(*pages, 1) : 0;
+    g.idx = idx;
+    g.counts = counts;
+    const bool in_place = rows_out == pages->rows;
+    g.rows_out = in_place ? nullptr : rows_out;
+    g.width = width;
+    g.heads = pages->heads;
+    g.inv_heads = reciprocal_u32((uint32_t)pages->heads);
+    g.cols = (uint32_t)cols;
+    g.inv_cols = reciprocal_u32(g.cols);
+    g.planes = (uint32_t)((uint64_t)pieces / cols);
+    g.blocks_per_sequence = (uint32_t)blocks;
+    g.inv_blocks = reciprocal_u32(g.blocks_per_sequence);
+    // how many tokens each sequence has says how far its list may reach; without an end of the call to cut it to
+    g.p.tokens = 0x7fffffff;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's
+    launch(keep_rows_kernel, dim3((uint32_t)(blocks * (uint64_t)pages->sequences)), dim3(kBlock), 0, s, g);
+    if (in_place) launch(kept_rows_kernel, dim3((uint32_t)((pages->sequences + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, g, rows_out);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(TOM_ERR_HIP, "keep_rows launch: %s", hipGetErrorString(e));
+    return TOM_OK;
+}
+
+}  // extern "C"

@@ -36,7 +36,9 @@ EXPORTS = ["tom_oqm_query_sizes", "tom_oqm_create", "tom_oqm_bind", "tom_oqm_res
            "tom_oqm_score_groups", "tom_oqm_topk", "tom_oqm_dequant_gather",
            "tom_oqm_assemble_active", "tom_oqm_retrieve", "tom_oqm_retrieve_noalloc",
            "tom_oqm_static_scratch_bytes", "tom_oqm_rotary_turns", "tom_oqm_rotate",
-           "tom_oqm_attend_workspace_bytes", "tom_oqm_attend", "tom_oqm_keep_groups", "tom_oqm_copy_groups"]
+           "tom_oqm_attend_workspace_bytes", "tom_oqm_attend", "tom_oqm_keep_groups", "tom_oqm_copy_groups",
+           "tom_oqm_draft_tree", "tom_oqm_append_rows", "tom_oqm_attend_pages_workspace_bytes", "tom_oqm_attend_pages",
+           "tom_oqm_keep_rows"]
 
 
 class TomError(RuntimeError):
@@ -63,6 +65,13 @@ class tom_oqm_rotary_t(C.Structure):
 class tom_oqm_view_t(C.Structure):
     _fields_ = [("data", C.c_void_p), ("head_stride", C.c_int64), ("row_stride", C.c_int64)] + \
                [(n, C.c_int32) for n in ("heads", "rows", "channels", "dtype")]
+
+
+class tom_oqm_pages_t(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v")] + \
+               [(n, C.c_int64) for n in ("layer_stride", "page_stride", "head_stride", "row_stride")] + \
+               [(n, C.c_int32) for n in ("n_layers", "n_pages", "heads", "page_rows", "channels", "dtype")] + \
+               [(n, C.c_void_p) for n in ("table", "rows", "starts")] + [(n, C.c_int32) for n in ("sequences", "table_pages")]
 
 
 def _load():
@@ -107,10 +116,17 @@ def _load():
     L.tom_oqm_attend.argtypes = [vp, i32, viewp, viewp, vp, i32] + [viewp] * 4 + [i32, f32, f32, vp, vp, C.c_size_t, vp]
     L.tom_oqm_keep_groups.argtypes = [vp, vp, i32, vp]
     L.tom_oqm_copy_groups.argtypes = [vp, vp, vp, i32, vp]
+    pagesp = C.POINTER(tom_oqm_pages_t)
+    L.tom_oqm_draft_tree.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp, vp]
+    L.tom_oqm_append_rows.argtypes = [pagesp, i32, C.POINTER(tom_oqm_rotary_t), vp, f32, vp] + [viewp] * 4 + [vp, vp, f32, vp]
+    L.tom_oqm_attend_pages_workspace_bytes.argtypes = [pagesp, i32, i32]
+    L.tom_oqm_attend_pages_workspace_bytes.restype = C.c_size_t
+    L.tom_oqm_attend_pages.argtypes = [pagesp, i32, viewp, viewp, vp, i32, i32, f32, f32] + [viewp] * 3 + [vp, C.c_size_t, vp]
+    L.tom_oqm_keep_rows.argtypes = [pagesp, vp, i32, vp, vp, vp]
     for name in EXPORTS:
         fn = getattr(L, name)
         if name not in ("tom_oqm_destroy", "tom_last_error", "tom_oqm_score_workspace_bytes",
-                        "tom_oqm_static_scratch_bytes", "tom_oqm_attend_workspace_bytes"):
+                        "tom_oqm_static_scratch_bytes", "tom_oqm_attend_workspace_bytes", "tom_oqm_attend_pages_workspace_bytes"):
             fn.restype = i32
     return L
 
@@ -340,6 +356,67 @@ def tom_oqm_keep_groups(h: int, idx, n: int, stream=None) -> None:
 def tom_oqm_copy_groups(to: int, source: int, idx, n: int, stream=None) -> None:
     """Groups idx[0 .. n) of `source` are appended to `to`."""
     _native.copy_groups(to, source, idx, n, stream)
+
+
+@dataclass
+class Pages:
+    """Rows of several sequences in pages of one pool, and the tensors that back them.  What `table`, `rows` and `starts`
+    hold is read when the work runs and may be changed in place between calls."""
+    config: tom_oqm_pages_t
+    k: torch.Tensor        # [layers][pages][heads][page_rows][channels], of any strides that are multiples of 16 bytes
+    v: torch.Tensor        # the same, with the same strides
+    table: torch.Tensor    # int32 [sequences][table_pages]
+    rows: torch.Tensor     # int32 [sequences]: before the call's tokens
+    starts: torch.Tensor | None  # int32 [sequences + 1]; None: one token each
+
+    @staticmethod
+    def create(k, v, table, rows, starts=None) -> "Pages":
+        assert k.dim() == 5 and k.shape == v.shape and k.dtype == v.dtype, "k and v: [layers][pages][heads][page_rows][channels] of one dtype"
+        assert k.dtype in _DTYPE_OF_TORCH, "float32, bfloat16 or float16 pages expected"
+        assert k.stride(4) == 1 and v.stride(4) == 1, "contiguous channel axis expected"
+        assert all(n == 1 or a == b for n, a, b in zip(k.shape, k.stride(), v.stride())), "k and v must have the same strides"
+        assert table.dim() == 2, "table: [sequences][table_pages]"
+        sequences = table.shape[0]
+        for name, t, n in (("table", table, table.numel()), ("rows", rows, sequences), ("starts", starts, sequences + 1)):
+            if t is None and name == "starts":
+                continue
+            assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n, f"{name}: a contiguous int32 tensor of {n} elements expected"
+            assert t.device == k.device, f"{name} must be on the pages' device"
+        assert v.device == k.device, "k and v must be on one device"
+        config = tom_oqm_pages_t(_ptr(k), _ptr(v), *k.stride()[:4], *k.shape, _DTYPE_OF_TORCH[k.dtype], _ptr(table), _ptr(rows), _ptr(starts), *table.shape)
+        return Pages(config, k, v, table, rows, starts)
+
+
+def tom_oqm_draft_tree(parents, starts, mask, positions=None, first=None, stream=None) -> None:
+    """parents int32 [tokens], starts int32 [sequences + 1] or None (one token each) -> mask int64 [tokens][words], positions int64 [tokens]
+    counted from first, int64 [sequences] or None (zeros)."""
+    tokens = parents.numel()
+    _native.draft_tree(parents, tokens, starts, tokens if starts is None else starts.numel() - 1, mask, first, positions, stream)
+
+
+def tom_oqm_append_rows(pages: Pages, layer: int, rotary: Rotary, positions, k, v, q=None, q_out=None, q_norm=None, k_norm=None, norm_eps: float = 1e-6,
+                        stream=None) -> None:
+    """Queries, keys and values [tokens][heads][channels] of any strides: q and k normed where weights are given and turned to `positions` (int64);
+    q into q_out, k and v into the rows behind their sequences'."""
+    _native.append_rows(C.addressof(pages.config), layer, C.addressof(rotary.config), rotary.turns, rotary.amplitude, positions, q, q_out, k, v, q_norm, k_norm,
+                        norm_eps, stream)
+
+
+def tom_oqm_attend_pages_workspace_bytes(pages: Pages, tokens: int, n_q_heads: int) -> int:
+    return lib.tom_oqm_attend_pages_workspace_bytes(C.byref(pages.config), tokens, n_q_heads)
+
+
+def tom_oqm_attend_pages(pages: Pages, layer: int, q, out, mask=None, causal: bool = True, scale: float | None = None, softcap: float = 0.0, prior_out=None,
+                         prior_lse=None, lse=None, workspace=None, stream=None) -> None:
+    """q, out, prior_out [H_q][tokens][d] of the pages' dtype and any strides that are multiples of 16 bytes; prior_lse, lse float32 [H_q][tokens]
+    of any strides; mask int64 [tokens][words], which then takes causal's place.  scale None: d ** -0.5."""
+    _native.attend_pages(C.addressof(pages.config), layer, q, out, mask, causal, scale, softcap, prior_out, prior_lse, lse, workspace, stream)
+
+
+def tom_oqm_keep_rows(pages: Pages, idx, counts, rows_out, stream=None) -> None:
+    """The rows idx[s][0 .. counts[s]) (int32 [sequences][width], ascending) of the call's tokens move together behind their sequences; rows_out
+    (int32 [sequences], may be pages.rows) is how many rows each then has."""
+    _native.keep_rows(C.addressof(pages.config), pages.config.sequences, idx, idx.shape[1], counts, rows_out, stream)
 
 
 # --------------------------------------------------------------------------- convenience
