@@ -27,13 +27,15 @@ struct PagesArgs {
     uint32_t* unit_first;        // [unit][2]: a block's first item, and its parts
 };
 
-// The kernel a call takes: how many query rows of a KV head a workgroup has, its tile of rows, and the least a part has.
+// The kernel a call takes: how many query rows of a KV head a workgroup has (16: the few form), and the least that a part of a sequence has.  By the
+// average of the sequences, since the host knows no more: all forms take any.
 struct PagesForm {
-    int32_t block_rows, tile_rows, least;
+    int32_t block_rows, least;
 };
 inline PagesForm pages_form(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads) {
-    (void)g, (void)tokens, (void)n_q_heads;
-    return {16, 32, 128};
+    const int64_t rows = ((int64_t)tokens + g.sequences - 1) / (g.sequences > 0 ? g.sequences : 1) * (n_q_heads / g.heads);
+    if (g.dtype == TOM_F32 || rows <= 16) return {16, 128};
+    return {rows <= 32 ? 32 : rows <= 64 ? 64 : 128, 256};
 }
 
 struct PagesCuts {
@@ -45,7 +47,7 @@ inline PagesCuts pages_cuts(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_
     const uint64_t repeat = (uint64_t)(n_q_heads / g.heads);
     const uint64_t units = g.starts ? (uint64_t)tokens * repeat / f.block_rows + (uint64_t)(g.sequences < tokens ? g.sequences : tokens)
                                     : (uint64_t)tokens * ((repeat + f.block_rows - 1) / f.block_rows);
-    const uint64_t target = 768;
+    const uint64_t target = f.block_rows == 16 ? 768 : f.block_rows == 32 ? 1024 : 512;
     uint64_t extra = target / (uint64_t)g.heads;
     if (extra < 1) extra = 1;
     if (units * (uint64_t)g.heads >= 2 * target || (int64_t)g.table_pages * g.page_rows <= f.least) extra = 0;

@@ -143,6 +143,15 @@ __device__ __forceinline__ uint32_t unit_of(const PagesArgs& g, int32_t s, int32
     return (uint32_t)first_token * (uint32_t)g.repeat / QT + (uint32_t)min(s, first_token) + (uint32_t)tile;
 }
 
+// For the join: where a block's items begin, and how many they are.
+template <int QT>
+__device__ __forceinline__ void tell_unit(const PagesArgs& g, const Block& b, uint32_t x, int head) {
+    if (g.extra == 0 || head != 0 || x != b.first_item || threadIdx.x != 0) return;
+    uint32_t* const unit = g.unit_first + 2 * (size_t)unit_of<QT>(g, b.sequence, b.first_token, b.tile);
+    unit[0] = b.first_item;
+    unit[1] = b.parts;
+}
+
 // Of the N rows (32 or 64) from t0 those that token `own` of a sequence sees, as bits; what lies behind the sequence's rows is left to the caller.
 template <int N>
 __device__ __forceinline__ uint64_t seen_from(const PagesArgs& g, int32_t t0, int32_t rows, int32_t own, const uint64_t* mask) {
@@ -192,32 +201,46 @@ __device__ __forceinline__ void take_odd(Operand<T>& x, Operand<T>& is) {
     }
 }
 
-// The result of four channels of a row out of its sums, the prior taken in: sums are counted from `from` (units of log 2).
-template <typename T>
-__device__ __forceinline__ void put_row(const PagesArgs& g, int32_t q_head, int32_t token, int c, float from, float total, f32x4 sum) {
-    typedef typename Element<T>::type E;
-    typedef E Vec __attribute__((ext_vector_type(4)));
+// How a row's sums, counted from `from` (units of log 2), become its result, the prior taken in: out = sums * mine + prior * theirs.
+struct RowEnd {
+    float mine, theirs, lse;
+};
+__device__ __forceinline__ RowEnd row_end(const PagesArgs& g, int32_t q_head, int32_t token, float from, float total) {
+    float mine = 1.0f, theirs = 0.0f;
     if (g.prior_lse) {
         const float before = g.prior_lse[q_head * g.prior_lse_head + token * g.prior_lse_row] * kLog2e;
         if (before > -__builtin_inff()) {
-            const float top = fmaxf(from, before), mine = exp2_of(from - top), theirs = exp2_of(before - top);
-            const Vec x = *reinterpret_cast<const Vec*>(g.prior_out + q_head * g.prior_head + token * g.prior_row + (int64_t)c * sizeof(E));
+            const float top = fmaxf(from, before);
+            mine = exp2_of(from - top);
+            theirs = exp2_of(before - top);
             from = top;
             total = total > 0.0f ? total * mine + theirs : theirs;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = sum[i] * mine + theirs * (float)x[i];
         }
     }
     const float by = total > 0.0f ? 1.0f / total : 0.0f;
+    return {mine * by, theirs * by, total > 0.0f ? (from + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff()};
+}
+template <typename T>
+__device__ __forceinline__ void put_channels(const PagesArgs& g, int32_t q_head, int32_t token, int c, f32x4 sum, const RowEnd& end) {
+    typedef typename Element<T>::type E;
+    typedef E Vec __attribute__((ext_vector_type(4)));
+    sum *= end.mine;
+    if (end.theirs != 0.0f) {
+        const Vec x = *reinterpret_cast<const Vec*>(g.prior_out + q_head * g.prior_head + token * g.prior_row + (int64_t)c * sizeof(E));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(end.theirs, (float)x[i], sum[i]);
+    }
     Vec y;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = (E)(sum[i] * by);
+    for (int i = 0; i < 4; ++i) y[i] = (E)sum[i];
     *reinterpret_cast<Vec*>(g.out + q_head * g.out_head + token * g.out_row + (int64_t)c * sizeof(E)) = y;
-    if (c == 0 && g.lse) g.lse[q_head * g.lse_head + token * g.lse_row] = total > 0.0f ? (from + __builtin_amdgcn_logf(total)) * kLn2 : -__builtin_inff();
+}
+// A row's lanes are of one wave and have all read the prior's sum before the row's own is written, so that both may be one array.
+__device__ __forceinline__ void put_lse(const PagesArgs& g, int32_t q_head, int32_t token, const RowEnd& end) {
+    if (g.lse) g.lse[q_head * g.lse_head + token * g.lse_row] = end.lse;
 }
 
-// Parts joined, four channels of a row a lane.  A row's lanes are of one wave: they have read the prior's sum when the first of them
-// writes the row's, so that both may be one array.
+// Parts joined, four channels of a row a lane.
 template <typename T, int QT>
 __global__ __launch_bounds__(kBlock) void join_pages_kernel(PagesArgs g, uint32_t lanes, uint32_t lanes_log2, uint32_t rows, uint32_t inv_heads_all) {
     const uint32_t i = blockIdx.x * kBlock + threadIdx.x, row = i >> lanes_log2;
@@ -257,7 +280,9 @@ __global__ __launch_bounds__(kBlock) void join_pages_kernel(PagesArgs g, uint32_
             sum = sum * mine + x[u] * theirs;
         }
     }
-    put_row<T>(g, (int32_t)q_head, (int32_t)token, c, from, total, sum);
+    const RowEnd end = row_end(g, (int32_t)q_head, (int32_t)token, from, total);
+    put_channels<T>(g, (int32_t)q_head, (int32_t)token, c, sum, end);
+    if (c == 0) put_lse(g, (int32_t)q_head, (int32_t)token, end);
 }
 template <typename T, int QT>
 void start_join_pages(const PagesArgs& g, hipStream_t s) {

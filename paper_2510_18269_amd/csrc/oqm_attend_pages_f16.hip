@@ -1,8 +1,14 @@
 // The attention over pages with queries and rows of f16.
 #include "oqm_attend_pages_few.h"
+#include "oqm_attend_pages_many.h"
 
 namespace oqm {
 
-void start_attend_pages_f16(const PagesArgs& g, const PagesForm&, hipStream_t s) { start_pages_few<In_f16>(g, s); }
+void start_attend_pages_f16(const PagesArgs& g, const PagesForm& form, hipStream_t s) {
+    if (form.block_rows == 16) start_pages_few<In_f16>(g, s);
+    else if (form.block_rows == 32) start_pages_many<In_f16, 1>(g, s);
+    else if (form.block_rows == 64) start_pages_many<In_f16, 2>(g, s);
+    else start_pages_many<In_f16, 4>(g, s);
+}
 
 }  // namespace oqm

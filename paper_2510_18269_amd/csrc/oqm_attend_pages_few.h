@@ -152,13 +152,7 @@ __global__ __launch_bounds__(kBlock) void attend_pages_few_kernel(PagesArgs g) {
     if (!block_of<kPagedRows, kPagedTile, kPagedLeast, kBlock>(g, x, found, b)) return;
     const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
-    if (b.parts > 1 && head == 0 && x == b.first_item && threadIdx.x == 0) {
-        uint32_t* const unit = g.unit_first + 2 * (size_t)unit_of<kPagedRows>(g, b.sequence, b.first_token, b.tile);
-        unit[0] = b.first_item;
-        unit[1] = b.parts;
-    }
-    if (b.parts == 1 && g.extra && head == 0 && threadIdx.x == 0)
-        g.unit_first[2 * (size_t)unit_of<kPagedRows>(g, b.sequence, b.first_token, b.tile) + 1] = 1;
+    tell_unit<kPagedRows>(g, b, x, head);
 
     const int32_t rows = b.tokens * g.repeat, row = b.tile * kPagedRows + a;
     const int32_t mine = row < rows ? row : rows - 1;
@@ -225,7 +219,10 @@ __global__ __launch_bounds__(kBlock) void attend_pages_few_kernel(PagesArgs g) {
             if (c == 0) g.part_stat[slot] = f32pair{from, total};
         } else {
             const int32_t t = (int32_t)div_by((uint32_t)row_at, (uint32_t)g.repeat, g.inv_repeat);
-            put_row<T>(g, head * g.repeat + (row_at - t * g.repeat), b.first_token + t, c, from, total, all);
+            const int32_t h = head * g.repeat + (row_at - t * g.repeat);
+            const RowEnd end = row_end(g, h, b.first_token + t, from, total);
+            put_channels<T>(g, h, b.first_token + t, c, all, end);
+            if (c == 0) put_lse(g, h, b.first_token + t, end);
         }
     }
 }

@@ -1,0 +1,318 @@
+// Attention over pages for many query rows a sequence (drafts, prompts), in 16 bits.
+//
+// A workgroup has 32 query rows of a KV head for each of its NW waves, and its waves share staged tiles of KT rows, two in LDS: the next one is on its way (from
+// memory into LDS past the registers) while a tile is worked on.  S^T = K Q^T in products of 32 x 32 x 16 leaves a lane, for one query row, the scores of 4 of
+// each 8 rows; they become the operand of O^T = V^T P^T where they are, if V^T's rows are taken in the same order, which the transposing LDS read does.
+// Probabilities enter as one part of the type (2^-8 of each in bfloat16, 2^-11 in binary16): its error is that of the output's own rounding, and a second part would make
+// the products half as long again.  Their sum is of the unrounded ones.
+//
+// In LDS a row lies as in memory, but its pieces of 16 bytes are exchanged by row, so that the lanes of a read, which differ in the row, do not meet in a bank.
+#pragma once
+
+#include "oqm_attend_pages_device.h"
+#include "oqm_attend_sums.h"
+
+namespace oqm {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x16 product32(const Operand<In_bf16>& a, const Operand<In_bf16>& b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.w), __builtin_bit_cast(bf16x8, b.w), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 product32(const Operand<In_f16>& a, const Operand<In_f16>& b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a.w), __builtin_bit_cast(f16x8, b.w), c, 0, 0, 0);
+}
+// Four rows of 16 channels, 8 bytes a lane of 16, turned: lane i of 16 gets channel i of the four rows.
+__device__ __forceinline__ u32x2 read_turned(const char* p) {
+    typedef __attribute__((address_space(3))) s16x4* At;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(uint32_t)(uintptr_t)p));
+}
+
+template <typename T_, int DP_, int NW_, bool SERIES>
+struct PagedTiles {
+    typedef T_ T;
+    static constexpr int DP = DP_, NW = NW_, KT = DP == 256 || NW < 4 ? 32 : 64, THREADS = NW * 64, QT = 32 * NW;
+    static constexpr int ROW = DP * 2, CPR = ROW / 16, PART = KT * ROW, STAGE = 2 * PART;  // bytes; pieces of a row
+    static constexpr int STEPS = DP / 16, NB = DP / 32;
+    static constexpr int LOADS = KT * CPR / 64 / NW;  // of a wave, of K and of V
+
+    f32x16 o[NB];
+    float ref, sum;
+
+    static __device__ __forceinline__ int key_swap(int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; }
+    static __device__ __forceinline__ int value_swap(int row) { return DP == 64 ? (row >> 1 & 1) << 2 : (row & 3) << 2; }
+
+    // The tile's rows from memory into LDS; place: of row (lane % KT); whole: all of them are there, and the heads have DP channels.  A load's lanes write
+    // 16 bytes each, one behind the other.
+    static __device__ __forceinline__ void stage(const PagesArgs& g, const char* k, const char* v, uint32_t place, bool whole, int wave, char* lds) {
+        const int lane = (int)__lane_id();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int first = (i * NW + wave) * 64, row = (first + lane) / CPR, piece = (first + lane) % CPR;
+            const uint32_t at = (uint32_t)__shfl((int)place, row, 64);
+            auto load = [&](const char* base, int c, char* to) {
+                const char* p = base + c * 16 + (int64_t)at * 16;
+                if (!whole && (at == kNoPlace || c * 8 >= g.channels)) p = reinterpret_cast<const char*>(kZeroRow);
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+            };
+            load(k, piece ^ key_swap(row), lds + first * 16);
+            load(v, piece ^ value_swap(row), lds + PART + first * 16);
+        }
+    }
+
+    // The operand of V^T of channels 32 n .. 32 n + 31 and rows 16 t .. 16 t + 15 of a tile.
+    static __device__ __forceinline__ Operand<T> values_of(const char* lds, int n, int t) {
+        const int lane = (int)__lane_id(), i = lane & 15, side = lane >> 4 & 1, half = lane >> 5, row = 4 * half + i / 4;
+        const char* const at = lds + (16 * t + row) * ROW + ((4 * n + 2 * side + i % 4 / 2) ^ value_swap(row)) * 16 + (i & 1) * 8;
+        const u32x2 a = read_turned(at), b = read_turned(at + 8 * ROW);
+        Operand<T> x;
+        x.w = u32x4{a[0], a[1], b[0], b[1]};
+        return x;
+    }
+    // Where a row is not for all, a probability of zero times what is not finite there would reach those who do not see it.  So such values are looked for in those tiles,
+    // by the workgroup together, and if there are any, their channels become infinite for those who see them, and the values zero for all.
+    static __device__ __forceinline__ bool odd_values(const char* lds) {
+        bool odd = false;
+        for (int i = (int)threadIdx.x; i < KT * CPR; i += THREADS) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(lds + PART + i * 16);
+            odd = odd || any_odd<T>(x[0]) || any_odd<T>(x[1]) || any_odd<T>(x[2]) || any_odd<T>(x[3]);
+        }
+        return odd;
+    }
+    static __device__ __forceinline__ void clear_odd_values(char* lds) {
+        for (int i = (int)threadIdx.x; i < KT * CPR; i += THREADS) {
+            Operand<T> x, is;
+            x.w = *reinterpret_cast<const u32x4*>(lds + PART + i * 16);
+            take_odd(x, is);
+            *reinterpret_cast<u32x4*>(lds + PART + i * 16) = x.w;
+        }
+    }
+    __device__ __forceinline__ void mark_odd_values(const char* lds, uint64_t see) {
+        const uint64_t mine = see >> (4 * ((int)__lane_id() >> 5));
+#pragma unroll 1
+        for (int t = 0; t < KT / 16; ++t) {
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = (mine >> (16 * t + 8 * (i / 4) + i % 4) & 1u) ? 1.0f : 0.0f;
+            Operand<T> ones;
+            ones.w = pack_items(T{}, e);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                Operand<T> x = values_of(lds + PART, n, t), is;
+                take_odd(x, is);
+                f32x16 count;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) count[j] = 0.0f;
+                count = product32(is, ones, count);
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (count[j] > 0.0f) o[n][j] = __builtin_inff();
+                __builtin_amdgcn_sched_barrier(0);  // one block after the other: this is rare, and its registers are not to be the kernel's
+            }
+        }
+    }
+
+    // 32 rows of a staged tile.  see: of them the lane's query row's; part: whether it is to be asked at all.
+    __device__ __forceinline__ void tile(const PagesArgs& g, const char* keys, const char* vals, const Operand<T> (&q)[STEPS], bool part, uint32_t see) {
+        const int lane = (int)__lane_id(), half = lane >> 5, key = lane & 31;
+        const float base = ref == -__builtin_inff() ? 0.0f : ref, start = g.cap_log2 != 0.0f ? 0.0f : -base;
+        float w[16];
+        {
+            f32x16 d;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) d[i] = 0.0f;
+#pragma unroll
+            for (int u = 0; u < STEPS; ++u) {
+                Operand<T> x;
+                x.w = *reinterpret_cast<const u32x4*>(keys + key * ROW + ((2 * u + half) ^ key_swap(key)) * 16);
+                d = product32(x, q[u], d);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = __builtin_fmaf(d[i], g.scale_log2, start);
+        }
+        if constexpr (SERIES) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = capped_exactly(w[i], g.cap_log2) - base;
+        } else if (g.cap_log2 != 0.0f) {
+            const float high = g.cap_log2 - base;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = capped(w[i], g.cap_log2, high);
+        }
+        const uint32_t mine = see >> (4 * half);
+        if (part) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(mine >> (8 * (i / 4) + i % 4) & 1u)) w[i] = -__builtin_inff();
+        }
+        float high = w[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) high = fmaxf(high, w[i]);
+        const float level = (ref - base) + kRaised<T>;  // RAISED, or -infinity
+        if (__any(high > level + kSlack<T>)) {  // as in Sums::probabilities
+            high = fmaxf(high, lane_xor<32>(high));
+            const float peak = fmaxf(high, level);
+            const float by = exp2_of(fminf(kRaised<T> - peak, 0.0f)), down = fmaxf(peak, -__FLT_MAX__);
+            ref = base + (peak - kRaised<T>);
+            sum *= by;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) o[n] *= by;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                w[i] -= down;
+                if constexpr (kRaised<T> != 0.0f) w[i] += kRaised<T>;
+            }
+        }
+        Operand<T> p[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                e[i] = exp2_of(w[8 * t + i]);
+                sum += e[i];
+            }
+            p[t].w = pack_items(T{}, e);
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) o[n] = product32(values_of(vals, n, t), p[t], o[n]);
+    }
+};
+
+template <typename F>
+__global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages_many_kernel(PagesArgs g) {
+    typedef typename F::T T;
+    constexpr int KT = F::KT, QT = F::QT, STEPS = F::STEPS, NB = F::NB;
+    __shared__ FoundItem found;
+    __shared__ __align__(16) char lds[2 * F::STAGE];
+    const uint32_t x = div_by(blockIdx.x, (uint32_t)g.kv_heads, g.inv_kv_heads);
+    const int head = (int)(blockIdx.x - x * (uint32_t)g.kv_heads);
+    Block b;
+    if (!block_of<QT, KT, 256, F::THREADS>(g, x, found, b)) return;
+    tell_unit<QT>(g, b, x, head);
+    const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int lane = (int)__lane_id(), half = lane >> 5;
+
+    const int32_t rows = b.tokens * g.repeat, row = b.tile * QT + wave * 32 + (lane & 31);
+    const int32_t mine = row < rows ? row : rows - 1;
+    const int32_t own = (int32_t)div_by((uint32_t)mine, (uint32_t)g.repeat, g.inv_repeat), token = b.first_token + own;
+    const int32_t q_head = head * g.repeat + (mine - own * g.repeat);
+    Operand<T> q[STEPS];
+    {
+        const char* const p = g.q + q_head * g.q_head + token * g.q_row;
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) {
+            const int c = 16 * u + 8 * half;
+            q[u].w = *reinterpret_cast<const u32x4*>(c < g.channels ? p + c * 2 : reinterpret_cast<const char*>(kZeroRow));
+        }
+    }
+    const uint64_t* const mask = g.mask ? g.mask + (int64_t)token * g.words : nullptr;
+    const int32_t* const table = g.p.table + (int64_t)b.sequence * g.p.table_pages;
+    const char* const k = g.k + head * g.p.head_bytes;
+    const char* const v = g.v + head * g.p.head_bytes;
+    const bool works = b.tile * QT + wave * 32 < rows;  // a wave of a block's end has no rows but stages with the others
+    // A row's entry is fetched two tiles ahead and looked at one ahead, behind a barrier that has waited for it: a wait of its own would be one for the staged
+    // rows too.
+    auto entry = [&](int32_t t0) {
+        const uint32_t r = (uint32_t)min(t0 + lane % KT, b.end - 1);
+        return table[div_by(r, (uint32_t)g.p.page_rows, g.p.inv_page_rows)];
+    };
+    auto place = [&](int32_t t0, int32_t page) {
+        const uint32_t r = (uint32_t)(t0 + lane % KT);
+        if (r >= (uint32_t)b.end || (uint32_t)page >= (uint32_t)g.p.n_pages) return kNoPlace;
+        return (uint32_t)page * g.p.page_step + (r - div_by(r, (uint32_t)g.p.page_rows, g.p.inv_page_rows) * (uint32_t)g.p.page_rows) * g.p.row_step;
+    };
+    F f;
+    f.ref = -__builtin_inff();
+    f.sum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f.o[n][i] = 0.0f;
+
+    constexpr uint64_t kAll = KT == 64 ? ~uint64_t{0} : 0xffffffffu;
+    const bool full = g.channels == F::DP;
+    uint64_t there = 0;
+    int32_t page = -1;
+    if (b.begin < b.end) {
+        const uint32_t first = place(b.begin, entry(b.begin));
+        there = __ballot(first != kNoPlace) & kAll;
+        page = entry(b.begin + KT);
+        F::stage(g, k, v, first, full && there == kAll, wave, lds);
+    }
+    for (int32_t t0 = b.begin; t0 < b.end; t0 += KT) {
+        char* const here = lds + ((t0 - b.begin) / KT & 1) * F::STAGE;
+        char* const there_next = lds + (((t0 - b.begin) / KT + 1) & 1) * F::STAGE;
+        __syncthreads();  // the tile is there, and the other buffer has been read by all
+        uint64_t next = 0;
+        if (t0 + KT < b.end) {
+            const uint32_t at = place(t0 + KT, page);
+            next = __ballot(at != kNoPlace) & kAll;
+            page = entry(t0 + 2 * KT);
+            if (full && next == kAll) F::stage(g, k, v, at, true, wave, there_next);
+            else F::stage(g, k, v, at, false, wave, there_next);
+        }
+        if (there) {
+            const bool part = there != kAll || t0 + KT > b.rows;
+            uint64_t see = there;
+            if (part) {
+                see &= seen_from<KT>(g, t0, b.rows, own, mask);
+                if (__syncthreads_or(F::odd_values(here))) {
+                    f.mark_odd_values(here, see);
+                    __syncthreads();
+                    F::clear_odd_values(here);
+                    __syncthreads();
+                }
+            }
+            if (works) {
+#pragma unroll
+                for (int i = 0; i < KT / 32; ++i)
+                    if (KT == 32 || (uint32_t)(there >> (32 * i)))
+                        f.tile(g, here + 32 * i * F::ROW, here + F::PART + 32 * i * F::ROW, q, part, (uint32_t)(see >> (32 * i)));
+            }
+        }
+        there = next;
+    }
+    float sum = f.sum;
+    sum += lane_xor<32>(sum);
+    if (row >= rows) return;
+    if (b.parts > 1) {
+        const size_t slot = ((size_t)x * g.kv_heads + head) * QT + wave * 32 + (lane & 31);
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int c = 32 * n + 8 * j + 4 * half;
+                if (c < g.channels) *reinterpret_cast<f32x4*>(g.part_out + slot * g.channels + c) = f32x4{f.o[n][4 * j], f.o[n][4 * j + 1], f.o[n][4 * j + 2], f.o[n][4 * j + 3]};
+            }
+        if (half == 0) g.part_stat[slot] = f32pair{f.ref, sum};
+    } else {
+        const RowEnd end = row_end(g, q_head, token, f.ref, sum);
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int c = 32 * n + 8 * j + 4 * half;
+                if (c < g.channels) put_channels<T>(g, q_head, token, c, f32x4{f.o[n][4 * j], f.o[n][4 * j + 1], f.o[n][4 * j + 2], f.o[n][4 * j + 3]}, end);
+            }
+        if (half == 0) put_lse(g, q_head, token, end);
+    }
+}
+
+template <typename T, int DP, int NW>
+void start_pages_many_of(const PagesArgs& g, hipStream_t s) {
+    const dim3 grid(g.items * (uint32_t)g.kv_heads), block(64 * NW);
+    if (g.cap_log2 > kPlainCap) launch(attend_pages_many_kernel<PagedTiles<T, DP, NW, true>>, grid, block, 0, s, g);
+    else launch(attend_pages_many_kernel<PagedTiles<T, DP, NW, false>>, grid, block, 0, s, g);
+    if (g.extra) start_join_pages<T, 32 * NW>(g, s);
+}
+template <typename T, int NW>
+void start_pages_many(const PagesArgs& g, hipStream_t s) {
+    if (g.channels <= 64) start_pages_many_of<T, 64, NW>(g, s);
+    else if (g.channels <= 128) start_pages_many_of<T, 128, NW>(g, s);
+    else start_pages_many_of<T, 256, NW>(g, s);
+}
+
+}  // namespace oqm
