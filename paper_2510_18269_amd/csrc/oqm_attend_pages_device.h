@@ -30,6 +30,24 @@ __device__ __forceinline__ uint32_t tiles_of(const PagesArgs& g, int32_t tokens)
     return ((uint32_t)tokens * (uint32_t)g.repeat + QT - 1) / QT;  // H_q * tokens is below 2^30
 }
 
+// How far the last token of a block sees: less for the earlier blocks of a sequence where a token does not see those behind it.
+template <int QT>
+__device__ __forceinline__ int32_t end_of(const PagesArgs& g, int32_t rows, int32_t tokens, int32_t tile) {
+    if (!g.causal || g.mask) return (int32_t)min((int64_t)rows + tokens, (int64_t)g.p.capacity);
+    const uint32_t last_row = min((uint32_t)(tile + 1) * QT, (uint32_t)tokens * (uint32_t)g.repeat) - 1;
+    return (int32_t)min((int64_t)rows + div_by(last_row, (uint32_t)g.repeat, g.inv_repeat) + 1, (int64_t)g.p.capacity);
+}
+// Of a sequence's blocks the first that sees `seen` rows or more (their number: none does).
+template <int QT>
+__device__ __forceinline__ uint32_t first_seeing(const PagesArgs& g, int32_t rows, int32_t tokens, int64_t seen) {
+    const uint32_t tiles = tiles_of<QT>(g, tokens);
+    if (seen <= 0 || tiles == 0) return 0;
+    if (min((int64_t)rows + tokens, (int64_t)g.p.capacity) < seen) return tiles;
+    if (!g.causal || g.mask || seen <= rows) return 0;
+    // token t (from 1) sees rows + t; block j's last is min(tokens, ((j + 1) QT - 1) / repeat + 1)
+    return (uint32_t)(((uint64_t)(seen - rows - 1) * (uint32_t)g.repeat) / QT);
+}
+
 // The same in every lane of the workgroup; false: there is nothing for it.
 // All workgroups look at all sequences: a sum over them says how long a part is (so that a long sequence among short ones is cut and they are not), a second
 // one where each one's items begin.  48 sequences cost two passes of one load a lane; the host knows none of the lengths.
@@ -46,7 +64,11 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
         s = 0;
         in_sequence = x;
         base = 0;
-        if (g.extra) {
+        if (!g.extra) {
+            const uint32_t tiles = tiles_of<QT>(g, max(start_of(g.p, 1) - start_of(g.p, 0), 0));
+            if (x >= tiles) return false;
+            in_sequence = tiles - 1 - x;  // the longest first
+        } else {
             const int32_t n = max(start_of(g.p, 1) - start_of(g.p, 0), 0);
             const uint64_t total = (uint64_t)tiles_of<QT>(g, n) * (uint64_t)min((int64_t)rows_of(g.p, 0) + n, (int64_t)g.p.capacity);
             chunk = part_length(total);
@@ -77,7 +99,31 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
             for (int w = 0; w < THREADS / 64; ++w) total += found.totals[w];
             chunk = part_length(total);
         }
+        // Without parts, blocks go by what they see, in steps of 64 rows, the longest first, so that none is left to run alone at the end: that many of them
+        // see `level` steps and more, and x counts on from those that see a step more.
+        int32_t level = 0;
+        uint32_t x_from = 0;
+        auto seeing = [&](int32_t i, int32_t steps) {
+            const int32_t n = max(start_of(g.p, i + 1) - start_of(g.p, i), 0);
+            return tiles_of<QT>(g, n) - first_seeing<QT>(g, rows_of(g.p, i), n, (int64_t)steps * 64);
+        };
+        if (!g.extra) {
+            for (int32_t bit = 1 << (31 - __builtin_clz((uint32_t)g.p.capacity / 64 + 1)); bit > 0; bit /= 2) {
+                uint32_t mine = 0;
+                for (int32_t i = from; i < to; ++i) mine += seeing(i, level + bit);
+                for (int m = 32; m > 0; m /= 2) mine += __shfl_xor(mine, m, 64);
+                if (lane == 0) found.counts[wave] = mine;
+                __syncthreads();
+                uint32_t all = 0;
+                for (int w = 0; w < THREADS / 64; ++w) all += found.counts[w];
+                __syncthreads();
+                if (all > x) level += bit;
+                else x_from = all;  // (the counts fall as levels rise: the last of these is that of one level more)
+            }
+            x -= x_from;
+        }
         auto items = [&](int32_t i) {
+            if (!g.extra) return seeing(i, level) - seeing(i, level + 1);
             uint32_t tiles, rows;
             shape(i, tiles, rows);
             return tiles * max((rows + (uint32_t)chunk - 1u) / (uint32_t)chunk, 1u);
@@ -109,6 +155,10 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
         if (s < 0) return false;
         base = found.base;
         in_sequence = x - base;
+        if (!g.extra) {
+            const int32_t n = max(start_of(g.p, s + 1) - start_of(g.p, s), 0);
+            in_sequence += first_seeing<QT>(g, rows_of(g.p, s), n, (int64_t)level * 64);
+        }
     }
     s = __builtin_amdgcn_readfirstlane(s);
     b.sequence = s;
@@ -127,12 +177,7 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
         b.begin = (int32_t)part * chunk;
         b.end = (int32_t)min((uint32_t)all, (uint32_t)b.begin + (uint32_t)chunk);
     }
-    if (g.causal && !g.mask) {
-        // the block's last token sees nothing behind itself
-        const int32_t last_row = min((b.tile + 1) * QT, b.tokens * g.repeat) - 1;
-        const int32_t last = (int32_t)div_by((uint32_t)last_row, (uint32_t)g.repeat, g.inv_repeat);
-        b.end = (int32_t)min((int64_t)b.end, (int64_t)b.rows + last + 1);
-    }
+    b.end = min(b.end, end_of<QT>(g, b.rows, b.tokens, b.tile));
     return true;
 }
 // Where a block's first item and its parts stand: unique, and below the units that the host counts.  (A sequence with tokens has as many in front of
@@ -240,12 +285,26 @@ __device__ __forceinline__ void put_lse(const PagesArgs& g, int32_t q_head, int3
     if (g.lse) g.lse[q_head * g.lse_head + token * g.lse_row] = end.lse;
 }
 
-// Parts joined, four channels of a row a lane.
-template <typename T, int QT>
-__global__ __launch_bounds__(kBlock) void join_pages_kernel(PagesArgs g, uint32_t lanes, uint32_t lanes_log2, uint32_t rows, uint32_t inv_heads_all) {
-    const uint32_t i = blockIdx.x * kBlock + threadIdx.x, row = i >> lanes_log2;
-    const int c = 4 * (int)(i & (lanes - 1));
-    if (row >= rows || c >= g.channels) return;
+constexpr uint64_t kWideJoin = 48 * 1024;
+// Parts joined, four channels of a row a lane: all of them by one lane, or (WIDE) a workgroup a row, whose sets of lanes take the parts in turn and then join what
+// they have found.
+struct JoinedRow {
+    float from = -__builtin_inff(), total = 0.0f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    __device__ __forceinline__ void add(float their_from, float their_total, f32x4 their_sum) {
+        const float top = fmaxf(from, their_from), base = top == -__builtin_inff() ? 0.0f : top;
+        const float mine = exp2_of(from - base), theirs = exp2_of(their_from - base);
+        from = top;
+        total = total * mine + their_total * theirs;
+        sum = sum * mine + their_sum * theirs;
+    }
+};
+template <typename T, int QT, bool WIDE>
+__global__ __launch_bounds__(kBlock) void join_pages_kernel(PagesArgs g, uint32_t lanes_log2, uint32_t rows, uint32_t inv_heads_all) {
+    const uint32_t lanes = 1u << lanes_log2, lane = threadIdx.x & (lanes - 1);
+    const uint32_t sets = WIDE ? kBlock >> lanes_log2 : 1u, set = WIDE ? threadIdx.x >> lanes_log2 : 0u;
+    const uint32_t row = WIDE ? blockIdx.x : (blockIdx.x * kBlock + threadIdx.x) >> lanes_log2;
+    if (row >= rows) return;
     const uint32_t heads = (uint32_t)(g.kv_heads * g.repeat), token = div_by(row, heads, inv_heads_all), q_head = row - token * heads;
     const int32_t s = sequence_of(g.p, (int32_t)token);
     if (s < 0) return;
@@ -255,40 +314,46 @@ __global__ __launch_bounds__(kBlock) void join_pages_kernel(PagesArgs g, uint32_
     const uint32_t* const unit = g.unit_first + 2 * (size_t)unit_of<QT>(g, s, first_token, (int32_t)(at / QT));
     const uint32_t first = unit[0], parts = min(unit[1], first < g.items ? g.items - first : 0u);  // (starts that overlap leave units that nobody has written)
     if (parts <= 1) return;
+    const int c = 4 * (int)lane, from_c = c < g.channels ? c : 0;
     const size_t step = (size_t)g.kv_heads * QT;
     const size_t slot = ((size_t)first * g.kv_heads + head) * QT + at % QT;
     const f32pair* const stat = g.part_stat + slot;
-    const float* const part = g.part_out + slot * g.channels + c;
+    const float* const part = g.part_out + slot * g.channels + from_c;
     constexpr int kAhead = 4;
-    float from = -__builtin_inff(), total = 0.0f;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t p0 = 0; p0 < parts; p0 += kAhead) {
+    JoinedRow j;
+    for (uint32_t p0 = set; p0 < parts; p0 += sets * kAhead) {
         f32pair st[kAhead];
         f32x4 x[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const size_t n = min(p0 + u, parts - 1) * step;  // behind the last: read again, and not added
+            const size_t n = min(p0 + u * sets, parts - 1) * step;  // behind the last: read again, and not added
             st[u] = stat[n];
             x[u] = *reinterpret_cast<const f32x4*>(part + n * g.channels);
         }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (p0 + u >= parts || st[u].x == -__builtin_inff()) continue;
-            const float top = fmaxf(from, st[u].x), mine = exp2_of(from - top), theirs = exp2_of(st[u].x - top);
-            from = top;
-            total = total * mine + st[u].y * theirs;
-            sum = sum * mine + x[u] * theirs;
-        }
+        for (int u = 0; u < kAhead; ++u)
+            if (p0 + u * sets < parts) j.add(st[u].x, st[u].y, x[u]);
     }
-    const RowEnd end = row_end(g, (int32_t)q_head, (int32_t)token, from, total);
-    put_channels<T>(g, (int32_t)q_head, (int32_t)token, c, sum, end);
+    if constexpr (WIDE) {
+        __shared__ f32pair stats[kBlock];
+        __shared__ f32x4 sums[kBlock];
+        stats[threadIdx.x] = f32pair{j.from, j.total};
+        sums[threadIdx.x] = j.sum;
+        __syncthreads();
+        if (set > 0) return;
+        for (uint32_t i = 1; i < sets; ++i) j.add(stats[i * lanes + lane].x, stats[i * lanes + lane].y, sums[i * lanes + lane]);
+    }
+    if (c >= g.channels) return;
+    const RowEnd end = row_end(g, (int32_t)q_head, (int32_t)token, j.from, j.total);
+    put_channels<T>(g, (int32_t)q_head, (int32_t)token, c, j.sum, end);
     if (c == 0) put_lse(g, (int32_t)q_head, (int32_t)token, end);
 }
 template <typename T, int QT>
 void start_join_pages(const PagesArgs& g, hipStream_t s) {
-    const uint32_t rows = (uint32_t)(g.kv_heads * g.repeat) * (uint32_t)g.p.tokens, lanes_log2 = g.channels <= 64 ? 4 : g.channels <= 128 ? 5 : 6;
-    launch(join_pages_kernel<T, QT>, dim3((uint32_t)((((uint64_t)rows << lanes_log2) + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, g, 1u << lanes_log2, lanes_log2,
-           rows, reciprocal_u32((uint32_t)(g.kv_heads * g.repeat)));
+    const uint32_t heads = (uint32_t)(g.kv_heads * g.repeat), rows = heads * (uint32_t)g.p.tokens;  // (calls with parts have less than 2^20 rows)
+    const uint32_t lanes_log2 = g.channels <= 64 ? 4 : g.channels <= 128 ? 5 : 6;
+    if ((uint64_t)rows << lanes_log2 < kWideJoin) launch(join_pages_kernel<T, QT, true>, dim3(rows), dim3(kBlock), 0, s, g, lanes_log2, rows, reciprocal_u32(heads));
+    else launch(join_pages_kernel<T, QT, false>, dim3((uint32_t)((((uint64_t)rows << lanes_log2) + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, g, lanes_log2, rows, reciprocal_u32(heads));
 }
 
 }  // namespace oqm

@@ -29,6 +29,14 @@ __device__ __forceinline__ u32x2 read_turned(const char* p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(uint32_t)(uintptr_t)p));
 }
 
+// 16 bytes a lane from memory into LDS, lane after lane from `to`, past the registers.  Written out, since the compiler, which cannot tell what it overwrites, would
+// wait for it in front of every turned read: the wait is wait_staged's.  (It has no register to write, and the address is taken when it is issued.)
+__device__ __forceinline__ void load_to_lds(const char* p, char* to) {
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(at) : "m0", "memory");
+}
+__device__ __forceinline__ void wait_staged() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 template <typename T_, int DP_, int NW_, bool SERIES>
 struct PagedTiles {
     typedef T_ T;
@@ -54,7 +62,7 @@ struct PagedTiles {
             auto load = [&](const char* base, int c, char* to) {
                 const char* p = base + c * 16 + (int64_t)at * 16;
                 if (!whole && (at == kNoPlace || c * 8 >= g.channels)) p = reinterpret_cast<const char*>(kZeroRow);
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+                load_to_lds(p, to);
             };
             load(k, piece ^ key_swap(row), lds + first * 16);
             load(v, piece ^ value_swap(row), lds + PART + first * 16);
@@ -113,71 +121,85 @@ struct PagedTiles {
         }
     }
 
-    // 32 rows of a staged tile.  see: of them the lane's query row's; part: whether it is to be asked at all.
-    __device__ __forceinline__ void tile(const PagesArgs& g, const char* keys, const char* vals, const Operand<T> (&q)[STEPS], bool part, uint32_t see) {
+    static __device__ __forceinline__ void load_keys(const char* lds, Operand<T> (&x)[STEPS]) {
         const int lane = (int)__lane_id(), half = lane >> 5, key = lane & 31;
-        const float base = ref == -__builtin_inff() ? 0.0f : ref, start = g.cap_log2 != 0.0f ? 0.0f : -base;
-        float w[16];
-        {
+#pragma unroll
+        for (int u = 0; u < STEPS; ++u) x[u].w = *reinterpret_cast<const u32x4*>(lds + key * ROW + ((2 * u + half) ^ key_swap(key)) * 16);
+    }
+    // A staged tile.  there: its rows that are; see: of them the lane's query row's; part: whether that is to be asked at all.  Reads go out a phase ahead: the values' in
+    // front of the softmax, the next keys' behind it, and the products find them there.
+    __device__ __forceinline__ void tile(const PagesArgs& g, const char* lds, const Operand<T> (&q)[STEPS], bool part, uint64_t there, uint64_t see) {
+        const int half = (int)__lane_id() >> 5;
+        Operand<T> k[STEPS], v[NB][2];
+        load_keys(lds, k);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < KT / 32; ++b) {
+            if (b > 0 && !(uint32_t)(there >> 32)) return;
+            const float base = ref == -__builtin_inff() ? 0.0f : ref, start = g.cap_log2 != 0.0f ? 0.0f : -base;
             f32x16 d;
 #pragma unroll
             for (int i = 0; i < 16; ++i) d[i] = 0.0f;
 #pragma unroll
-            for (int u = 0; u < STEPS; ++u) {
-                Operand<T> x;
-                x.w = *reinterpret_cast<const u32x4*>(keys + key * ROW + ((2 * u + half) ^ key_swap(key)) * 16);
-                d = product32(x, q[u], d);
-            }
+            for (int u = 0; u < STEPS; ++u) d = product32(k[u], q[u], d);
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) v[n][t] = values_of(lds + PART, n, 2 * b + t);
+            __builtin_amdgcn_sched_barrier(0);
+            float w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = __builtin_fmaf(d[i], g.scale_log2, start);
-        }
-        if constexpr (SERIES) {
+            if constexpr (SERIES) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = capped_exactly(w[i], g.cap_log2) - base;
-        } else if (g.cap_log2 != 0.0f) {
-            const float high = g.cap_log2 - base;
+                for (int i = 0; i < 16; ++i) w[i] = capped_exactly(w[i], g.cap_log2) - base;
+            } else if (g.cap_log2 != 0.0f) {
+                const float high = g.cap_log2 - base;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = capped(w[i], g.cap_log2, high);
-        }
-        const uint32_t mine = see >> (4 * half);
-        if (part) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (!(mine >> (8 * (i / 4) + i % 4) & 1u)) w[i] = -__builtin_inff();
-        }
-        float high = w[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) high = fmaxf(high, w[i]);
-        const float level = (ref - base) + kRaised<T>;  // RAISED, or -infinity
-        if (__any(high > level + kSlack<T>)) {  // as in Sums::probabilities
-            high = fmaxf(high, lane_xor<32>(high));
-            const float peak = fmaxf(high, level);
-            const float by = exp2_of(fminf(kRaised<T> - peak, 0.0f)), down = fmaxf(peak, -__FLT_MAX__);
-            ref = base + (peak - kRaised<T>);
-            sum *= by;
-#pragma unroll
-            for (int n = 0; n < NB; ++n) o[n] *= by;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                w[i] -= down;
-                if constexpr (kRaised<T> != 0.0f) w[i] += kRaised<T>;
+                for (int i = 0; i < 16; ++i) w[i] = capped(w[i], g.cap_log2, high);
             }
-        }
-        Operand<T> p[2];
+            if (part) {
+                const uint32_t mine = (uint32_t)(see >> (32 * b + 4 * half));
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            float e[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                e[i] = exp2_of(w[8 * t + i]);
-                sum += e[i];
+                for (int i = 0; i < 16; ++i)
+                    if (!(mine >> (8 * (i / 4) + i % 4) & 1u)) w[i] = -__builtin_inff();
             }
-            p[t].w = pack_items(T{}, e);
+            float high = w[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) high = fmaxf(high, w[i]);
+            const float level = (ref - base) + kRaised<T>;  // RAISED, or -infinity
+            if (__any(high > level + kSlack<T>)) {  // as in Sums::probabilities
+                high = fmaxf(high, lane_xor<32>(high));
+                const float peak = fmaxf(high, level);
+                const float by = exp2_of(fminf(kRaised<T> - peak, 0.0f)), down = fmaxf(peak, -__FLT_MAX__);
+                ref = base + (peak - kRaised<T>);
+                sum *= by;
+#pragma unroll
+                for (int n = 0; n < NB; ++n) o[n] *= by;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    w[i] -= down;
+                    if constexpr (kRaised<T> != 0.0f) w[i] += kRaised<T>;
+                }
+            }
+            Operand<T> p[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    e[i] = exp2_of(w[8 * t + i]);
+                    sum += e[i];
+                }
+                p[t].w = pack_items(T{}, e);
+            }
+            if (b + 1 < KT / 32) load_keys(lds + 32 * (b + 1) * ROW, k);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) o[n] = product32(v[n][t], p[t], o[n]);
         }
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) o[n] = product32(values_of(vals, n, t), p[t], o[n]);
     }
 };
 
@@ -242,18 +264,22 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
         page = entry(b.begin + KT);
         F::stage(g, k, v, first, full && there == kAll, wave, lds);
     }
+    // the queries have arrived: waited for in the loop, they would be waited for in every round, and the staged rows with them
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) asm volatile("" : "+v"(q[u].w));
     for (int32_t t0 = b.begin; t0 < b.end; t0 += KT) {
         char* const here = lds + ((t0 - b.begin) / KT & 1) * F::STAGE;
         char* const there_next = lds + (((t0 - b.begin) / KT + 1) & 1) * F::STAGE;
+        wait_staged();
         __syncthreads();  // the tile is there, and the other buffer has been read by all
         uint64_t next = 0;
         if (t0 + KT < b.end) {
             const uint32_t at = place(t0 + KT, page);
             next = __ballot(at != kNoPlace) & kAll;
-            page = entry(t0 + 2 * KT);
             if (full && next == kAll) F::stage(g, k, v, at, true, wave, there_next);
             else F::stage(g, k, v, at, false, wave, there_next);
         }
+        page = entry(t0 + 2 * KT);
         if (there) {
             const bool part = there != kAll || t0 + KT > b.rows;
             uint64_t see = there;
@@ -266,12 +292,7 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
                     __syncthreads();
                 }
             }
-            if (works) {
-#pragma unroll
-                for (int i = 0; i < KT / 32; ++i)
-                    if (KT == 32 || (uint32_t)(there >> (32 * i)))
-                        f.tile(g, here + 32 * i * F::ROW, here + F::PART + 32 * i * F::ROW, q, part, (uint32_t)(see >> (32 * i)));
-            }
+            if (works) f.tile(g, here, q, part, there, see);
         }
         there = next;
     }
