@@ -31,11 +31,14 @@ __device__ __forceinline__ u32x2 read_turned(const char* p) {
 
 // 16 bytes a lane from memory into LDS, lane after lane from `to`, past the registers.  Written out, since the compiler, which cannot tell what it overwrites, would
 // wait for it in front of every turned read: the wait is wait_staged's.  (It has no register to write, and the address is taken when it is issued.)
-__device__ __forceinline__ void load_to_lds(const char* p, char* to) {
-    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)to);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(at) : "m0", "memory");
+__device__ __forceinline__ void load_to_lds(const char* p, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(to) : "m0", "memory");
 }
 __device__ __forceinline__ void wait_staged() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The tanh by its first terms where all of a wave's |y| are below a quarter, in units of z = 2 log2(e) y: five operations instead of two transcendental ones, a
+// multiplication and an addition.
+constexpr float kSmallTanh = 0.25f * 2.0f * kLog2e;
 
 template <typename T_, int DP_, int NW_, bool SERIES>
 struct PagedTiles {
@@ -53,19 +56,19 @@ struct PagedTiles {
 
     // The tile's rows from memory into LDS; place: of row (lane % KT); whole: all of them are there, and the heads have DP channels.  A load's lanes write
     // 16 bytes each, one behind the other.
-    static __device__ __forceinline__ void stage(const PagesArgs& g, const char* k, const char* v, uint32_t place, bool whole, int wave, char* lds) {
+    static __device__ __forceinline__ void stage(const PagesArgs& g, const char* k, const char* v, uint32_t place, bool whole, int wave, uint32_t lds) {
         const int lane = (int)__lane_id();
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int first = (i * NW + wave) * 64, row = (first + lane) / CPR, piece = (first + lane) % CPR;
             const uint32_t at = (uint32_t)__shfl((int)place, row, 64);
-            auto load = [&](const char* base, int c, char* to) {
+            auto load = [&](const char* base, int c, uint32_t to) {
                 const char* p = base + c * 16 + (int64_t)at * 16;
                 if (!whole && (at == kNoPlace || c * 8 >= g.channels)) p = reinterpret_cast<const char*>(kZeroRow);
                 load_to_lds(p, to);
             };
-            load(k, piece ^ key_swap(row), lds + first * 16);
-            load(v, piece ^ value_swap(row), lds + PART + first * 16);
+            load(k, piece ^ key_swap(row), lds + (uint32_t)(first * 16));
+            load(v, piece ^ value_swap(row), lds + (uint32_t)(PART + first * 16));
         }
     }
 
@@ -136,7 +139,7 @@ struct PagedTiles {
 #pragma unroll
         for (int b = 0; b < KT / 32; ++b) {
             if (b > 0 && !(uint32_t)(there >> 32)) return;
-            const float base = ref == -__builtin_inff() ? 0.0f : ref, start = g.cap_log2 != 0.0f ? 0.0f : -base;
+            const float base = ref == -__builtin_inff() ? 0.0f : ref;
             f32x16 d;
 #pragma unroll
             for (int i = 0; i < 16; ++i) d[i] = 0.0f;
@@ -147,16 +150,31 @@ struct PagedTiles {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) v[n][t] = values_of(lds + PART, n, 2 * b + t);
             __builtin_amdgcn_sched_barrier(0);
+            // A bound of the scores' size: of what is not seen too, and of negative ones, so that it only says when to look closer.
+            float size = fabsf(d[0]);
+#pragma unroll
+            for (int i = 1; i < 16; ++i) size = fmaxf(size, fabsf(d[i]));
+            size *= fabsf(g.scale_log2);
             float w[16];
+            if (g.cap_log2 == 0.0f) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = __builtin_fmaf(d[i], g.scale_log2, start);
-            if constexpr (SERIES) {
+                for (int i = 0; i < 16; ++i) w[i] = __builtin_fmaf(d[i], g.scale_log2, -base);
+            } else if (!__any(size > kSmallTanh)) {
+                // softcap tanh(y) = softcap y (1 - y^2 / 3 + 2 y^4 / 15 - 17 y^6 / 315), y = z / (2 log2 e): the term left out is below 2^-21 of it
+                const float c0 = g.scale_log2 * g.cap_log2 * (0.5f * kLn2), y2 = g.scale_log2 * g.scale_log2 * (0.25f * kLn2 * kLn2);
+                const float c1 = c0 * y2 * (-1.0f / 3.0f), c2 = c0 * y2 * y2 * (2.0f / 15.0f), c3 = c0 * y2 * y2 * y2 * (-17.0f / 315.0f);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = capped_exactly(w[i], g.cap_log2) - base;
-            } else if (g.cap_log2 != 0.0f) {
+                for (int i = 0; i < 16; ++i) {
+                    const float x = d[i] * d[i];
+                    w[i] = __builtin_fmaf(d[i], __builtin_fmaf(x, __builtin_fmaf(x, __builtin_fmaf(x, c3, c2), c1), c0), -base);
+                }
+            } else if constexpr (SERIES) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = capped_exactly(d[i] * g.scale_log2, g.cap_log2) - base;
+            } else {
                 const float high = g.cap_log2 - base;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = capped(w[i], g.cap_log2, high);
+                for (int i = 0; i < 16; ++i) w[i] = capped(d[i] * g.scale_log2, g.cap_log2, high);
             }
             if (part) {
                 const uint32_t mine = (uint32_t)(see >> (32 * b + 4 * half));
@@ -164,22 +182,24 @@ struct PagedTiles {
                 for (int i = 0; i < 16; ++i)
                     if (!(mine >> (8 * (i / 4) + i % 4) & 1u)) w[i] = -__builtin_inff();
             }
-            float high = w[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) high = fmaxf(high, w[i]);
             const float level = (ref - base) + kRaised<T>;  // RAISED, or -infinity
-            if (__any(high > level + kSlack<T>)) {  // as in Sums::probabilities
-                high = fmaxf(high, lane_xor<32>(high));
-                const float peak = fmaxf(high, level);
-                const float by = exp2_of(fminf(kRaised<T> - peak, 0.0f)), down = fmaxf(peak, -__FLT_MAX__);
-                ref = base + (peak - kRaised<T>);
-                sum *= by;
+            if (__any((g.cap_log2 != 0.0f ? g.cap_log2 * (0.5f * kLn2) * size : size) > level + base + kSlack<T>)) {
+                float high = w[0];
 #pragma unroll
-                for (int n = 0; n < NB; ++n) o[n] *= by;
+                for (int i = 1; i < 16; ++i) high = fmaxf(high, w[i]);
+                if (__any(high > level + kSlack<T>)) {  // as in Sums::probabilities
+                    high = fmaxf(high, lane_xor<32>(high));
+                    const float peak = fmaxf(high, level);
+                    const float by = exp2_of(fminf(kRaised<T> - peak, 0.0f)), down = fmaxf(peak, -__FLT_MAX__);
+                    ref = base + (peak - kRaised<T>);
+                    sum *= by;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    w[i] -= down;
-                    if constexpr (kRaised<T> != 0.0f) w[i] += kRaised<T>;
+                    for (int n = 0; n < NB; ++n) o[n] *= by;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        w[i] -= down;
+                        if constexpr (kRaised<T> != 0.0f) w[i] += kRaised<T>;
+                    }
                 }
             }
             Operand<T> p[2];
@@ -256,20 +276,22 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
 
     constexpr uint64_t kAll = KT == 64 ? ~uint64_t{0} : 0xffffffffu;
     const bool full = g.channels == F::DP;
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     uint64_t there = 0;
-    int32_t page = -1;
+    int32_t page = -1, turn = 0;
     if (b.begin < b.end) {
         const uint32_t first = place(b.begin, entry(b.begin));
         there = __ballot(first != kNoPlace) & kAll;
         page = entry(b.begin + KT);
-        F::stage(g, k, v, first, full && there == kAll, wave, lds);
+        F::stage(g, k, v, first, full && there == kAll, wave, lds_at);
     }
     // the queries have arrived: waited for in the loop, they would be waited for in every round, and the staged rows with them
 #pragma unroll
     for (int u = 0; u < STEPS; ++u) asm volatile("" : "+v"(q[u].w));
     for (int32_t t0 = b.begin; t0 < b.end; t0 += KT) {
-        char* const here = lds + ((t0 - b.begin) / KT & 1) * F::STAGE;
-        char* const there_next = lds + (((t0 - b.begin) / KT + 1) & 1) * F::STAGE;
+        char* const here = lds + turn * F::STAGE;
+        turn ^= 1;
+        const uint32_t there_next = lds_at + (uint32_t)turn * F::STAGE;
         wait_staged();
         __syncthreads();  // the tile is there, and the other buffer has been read by all
         uint64_t next = 0;
