@@ -22,6 +22,7 @@ struct PagesArgs {
     // The workgroups of a KV head.  Each sequence's query rows (token by token, the heads of a token beside each other) are cut into blocks,
     // and where `extra` is not zero its rows into parts of one length, the least that the workgroups suffice for.
     uint32_t items, extra;
+    int32_t sorted;              // the blocks that see most go first (there are no parts then)
     float* part_out;             // [items][kv_heads][rows of a block][channels], not normalised; written where there are several parts
     f32pair* part_stat;          // [items][kv_heads][rows of a block]: what scores are counted from, and the sum
     uint32_t* unit_first;        // [unit][2]: a block's first item, and its parts

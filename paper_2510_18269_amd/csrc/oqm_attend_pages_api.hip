@@ -123,6 +123,7 @@ tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, c
     a.inv_repeat = reciprocal_u32((uint32_t)a.repeat);
     a.items = cuts.items;
     a.extra = cuts.extra;
+    a.sorted = cuts.extra == 0 && cuts.items * (uint64_t)pages->heads > 256;
     // Under a cap below 2^-30 all scores are zero to float32's last place beside the one of exp(0); one above 2^40 changes none of up to 2^28.
     if (softcap > 0.0f && softcap < 0x1p-30f) scale = softcap = 0.0f;
     if (softcap > 0x1p40f) softcap = 0.0f;

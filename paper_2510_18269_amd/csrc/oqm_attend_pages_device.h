@@ -99,7 +99,7 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
             for (int w = 0; w < THREADS / 64; ++w) total += found.totals[w];
             chunk = part_length(total);
         }
-        // Without parts, blocks go by what they see, in steps of 64 rows, the longest first, so that none is left to run alone at the end: that many of them
+        // More blocks than run at a time go by what they see, in steps of 64 rows, the longest first, so that none is left to run alone at the end: that many of them
         // see `level` steps and more, and x counts on from those that see a step more.
         int32_t level = 0;
         uint32_t x_from = 0;
@@ -107,7 +107,7 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
             const int32_t n = max(start_of(g.p, i + 1) - start_of(g.p, i), 0);
             return tiles_of<QT>(g, n) - first_seeing<QT>(g, rows_of(g.p, i), n, (int64_t)steps * 64);
         };
-        if (!g.extra) {
+        if (g.sorted) {
             for (int32_t bit = 1 << (31 - __builtin_clz((uint32_t)g.p.capacity / 64 + 1)); bit > 0; bit /= 2) {
                 uint32_t mine = 0;
                 for (int32_t i = from; i < to; ++i) mine += seeing(i, level + bit);
@@ -123,7 +123,7 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
             x -= x_from;
         }
         auto items = [&](int32_t i) {
-            if (!g.extra) return seeing(i, level) - seeing(i, level + 1);
+            if (g.sorted) return seeing(i, level) - seeing(i, level + 1);
             uint32_t tiles, rows;
             shape(i, tiles, rows);
             return tiles * max((rows + (uint32_t)chunk - 1u) / (uint32_t)chunk, 1u);
@@ -155,7 +155,7 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
         if (s < 0) return false;
         base = found.base;
         in_sequence = x - base;
-        if (!g.extra) {
+        if (g.sorted) {
             const int32_t n = max(start_of(g.p, s + 1) - start_of(g.p, s), 0);
             in_sequence += first_seeing<QT>(g, rows_of(g.p, s), n, (int64_t)level * 64);
         }
