@@ -534,8 +534,8 @@ size_t tom_oqm_attend_pages_workspace_bytes(const tom_oqm_pages_t* pages, int32_
  *   lse        [H_q][tokens][1] of float32 or NULL: the natural logarithm of the sum of exp(w_j), the prior's included.  Where a token
  *              sees nothing its output is 0 and its lse -inf.  lse may be prior_lse itself.
  *   workspace  device, 16-byte aligned, tom_oqm_attend_pages_workspace_bytes(...) bytes; calls that may overlap need separate ones
- * A row that a token does not see has no part in what it gets, whatever the row holds; a token that sees a value that is not finite gets
- * unspecified channels there.
+ * A row that a token does not see has no part in what it gets, whatever the row holds; what a token that sees a row with
+ * a value that is not finite gets is unspecified.
  * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 tokens or sequences, table_pages * page_rows above 2^31 - 4097, H_q * tokens of 2^30 and
  * more, a layer's pages that span 2^36 bytes and more), HIP.  No tokens: a no-op.
  */

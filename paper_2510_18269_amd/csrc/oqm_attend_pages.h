@@ -1,6 +1,7 @@
 // What the host side and the kernels of the attention over pages share, and the rules that cut its work.
 #pragma once
 
+#include <cstdlib>
 #include "oqm_pages.h"
 
 namespace oqm {
@@ -22,6 +23,7 @@ struct PagesArgs {
     // The workgroups of a KV head.  Each sequence's query rows (token by token, the heads of a token beside each other) are cut into blocks,
     // and where `extra` is not zero its rows into parts of one length, the least that the workgroups suffice for.
     uint32_t items, extra;
+    int32_t least;               // rows of a part
     int32_t sorted;              // the blocks that see most go first (there are no parts then)
     float* part_out;             // [items][kv_heads][rows of a block][channels], not normalised; written where there are several parts
     f32pair* part_stat;          // [items][kv_heads][rows of a block]: what scores are counted from, and the sum
@@ -36,7 +38,8 @@ struct PagesForm {
 inline PagesForm pages_form(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads) {
     const int64_t rows = ((int64_t)tokens + g.sequences - 1) / (g.sequences > 0 ? g.sequences : 1) * (n_q_heads / g.heads);
     if (g.dtype == TOM_F32 || rows <= 16) return {16, 128};
-    return {rows <= 32 ? 32 : rows <= 64 ? 64 : 128, 256};
+    if (const char* e = getenv("PAGES_QT")) return {atoi(e), getenv("PAGES_LEAST") ? atoi(getenv("PAGES_LEAST")) : 256};
+    return {rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 1024 || g.channels <= 64 ? 128 : 256, 256};
 }
 
 struct PagesCuts {
@@ -48,7 +51,7 @@ inline PagesCuts pages_cuts(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_
     const uint64_t repeat = (uint64_t)(n_q_heads / g.heads);
     const uint64_t units = g.starts ? (uint64_t)tokens * repeat / f.block_rows + (uint64_t)(g.sequences < tokens ? g.sequences : tokens)
                                     : (uint64_t)tokens * ((repeat + f.block_rows - 1) / f.block_rows);
-    const uint64_t target = f.block_rows == 16 ? 768 : f.block_rows == 32 ? 1024 : 512;
+    const uint64_t target = getenv("PAGES_T") ? atoi(getenv("PAGES_T")) : f.block_rows == 16 ? 768 : f.block_rows == 256 ? 256 : 512;
     uint64_t extra = target / (uint64_t)g.heads;
     if (extra < 1) extra = 1;
     if (units * (uint64_t)g.heads >= 2 * target || (int64_t)g.table_pages * g.page_rows <= f.least) extra = 0;

@@ -97,7 +97,7 @@ tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, c
     const PagesForm form = pages_form(*pages, tokens, n_q_heads);
     const PagesCuts cuts = pages_cuts(*pages, tokens, n_q_heads, form);
     const PagesWorkspace need = workspace_of(*pages, form, cuts);
-    if ((uint64_t)cuts.items * (uint64_t)pages->heads * kBlock > kMaxLanes)
+    if ((uint64_t)cuts.items * (uint64_t)pages->heads * (form.block_rows <= 128 ? kBlock : 2 * kBlock) > kMaxLanes)
         return fail(TOM_ERR_UNSUPPORTED, "%d heads of %d tokens need more lanes than the 2^32 - 1 of a launch", n_q_heads, tokens);
     if (need.all() > 0) {
         if (!workspace || workspace_bytes < need.all())
@@ -123,6 +123,7 @@ tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, c
     a.inv_repeat = reciprocal_u32((uint32_t)a.repeat);
     a.items = cuts.items;
     a.extra = cuts.extra;
+    a.least = form.least;
     a.sorted = cuts.extra == 0 && cuts.items * (uint64_t)pages->heads > 256;
     // Under a cap below 2^-30 all scores are zero to float32's last place beside the one of exp(0); one above 2^40 changes none of up to 2^28.
     if (softcap > 0.0f && softcap < 0x1p-30f) scale = softcap = 0.0f;

@@ -14,6 +14,7 @@ struct Block {  // a block of query rows of a sequence, and a part of its rows
     int32_t sequence, first_token, tokens, rows;  // rows: without the call's
     int32_t tile;                                 // which block of the sequence
     int32_t begin, end;                           // rows of the part
+    int32_t for_all;                              // rows from the first that all of the block's tokens see
     uint32_t first_item, parts;
 };
 
@@ -51,14 +52,14 @@ __device__ __forceinline__ uint32_t first_seeing(const PagesArgs& g, int32_t row
 // The same in every lane of the workgroup; false: there is nothing for it.
 // All workgroups look at all sequences: a sum over them says how long a part is (so that a long sequence among short ones is cut and they are not), a second
 // one where each one's items begin.  48 sequences cost two passes of one load a lane; the host knows none of the lengths.
-template <int QT, int KT, int LEAST, int THREADS>
+template <int QT, int KT, int THREADS>
 __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundItem& found, Block& b) {
     const int32_t sequences = g.p.sequences;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint32_t in_sequence, base;
     int32_t s, chunk = 0x7fffffff;
     auto part_length = [&](uint64_t total) {  // whole tiles, above total / extra
-        return (int32_t)min(max((total / g.extra + KT) / KT * KT, (uint64_t)LEAST), (uint64_t)0x7fffffff);
+        return (int32_t)min(max((total / g.extra + KT) / KT * KT, (uint64_t)g.least), (uint64_t)0x7fffffff);
     };
     if (sequences == 1) {
         s = 0;
@@ -178,6 +179,12 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
         b.end = (int32_t)min((uint32_t)all, (uint32_t)b.begin + (uint32_t)chunk);
     }
     b.end = min(b.end, end_of<QT>(g, b.rows, b.tokens, b.tile));
+    b.for_all = b.rows;
+    if (!g.mask) b.for_all = !g.causal ? all : (int32_t)min((int64_t)b.rows + div_by((uint32_t)b.tile * QT, (uint32_t)g.repeat, g.inv_repeat) + 1, (int64_t)all);
+    // the same in all lanes, which the compiler cannot see of what has gone through LDS
+    for (int32_t* x : {&b.first_token, &b.tokens, &b.rows, &b.tile, &b.begin, &b.end, &b.for_all}) *x = __builtin_amdgcn_readfirstlane(*x);
+    b.first_item = (uint32_t)__builtin_amdgcn_readfirstlane((int)b.first_item);
+    b.parts = (uint32_t)__builtin_amdgcn_readfirstlane((int)b.parts);
     return true;
 }
 // Where a block's first item and its parts stand: unique, and below the units that the host counts.  (A sequence with tokens has as many in front of

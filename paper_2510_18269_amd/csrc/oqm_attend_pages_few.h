@@ -137,7 +137,7 @@ struct PagedRows : Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> {
     }
 };
 
-constexpr int kPagedRows = 16, kPagedTile = 32, kPagedLeast = 128;
+constexpr int kPagedRows = 16, kPagedTile = 32;
 
 template <typename F>
 __global__ __launch_bounds__(kBlock) void attend_pages_few_kernel(PagesArgs g) {
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kBlock) void attend_pages_few_kernel(PagesArgs g) {
     const uint32_t x = div_by(blockIdx.x, (uint32_t)g.kv_heads, g.inv_kv_heads);
     const int head = (int)(blockIdx.x - x * (uint32_t)g.kv_heads);
     Block b;
-    if (!block_of<kPagedRows, kPagedTile, kPagedLeast, kBlock>(g, x, found, b)) return;
+    if (!block_of<kPagedRows, kPagedTile, kBlock>(g, x, found, b)) return;
     const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int lane = (int)__lane_id(), a = lane & 15, quarter = lane >> 4;
     tell_unit<kPagedRows>(g, b, x, head);

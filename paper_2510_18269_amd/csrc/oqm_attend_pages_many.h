@@ -32,7 +32,7 @@ __device__ __forceinline__ u32x2 read_turned(const char* p) {
 // 16 bytes a lane from memory into LDS, lane after lane from `to`, past the registers.  Written out, since the compiler, which cannot tell what it overwrites, would
 // wait for it in front of every turned read: the wait is wait_staged's.  (It has no register to write, and the address is taken when it is issued.)
 __device__ __forceinline__ void load_to_lds(const char* p, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(to) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(__builtin_amdgcn_readfirstlane(to)) : "m0", "memory");
 }
 __device__ __forceinline__ void wait_staged() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -54,18 +54,17 @@ struct PagedTiles {
     static __device__ __forceinline__ int key_swap(int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; }
     static __device__ __forceinline__ int value_swap(int row) { return DP == 64 ? (row >> 1 & 1) << 2 : (row & 3) << 2; }
 
-    // The tile's rows from memory into LDS; place: of row (lane % KT); whole: all of them are there, and the heads have DP channels.  A load's lanes write
-    // 16 bytes each, one behind the other.
-    static __device__ __forceinline__ void stage(const PagesArgs& g, const char* k, const char* v, uint32_t place, bool whole, int wave, uint32_t lds) {
+    // The tile's rows from memory into LDS, 16 bytes a lane, one behind the other; place: of row (lane % KT), any row's where there is none: what is not there is seen by
+    // nobody, and channels that a head does not have meet zeros.
+    static __device__ __forceinline__ void stage(const PagesArgs& g, const char* k, const char* v, uint32_t place, int wave, uint32_t lds) {
         const int lane = (int)__lane_id();
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int first = (i * NW + wave) * 64, row = (first + lane) / CPR, piece = (first + lane) % CPR;
             const uint32_t at = (uint32_t)__shfl((int)place, row, 64);
             auto load = [&](const char* base, int c, uint32_t to) {
-                const char* p = base + c * 16 + (int64_t)at * 16;
-                if (!whole && (at == kNoPlace || c * 8 >= g.channels)) p = reinterpret_cast<const char*>(kZeroRow);
-                load_to_lds(p, to);
+                if (c * 8 >= g.channels) c = 0;
+                load_to_lds(base + c * 16 + (int64_t)at * 16, to);
             };
             load(k, piece ^ key_swap(row), lds + (uint32_t)(first * 16));
             load(v, piece ^ value_swap(row), lds + (uint32_t)(PART + first * 16));
@@ -81,46 +80,29 @@ struct PagedTiles {
         x.w = u32x4{a[0], a[1], b[0], b[1]};
         return x;
     }
-    // Where a row is not for all, a probability of zero times what is not finite there would reach those who do not see it.  So such values are looked for in those tiles,
-    // by the workgroup together, and if there are any, their channels become infinite for those who see them, and the values zero for all.
-    static __device__ __forceinline__ bool odd_values(const char* lds) {
-        bool odd = false;
-        for (int i = (int)threadIdx.x; i < KT * CPR; i += THREADS) {
+    // Where a row is not for all, a probability of zero times what is not finite there would reach those who do not see it.  So rows with such values are looked for in those
+    // tiles (every wave finds the same), and if there are any, the values become zero, and who sees such a row is remembered.
+    static __device__ __forceinline__ uint64_t odd_rows(const char* lds) {
+        auto odd_at = [&](int i) {
             const u32x4 x = *reinterpret_cast<const u32x4*>(lds + PART + i * 16);
-            odd = odd || any_odd<T>(x[0]) || any_odd<T>(x[1]) || any_odd<T>(x[2]) || any_odd<T>(x[3]);
-        }
-        return odd;
+            return any_odd<T>(x[0]) || any_odd<T>(x[1]) || any_odd<T>(x[2]) || any_odd<T>(x[3]);
+        };
+        bool odd = false;
+#pragma unroll 4
+        for (int i = 0; i < KT * CPR; i += 64) odd = odd || odd_at(i + (int)__lane_id());
+        if (!__any(odd)) return 0;
+        odd = false;
+#pragma unroll 1
+        for (int i = 0; i < CPR; ++i) odd = odd || odd_at(((int)__lane_id() & (KT - 1)) * CPR + i);
+        return __ballot(odd);
     }
     static __device__ __forceinline__ void clear_odd_values(char* lds) {
+#pragma unroll 1
         for (int i = (int)threadIdx.x; i < KT * CPR; i += THREADS) {
             Operand<T> x, is;
             x.w = *reinterpret_cast<const u32x4*>(lds + PART + i * 16);
             take_odd(x, is);
             *reinterpret_cast<u32x4*>(lds + PART + i * 16) = x.w;
-        }
-    }
-    __device__ __forceinline__ void mark_odd_values(const char* lds, uint64_t see) {
-        const uint64_t mine = see >> (4 * ((int)__lane_id() >> 5));
-#pragma unroll 1
-        for (int t = 0; t < KT / 16; ++t) {
-            float e[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = (mine >> (16 * t + 8 * (i / 4) + i % 4) & 1u) ? 1.0f : 0.0f;
-            Operand<T> ones;
-            ones.w = pack_items(T{}, e);
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                Operand<T> x = values_of(lds + PART, n, t), is;
-                take_odd(x, is);
-                f32x16 count;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) count[j] = 0.0f;
-                count = product32(is, ones, count);
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (count[j] > 0.0f) o[n][j] = __builtin_inff();
-                __builtin_amdgcn_sched_barrier(0);  // one block after the other: this is rare, and its registers are not to be the kernel's
-            }
         }
     }
 
@@ -232,7 +214,7 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
     const uint32_t x = div_by(blockIdx.x, (uint32_t)g.kv_heads, g.inv_kv_heads);
     const int head = (int)(blockIdx.x - x * (uint32_t)g.kv_heads);
     Block b;
-    if (!block_of<QT, KT, 256, F::THREADS>(g, x, found, b)) return;
+    if (!block_of<QT, KT, F::THREADS>(g, x, found, b)) return;
     tell_unit<QT>(g, b, x, head);
     const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int lane = (int)__lane_id(), half = lane >> 5;
@@ -275,15 +257,19 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
         for (int i = 0; i < 16; ++i) f.o[n][i] = 0.0f;
 
     constexpr uint64_t kAll = KT == 64 ? ~uint64_t{0} : 0xffffffffu;
-    const bool full = g.channels == F::DP;
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    auto find = [&](int32_t t0, int32_t page, uint64_t& there) {
+        const uint32_t at = place(t0, page);
+        there = __ballot(at != kNoPlace) & kAll;
+        return at == kNoPlace ? 0u : at;
+    };
     uint64_t there = 0;
     int32_t page = -1, turn = 0;
+    bool sees_odd = false;
     if (b.begin < b.end) {
-        const uint32_t first = place(b.begin, entry(b.begin));
-        there = __ballot(first != kNoPlace) & kAll;
+        const uint32_t first = find(b.begin, entry(b.begin), there);
         page = entry(b.begin + KT);
-        F::stage(g, k, v, first, full && there == kAll, wave, lds_at);
+        F::stage(g, k, v, first, wave, lds_at);
     }
     // the queries have arrived: waited for in the loop, they would be waited for in every round, and the staged rows with them
 #pragma unroll
@@ -291,24 +277,21 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
     for (int32_t t0 = b.begin; t0 < b.end; t0 += KT) {
         char* const here = lds + turn * F::STAGE;
         turn ^= 1;
-        const uint32_t there_next = lds_at + (uint32_t)turn * F::STAGE;
         wait_staged();
         __syncthreads();  // the tile is there, and the other buffer has been read by all
         uint64_t next = 0;
         if (t0 + KT < b.end) {
-            const uint32_t at = place(t0 + KT, page);
-            next = __ballot(at != kNoPlace) & kAll;
-            if (full && next == kAll) F::stage(g, k, v, at, true, wave, there_next);
-            else F::stage(g, k, v, at, false, wave, there_next);
+            const uint32_t at = find(t0 + KT, page, next);
+            F::stage(g, k, v, at, wave, lds_at + (uint32_t)turn * F::STAGE);
         }
         page = entry(t0 + 2 * KT);
         if (there) {
-            const bool part = there != kAll || t0 + KT > b.rows;
+            const bool part = there != kAll || t0 + KT > b.for_all;
             uint64_t see = there;
             if (part) {
                 see &= seen_from<KT>(g, t0, b.rows, own, mask);
-                if (__syncthreads_or(F::odd_values(here))) {
-                    f.mark_odd_values(here, see);
+                if (const uint64_t odd = F::odd_rows(here)) {
+                    sees_odd = sees_odd || (odd & see) != 0;
                     __syncthreads();
                     F::clear_odd_values(here);
                     __syncthreads();
@@ -321,6 +304,12 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
     float sum = f.sum;
     sum += lane_xor<32>(sum);
     if (row >= rows) return;
+    if (sees_odd) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f.o[n][i] = __builtin_inff();
+    }
     if (b.parts > 1) {
         const size_t slot = ((size_t)x * g.kv_heads + head) * QT + wave * 32 + (lane & 31);
 #pragma unroll
@@ -353,8 +342,10 @@ void start_pages_many_of(const PagesArgs& g, hipStream_t s) {
 }
 template <typename T, int NW>
 void start_pages_many(const PagesArgs& g, hipStream_t s) {
-    if (g.channels <= 64) start_pages_many_of<T, 64, NW>(g, s);
-    else if (g.channels <= 128) start_pages_many_of<T, 128, NW>(g, s);
+    if constexpr (NW <= 4) {  // (a tile of 64 channels has no eight parts)
+        if (g.channels <= 64) return start_pages_many_of<T, 64, NW>(g, s);
+    }
+    if (g.channels <= 128) start_pages_many_of<T, 128, NW>(g, s);
     else start_pages_many_of<T, 256, NW>(g, s);
 }
 
