@@ -1,7 +1,6 @@
 // What the host side and the kernels of the attention over pages share, and the rules that cut its work.
 #pragma once
 
-#include <cstdlib>
 #include "oqm_pages.h"
 
 namespace oqm {
@@ -38,8 +37,7 @@ struct PagesForm {
 inline PagesForm pages_form(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads) {
     const int64_t rows = ((int64_t)tokens + g.sequences - 1) / (g.sequences > 0 ? g.sequences : 1) * (n_q_heads / g.heads);
     if (g.dtype == TOM_F32 || rows <= 16) return {16, 128};
-    if (const char* e = getenv("PAGES_QT")) return {atoi(e), getenv("PAGES_LEAST") ? atoi(getenv("PAGES_LEAST")) : 256};
-    return {rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 1024 || g.channels <= 64 ? 128 : 256, 256};
+    return {rows <= 64 ? 64 : rows <= 1024 || g.channels <= 64 || g.channels > 128 ? 128 : 256, 256};
 }
 
 struct PagesCuts {
@@ -51,7 +49,7 @@ inline PagesCuts pages_cuts(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_
     const uint64_t repeat = (uint64_t)(n_q_heads / g.heads);
     const uint64_t units = g.starts ? (uint64_t)tokens * repeat / f.block_rows + (uint64_t)(g.sequences < tokens ? g.sequences : tokens)
                                     : (uint64_t)tokens * ((repeat + f.block_rows - 1) / f.block_rows);
-    const uint64_t target = getenv("PAGES_T") ? atoi(getenv("PAGES_T")) : f.block_rows == 16 ? 768 : f.block_rows == 256 ? 256 : 512;
+    const uint64_t target = f.block_rows == 16 ? 1536 : f.block_rows == 256 ? 256 : 512;
     uint64_t extra = target / (uint64_t)g.heads;
     if (extra < 1) extra = 1;
     if (units * (uint64_t)g.heads >= 2 * target || (int64_t)g.table_pages * g.page_rows <= f.least) extra = 0;

@@ -229,28 +229,12 @@ __device__ __forceinline__ bool any_odd(uint32_t w) {
     if constexpr (__is_same(T, In_f32)) return (w & m) == m;
     else return (w & m) == m || (w & m << 16) == m << 16;
 }
-// Puts zeros in their places, and ones into `is`.
+// The word with zeros in their places.
 template <typename T>
-__device__ __forceinline__ void take_odd(Operand<T>& x, Operand<T>& is) {
-    if constexpr (__is_same(T, In_f32)) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint32_t w = __float_as_uint(x.x[i]);
-            asm("" : "+v"(w));  // a number of its own: of a float's bits the compiler would ask for infinity alone
-            const bool odd = any_odd<T>(w);
-            is.x[i] = odd ? 1.0f : 0.0f;
-            x.x[i] = __uint_as_float(odd ? 0u : w);
-        }
-    } else {
-        constexpr uint32_t m = __is_same(T, In_bf16) ? 0x7f80u : 0x7c00u, one = __is_same(T, In_bf16) ? 0x3f80u : 0x3c00u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t w = x.w[i];
-            const bool low = (w & m) == m, high = (w & m << 16) == m << 16;
-            is.w[i] = (low ? one : 0u) | (high ? one << 16 : 0u);
-            x.w[i] = w & ((low ? 0u : 0xffffu) | (high ? 0u : 0xffff0000u));
-        }
-    }
+__device__ __forceinline__ uint32_t without_odd(uint32_t w) {
+    constexpr uint32_t m = __is_same(T, In_f32) ? 0x7f800000u : __is_same(T, In_bf16) ? 0x7f80u : 0x7c00u;
+    if constexpr (__is_same(T, In_f32)) return (w & m) == m ? 0u : w;
+    else return w & (((w & m) == m ? 0u : 0xffffu) | ((w & m << 16) == m << 16 ? 0u : 0xffff0000u));
 }
 
 // How a row's sums, counted from `from` (units of log 2), become its result, the prior taken in: out = sums * mine + prior * theirs.

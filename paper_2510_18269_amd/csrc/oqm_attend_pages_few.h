@@ -16,8 +16,10 @@ struct PagedRows : Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> {
     typedef Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> S;
     using S::GS, S::VU, S::VN, S::STEPS, S::o;
     static constexpr int DP = DP_, E = elem_bytes<T>::value, KW = 8 * E / 16;  // KW: loads of 16 bytes of 8 channels
+    static constexpr int WAVES = DP == 256 ? 1 : DP == 128 ? (E == 4 ? 2 : 3) : 4;                  // a SIMD: as many as their registers leave without spilling
     static constexpr int VW = VU * E / 4;                                      // words of a value piece
     typedef uint32_t Piece __attribute__((ext_vector_type(VW)));
+    bool sees_odd;
 
     // Channel c of what begins at p, or zeros where the head has no such channel.
     static __device__ __forceinline__ const char* channel(const PagesArgs& g, const char* p, int c) {
@@ -72,43 +74,27 @@ struct PagedRows : Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> {
         this->probabilities(w, base);
         Operand<T> hi, lo;
         split(w[0], hi, lo);
-        // Where a row is not for all, a probability of zero times what is not finite there would reach those who do not see it.
-        bool odd = false;
+        // Where a row is not for all, a probability of zero times what is not finite there would reach those who do not see it: such values become zero, and who sees such a
+        // row is remembered.
         if (__any(see != there)) {
+            bool odd = false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < 8; ++i) odd = odd || odd_piece(vx[i]);
+            if (__any(odd)) {
+                uint32_t rows = 0;
 #pragma unroll
-                for (int n = 0; n < VN; ++n)
+                for (int i = 0; i < 8; ++i) {
+                    const uint64_t lanes = __ballot(odd_piece(vx[i]));
 #pragma unroll
-                    for (int u = 0; u < VW; ++u) odd = odd || any_odd<T>(vx[i][n][u]);
+                    for (int n = 0; n < 4; ++n) rows |= (uint32_t)(lanes >> (16 * n) & 0xffffu ? 1u : 0u) << (16 * (i / 4) + 4 * n + i % 4);
+#pragma unroll
+                    for (int n = 0; n < VN; ++n)
+#pragma unroll
+                        for (int u = 0; u < VW; ++u) vx[i][n][u] = without_odd<T>(vx[i][n][u]);
+                }
+                sees_odd = sees_odd || (rows & see) != 0;
+            }
         }
-        if (__any(odd)) {
-            Operand<T> ones;
-            float one[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) one[i] = seen(i) ? 1.0f : 0.0f;
-            Operand<T> none;
-            split(one, ones, none);
-            values<true>(vx, hi, lo, ones);
-        } else {
-            values<false>(vx, hi, lo, hi);
-        }
-    }
-    template <bool ODD>
-    __device__ __forceinline__ void add(Operand<T> x, const Operand<T>& hi, const Operand<T>& lo, const Operand<T>& ones, f32x4& sum) {
-        if constexpr (ODD) {
-            Operand<T> is;
-            take_odd(x, is);
-            const f32x4 count = product(is, ones, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (count[i] > 0.0f) sum[i] = __builtin_inff();
-        }
-        sum = product(x, hi, sum);
-        if constexpr (E == 2) sum = product(x, lo, sum);
-    }
-    template <bool ODD>
-    __device__ __forceinline__ void values(const Piece (&vx)[8][VN], const Operand<T>& hi, const Operand<T>& lo, const Operand<T>& ones) {
 #pragma unroll
         for (int n = 0; n < VN; ++n) {
             if constexpr (E == 2) {
@@ -121,8 +107,11 @@ struct PagedRows : Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> {
                         even.w[i] = __builtin_amdgcn_perm(y, x, 0x05040100u);
                         odd.w[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
                     }
-                    add<ODD>(even, hi, lo, ones, o[0][n * VU + u]);
-                    add<ODD>(odd, hi, lo, ones, o[0][n * VU + u + 1]);
+                    f32x4 &e = o[0][n * VU + u], &f = o[0][n * VU + u + 1];
+                    e = product(even, hi, e);
+                    e = product(even, lo, e);
+                    f = product(odd, hi, f);
+                    f = product(odd, lo, f);
                 }
             } else {
 #pragma unroll
@@ -130,17 +119,25 @@ struct PagedRows : Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> {
                     Operand<T> x;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x.x[i] = __uint_as_float(vx[i][n][u]);
-                    add<ODD>(x, hi, lo, ones, o[0][n * VU + u]);
+                    o[0][n * VU + u] = product(x, hi, o[0][n * VU + u]);
                 }
             }
         }
+    }
+    static __device__ __forceinline__ bool odd_piece(const Piece (&x)[VN]) {
+        bool odd = false;
+#pragma unroll
+        for (int n = 0; n < VN; ++n)
+#pragma unroll
+            for (int u = 0; u < VW; ++u) odd = odd || any_odd<T>(x[n][u]);
+        return odd;
     }
 };
 
 constexpr int kPagedRows = 16, kPagedTile = 32;
 
 template <typename F>
-__global__ __launch_bounds__(kBlock) void attend_pages_few_kernel(PagesArgs g) {
+__global__ __launch_bounds__(kBlock, F::WAVES) void attend_pages_few_kernel(PagesArgs g) {
     typedef typename F::T T;
     constexpr int DP = F::DP, STEPS = F::STEPS, VU = F::VU, VN = F::VN, GS = F::GS, NW = kBlock / 64;
     __shared__ FoundItem found;
@@ -170,6 +167,7 @@ __global__ __launch_bounds__(kBlock) void attend_pages_few_kernel(PagesArgs g) {
     const char* const v = g.v + head * g.p.head_bytes;
     F f;
     f.clear();
+    f.sees_odd = false;
     uint32_t next = kNoPlace;
     int32_t t0 = b.begin + wave * kPagedTile;
     if (t0 < b.end) next = place_of(g.p, table, (uint32_t)(t0 + (lane & 31)), (uint32_t)b.end);
@@ -193,7 +191,7 @@ __global__ __launch_bounds__(kBlock) void attend_pages_few_kernel(PagesArgs g) {
             for (int u = 0; u < VU; u += 4) {
                 Vec y;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = f.o[0][n * VU + u + j][i];
+                for (int j = 0; j < 4; ++j) y[j] = f.sees_odd ? __builtin_inff() : f.o[0][n * VU + u + j][i];
                 *reinterpret_cast<Vec*>(&sums[wave][a][n * GS + (4 * quarter + i) * VU + u]) = y;
             }
         }

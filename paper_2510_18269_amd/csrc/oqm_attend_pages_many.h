@@ -99,25 +99,35 @@ struct PagedTiles {
     static __device__ __forceinline__ void clear_odd_values(char* lds) {
 #pragma unroll 1
         for (int i = (int)threadIdx.x; i < KT * CPR; i += THREADS) {
-            Operand<T> x, is;
-            x.w = *reinterpret_cast<const u32x4*>(lds + PART + i * 16);
-            take_odd(x, is);
-            *reinterpret_cast<u32x4*>(lds + PART + i * 16) = x.w;
+            u32x4 x = *reinterpret_cast<const u32x4*>(lds + PART + i * 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = without_odd<T>(x[j]);
+            *reinterpret_cast<u32x4*>(lds + PART + i * 16) = x;
         }
     }
 
-    static __device__ __forceinline__ void load_keys(const char* lds, Operand<T> (&x)[STEPS]) {
+    // The operand of K of 32 rows and channels 16 u .. 16 u + 15.
+    static __device__ __forceinline__ Operand<T> key_of(const char* lds, int u) {
         const int lane = (int)__lane_id(), half = lane >> 5, key = lane & 31;
+        Operand<T> x;
+        x.w = *reinterpret_cast<const u32x4*>(lds + key * ROW + ((2 * u + half) ^ key_swap(key)) * 16);
+        return x;
+    }
+    static __device__ __forceinline__ void load_keys(const char* lds, Operand<T> (&x)[STEPS]) {
 #pragma unroll
-        for (int u = 0; u < STEPS; ++u) x[u].w = *reinterpret_cast<const u32x4*>(lds + key * ROW + ((2 * u + half) ^ key_swap(key)) * 16);
+        for (int u = 0; u < STEPS; ++u) x[u] = key_of(lds, u);
     }
     // A staged tile.  there: its rows that are; see: of them the lane's query row's; part: whether that is to be asked at all.  Reads go out a phase ahead: the values' in
     // front of the softmax, the next keys' behind it, and the products find them there.
     __device__ __forceinline__ void tile(const PagesArgs& g, const char* lds, const Operand<T> (&q)[STEPS], bool part, uint64_t there, uint64_t see) {
         const int half = (int)__lane_id() >> 5;
+        // (at 256 channels there are no registers for it)
+        constexpr bool AHEAD = DP < 256;
         Operand<T> k[STEPS], v[NB][2];
-        load_keys(lds, k);
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (AHEAD) {
+            load_keys(lds, k);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int b = 0; b < KT / 32; ++b) {
             if (b > 0 && !(uint32_t)(there >> 32)) return;
@@ -126,12 +136,14 @@ struct PagedTiles {
 #pragma unroll
             for (int i = 0; i < 16; ++i) d[i] = 0.0f;
 #pragma unroll
-            for (int u = 0; u < STEPS; ++u) d = product32(k[u], q[u], d);
+            for (int u = 0; u < STEPS; ++u) d = product32(AHEAD ? k[u] : key_of(lds + 32 * b * ROW, u), q[u], d);
+            if constexpr (AHEAD) {
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+                for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) v[n][t] = values_of(lds + PART, n, 2 * b + t);
-            __builtin_amdgcn_sched_barrier(0);
+                    for (int t = 0; t < 2; ++t) v[n][t] = values_of(lds + PART, n, 2 * b + t);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             // A bound of the scores' size: of what is not seen too, and of negative ones, so that it only says when to look closer.
             float size = fabsf(d[0]);
 #pragma unroll
@@ -195,12 +207,14 @@ struct PagedTiles {
                 }
                 p[t].w = pack_items(T{}, e);
             }
-            if (b + 1 < KT / 32) load_keys(lds + 32 * (b + 1) * ROW, k);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (AHEAD) {
+                if (b + 1 < KT / 32) load_keys(lds + 32 * (b + 1) * ROW, k);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) o[n] = product32(v[n][t], p[t], o[n]);
+                for (int t = 0; t < 2; ++t) o[n] = product32(AHEAD ? v[n][t] : values_of(lds + PART, n, 2 * b + t), p[t], o[n]);
         }
     }
 };
