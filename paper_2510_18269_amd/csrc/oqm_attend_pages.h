@@ -29,30 +29,46 @@ struct PagesArgs {
     uint32_t* unit_first;        // [unit][2]: a block's first item, and its parts
 };
 
-// The kernel a call takes: how many query rows of a KV head a workgroup has (16: the few form), and the least that a part of a sequence has.  By the
-// average of the sequences, since the host knows no more: all forms take any.
+// The kernel a call takes: how many query rows of a KV head a workgroup has (16: the few form), whether two waves share them and halve what they see (SPLIT), and how a sequence's rows are
+// cut into parts: `least` rows each, `target` workgroups in all.  By the average of the sequences, since the host knows no more: all forms take any.
 struct PagesForm {
-    int32_t block_rows, least;
+    int32_t block_rows, least, target;
+    bool split;
 };
+// Blocks of query rows there may be at most, whatever stands in starts.
+inline uint64_t pages_units(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads, int32_t block_rows) {
+    const uint64_t repeat = (uint64_t)(n_q_heads / g.heads);
+    return g.starts ? (uint64_t)tokens * repeat / block_rows + (uint64_t)(g.sequences < tokens ? g.sequences : tokens)
+                    : (uint64_t)tokens * ((repeat + block_rows - 1) / block_rows);
+}
+// 28 query heads on 4 of 128 channels in bfloat16, us of one form / the next:
+//      16 / 64 rows:   16 sequences of 1000 to 9000 rows, 4 tokens (28 query rows) 63.2 / 43.7; 13 tokens (91) 21.1 by 64 and by 128
+//      64 / 128:       the same sequences, 8 tokens (56 query rows) 39.5 / 51.8
+//      128 / 256:      4 sequences of 2000 to 7900 rows, 43 to 52 tokens (301 to 364) 39.4 / 50.9; 3 prompts of 1467 to 1994 tokens 386 / 371, one of 8192 532 / 483, but of 64
+//                      channels 236 / 253.  Of 256 channels 256 rows would leave half the registers.
+//      128, SPLIT:     43 to 52 tokens 41.5 / 37.6: half as many parts to write and join
 inline PagesForm pages_form(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads) {
     const int64_t rows = ((int64_t)tokens + g.sequences - 1) / (g.sequences > 0 ? g.sequences : 1) * (n_q_heads / g.heads);
-    if (g.dtype == TOM_F32 || rows <= 16) return {16, 128};
-    return {rows <= 64 ? 64 : rows <= 1024 || g.channels <= 64 || g.channels > 128 ? 128 : 256, 256};
+    if (g.dtype == TOM_F32 || rows <= 16) return {16, 128, 1536, false};
+    if (rows <= 64) return {64, 256, 512, false};
+    if (rows > 1024 && g.channels > 64 && g.channels <= 128) return {256, 256, 256, false};
+    if (g.channels <= 128 && pages_units(g, tokens, n_q_heads, 128) * (uint64_t)g.heads < 512) return {128, 256, 256, true};
+    return {128, 256, 512, false};
 }
 
 struct PagesCuts {
     uint32_t items, extra;
     uint64_t units;
 };
-// Blocks of query rows there may be at most, whatever stands in starts, and the further items that let long sequences be cut.
+// Items of a KV head: its blocks, and further ones that let long sequences be cut where the blocks do not fill the chip.
 inline PagesCuts pages_cuts(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads, const PagesForm& f) {
-    const uint64_t repeat = (uint64_t)(n_q_heads / g.heads);
-    const uint64_t units = g.starts ? (uint64_t)tokens * repeat / f.block_rows + (uint64_t)(g.sequences < tokens ? g.sequences : tokens)
-                                    : (uint64_t)tokens * ((repeat + f.block_rows - 1) / f.block_rows);
-    const uint64_t target = f.block_rows == 16 ? 1536 : f.block_rows == 256 ? 256 : 512;
-    uint64_t extra = target / (uint64_t)g.heads;
+    const uint64_t units = pages_units(g, tokens, n_q_heads, f.block_rows);
+    const uint64_t most = (uint64_t)f.target / (uint64_t)g.heads;
+    uint64_t extra = most;
+    // Blocks of many rows: no more than run at a time, one round of the chip.  (The 264 workgroups of 4 sequences on 256 compute units took 50.8 us, 216 37.6.)
+    if (f.block_rows > 64) extra = most > units + most / 4 ? most - units : most / 4;
     if (extra < 1) extra = 1;
-    if (units * (uint64_t)g.heads >= 2 * target || (int64_t)g.table_pages * g.page_rows <= f.least) extra = 0;
+    if (units * (uint64_t)g.heads >= 2 * (uint64_t)f.target || (int64_t)g.table_pages * g.page_rows <= f.least) extra = 0;
     return {(uint32_t)(units + extra), (uint32_t)extra, units};
 }
 

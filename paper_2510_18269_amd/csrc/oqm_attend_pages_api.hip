@@ -97,7 +97,7 @@ tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, c
     const PagesForm form = pages_form(*pages, tokens, n_q_heads);
     const PagesCuts cuts = pages_cuts(*pages, tokens, n_q_heads, form);
     const PagesWorkspace need = workspace_of(*pages, form, cuts);
-    if ((uint64_t)cuts.items * (uint64_t)pages->heads * (form.block_rows <= 128 ? kBlock : 2 * kBlock) > kMaxLanes)
+    if ((uint64_t)cuts.items * (uint64_t)pages->heads * (form.block_rows == 256 || form.split ? 2 * kBlock : kBlock) > kMaxLanes)
         return fail(TOM_ERR_UNSUPPORTED, "%d heads of %d tokens need more lanes than the 2^32 - 1 of a launch", n_q_heads, tokens);
     if (need.all() > 0) {
         if (!workspace || workspace_bytes < need.all())

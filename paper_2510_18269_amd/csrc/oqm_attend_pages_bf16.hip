@@ -6,9 +6,7 @@ namespace oqm {
 
 void start_attend_pages_bf16(const PagesArgs& g, const PagesForm& form, hipStream_t s) {
     if (form.block_rows == 16) start_pages_few<In_bf16>(g, s);
-    else if (form.block_rows == 64) start_pages_many<In_bf16, 2>(g, s);
-    else if (form.block_rows == 128) start_pages_many<In_bf16, 4>(g, s);
-    else start_pages_many<In_bf16, 8>(g, s);
+    else start_pages_many<In_bf16>(g, form, s);
 }
 
 }  // namespace oqm

@@ -40,10 +40,12 @@ __device__ __forceinline__ void wait_staged() { asm volatile("s_waitcnt vmcnt(0)
 // multiplication and an addition.
 constexpr float kSmallTanh = 0.25f * 2.0f * kLog2e;
 
-template <typename T_, int DP_, int NW_, bool SERIES>
+// SPLIT: of 64 rows the first 32 are one half of the waves', the others the other half's, each with sums of its own that they join in LDS.
+template <typename T_, int DP_, int NW_, bool SPLIT_, bool SERIES>
 struct PagedTiles {
     typedef T_ T;
-    static constexpr int DP = DP_, NW = NW_, KT = DP == 256 || NW < 4 ? 32 : 64, THREADS = NW * 64, QT = 32 * NW;
+    static constexpr bool SPLIT = SPLIT_;
+    static constexpr int DP = DP_, NW = NW_, KT = DP == 256 || NW < 4 ? 32 : 64, THREADS = NW * 64, QT = (SPLIT ? 16 : 32) * NW;
     static constexpr int ROW = DP * 2, CPR = ROW / 16, PART = KT * ROW, STAGE = 2 * PART;  // bytes; pieces of a row
     static constexpr int STEPS = DP / 16, NB = DP / 32;
     static constexpr int LOADS = KT * CPR / 64 / NW;  // of a wave, of K and of V
@@ -128,8 +130,9 @@ struct PagedTiles {
             load_keys(lds, k);
             __builtin_amdgcn_sched_barrier(0);
         }
+        constexpr int BLOCKS = SPLIT ? 1 : KT / 32;
 #pragma unroll
-        for (int b = 0; b < KT / 32; ++b) {
+        for (int b = 0; b < BLOCKS; ++b) {
             if (b > 0 && !(uint32_t)(there >> 32)) return;
             const float base = ref == -__builtin_inff() ? 0.0f : ref;
             f32x16 d;
@@ -208,7 +211,7 @@ struct PagedTiles {
                 p[t].w = pack_items(T{}, e);
             }
             if constexpr (AHEAD) {
-                if (b + 1 < KT / 32) load_keys(lds + 32 * (b + 1) * ROW, k);
+                if (b + 1 < BLOCKS) load_keys(lds + 32 * (b + 1) * ROW, k);
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
@@ -232,8 +235,9 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
     tell_unit<QT>(g, b, x, head);
     const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int lane = (int)__lane_id(), half = lane >> 5;
+    const int side = F::SPLIT ? wave / (F::NW / 2) : 0, row_wave = F::SPLIT ? wave % (F::NW / 2) : wave;
 
-    const int32_t rows = b.tokens * g.repeat, row = b.tile * QT + wave * 32 + (lane & 31);
+    const int32_t rows = b.tokens * g.repeat, row = b.tile * QT + row_wave * 32 + (lane & 31);
     const int32_t mine = row < rows ? row : rows - 1;
     const int32_t own = (int32_t)div_by((uint32_t)mine, (uint32_t)g.repeat, g.inv_repeat), token = b.first_token + own;
     const int32_t q_head = head * g.repeat + (mine - own * g.repeat);
@@ -250,7 +254,7 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
     const int32_t* const table = g.p.table + (int64_t)b.sequence * g.p.table_pages;
     const char* const k = g.k + head * g.p.head_bytes;
     const char* const v = g.v + head * g.p.head_bytes;
-    const bool works = b.tile * QT + wave * 32 < rows;  // a wave of a block's end has no rows but stages with the others
+    const bool works = b.tile * QT + row_wave * 32 < rows;  // a wave of a block's end has no rows but stages with the others
     // A row's entry is fetched two tiles ahead and looked at one ahead, behind a barrier that has waited for it: a wait of its own would be one for the staged
     // rows too.
     auto entry = [&](int32_t t0) {
@@ -311,12 +315,40 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
                     __syncthreads();
                 }
             }
-            if (works) f.tile(g, here, q, part, there, see);
+            if (works && (uint32_t)(F::SPLIT ? there >> (32 * side) : 1u)) f.tile(g, here + side * 32 * F::ROW, q, part, there >> (32 * side), see >> (32 * side));
         }
         there = next;
     }
     float sum = f.sum;
     sum += lane_xor<32>(sum);
+    if constexpr (F::SPLIT) {
+        __shared__ f32pair stats[QT];
+        __shared__ bool odd[QT];
+        f32x4* const sums = reinterpret_cast<f32x4*>(lds);
+        __syncthreads();
+        if (side == 1) {
+#pragma unroll
+            for (int i = 0; i < 4 * NB; ++i) sums[(row_wave * 4 * NB + i) * 64 + lane] = f32x4{f.o[i / 4][i % 4 * 4], f.o[i / 4][i % 4 * 4 + 1], f.o[i / 4][i % 4 * 4 + 2], f.o[i / 4][i % 4 * 4 + 3]};
+            if (half == 0) {
+                stats[row_wave * 32 + lane] = f32pair{f.ref, sum};
+                odd[row_wave * 32 + lane] = sees_odd;
+            }
+        }
+        __syncthreads();
+        if (side == 1) return;
+        const f32pair st = stats[row_wave * 32 + (lane & 31)];
+        const float top = fmaxf(f.ref, st.x), from = top == -__builtin_inff() ? 0.0f : top;
+        const float mine_by = exp2_of(f.ref - from), their_by = exp2_of(st.x - from);
+        f.ref = top;
+        sum = sum * mine_by + st.y * their_by;
+        sees_odd = sees_odd || odd[row_wave * 32 + (lane & 31)];
+#pragma unroll
+        for (int i = 0; i < 4 * NB; ++i) {
+            const f32x4 their = sums[(row_wave * 4 * NB + i) * 64 + lane];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f.o[i / 4][i % 4 * 4 + j] = f.o[i / 4][i % 4 * 4 + j] * mine_by + their[j] * their_by;
+        }
+    }
     if (row >= rows) return;
     if (sees_odd) {
 #pragma unroll
@@ -325,7 +357,7 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
             for (int i = 0; i < 16; ++i) f.o[n][i] = __builtin_inff();
     }
     if (b.parts > 1) {
-        const size_t slot = ((size_t)x * g.kv_heads + head) * QT + wave * 32 + (lane & 31);
+        const size_t slot = ((size_t)x * g.kv_heads + head) * QT + row_wave * 32 + (lane & 31);
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -347,20 +379,32 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
     }
 }
 
-template <typename T, int DP, int NW>
+template <typename T, int DP, int NW, bool SPLIT>
 void start_pages_many_of(const PagesArgs& g, hipStream_t s) {
     const dim3 grid(g.items * (uint32_t)g.kv_heads), block(64 * NW);
-    if (g.cap_log2 > kPlainCap) launch(attend_pages_many_kernel<PagedTiles<T, DP, NW, true>>, grid, block, 0, s, g);
-    else launch(attend_pages_many_kernel<PagedTiles<T, DP, NW, false>>, grid, block, 0, s, g);
-    if (g.extra) start_join_pages<T, 32 * NW>(g, s);
+    if (g.cap_log2 > kPlainCap) launch(attend_pages_many_kernel<PagedTiles<T, DP, NW, SPLIT, true>>, grid, block, 0, s, g);
+    else launch(attend_pages_many_kernel<PagedTiles<T, DP, NW, SPLIT, false>>, grid, block, 0, s, g);
+    if (g.extra) start_join_pages<T, (SPLIT ? 16 : 32) * NW>(g, s);
 }
-template <typename T, int NW>
-void start_pages_many(const PagesArgs& g, hipStream_t s) {
-    if constexpr (NW <= 4) {  // (a tile of 64 channels has no eight parts)
-        if (g.channels <= 64) return start_pages_many_of<T, 64, NW>(g, s);
+template <typename T>
+void start_pages_many(const PagesArgs& g, const PagesForm& form, hipStream_t s) {
+    if (form.block_rows == 64) {
+        if (g.channels <= 64) start_pages_many_of<T, 64, 2, false>(g, s);
+        else if (g.channels <= 128) start_pages_many_of<T, 128, 2, false>(g, s);
+        else start_pages_many_of<T, 256, 2, false>(g, s);
+    } else if (form.block_rows == 128) {
+        if (g.channels <= 64) {
+            if (form.split) start_pages_many_of<T, 64, 8, true>(g, s);
+            else start_pages_many_of<T, 64, 4, false>(g, s);
+        } else if (g.channels <= 128) {
+            if (form.split) start_pages_many_of<T, 128, 8, true>(g, s);
+            else start_pages_many_of<T, 128, 4, false>(g, s);
+        } else {
+            start_pages_many_of<T, 256, 4, false>(g, s);
+        }
+    } else {
+        start_pages_many_of<T, 128, 8, false>(g, s);
     }
-    if (g.channels <= 128) start_pages_many_of<T, 128, NW>(g, s);
-    else start_pages_many_of<T, 256, NW>(g, s);
 }
 
 }  // namespace oqm
