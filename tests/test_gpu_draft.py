@@ -57,6 +57,18 @@ def test_parents_that_are_none(oqm):
     assert torch.equal(mask.cpu(), paged.to_words(want, 2)) and positions.tolist() == [len(w) - 1 for w in want]
 
 
+def test_tokens_behind_the_most_that_a_draft_may_have(oqm):
+    T = 65536 + 70
+    mask, positions = torch.full((T + 5, 2), 7, dtype=torch.int64, device="cuda"), torch.full((T + 5,), 7, dtype=torch.int64, device="cuda")
+    oqm.tom_oqm_draft_tree(ints([-1] * (T + 5)), ints([0, T, T + 5]), mask, positions)
+    assert (positions[:65536] == 0).all() and (positions[65536:T] == 7).all() and (positions[T:] == 0).all()
+    want = torch.zeros((65536, 2), dtype=torch.int64)
+    for i in range(128):
+        want[i, i // 64] = -2 ** 63 if i % 64 == 63 else 1 << (i % 64)
+    assert torch.equal(mask[:65536].cpu(), want) and (mask[65536:T] == 7).all()
+    assert mask[T:, 0].tolist() == [1 << i for i in range(5)] and (mask[T:, 1] == 0).all()
+
+
 def test_one_token_each(oqm):
     mask, positions = torch.empty((70, 1), dtype=torch.int64, device="cuda"), torch.empty(70, dtype=torch.int64, device="cuda")
     oqm.tom_oqm_draft_tree(ints([-1] * 70), None, mask, positions, ints(list(range(70)), torch.int64))
