@@ -479,6 +479,7 @@ typedef struct {
 /*
  * The tree of drafted tokens: from each token's parent the mask of the tokens that it sees (itself, its parent, and so on
  * up) and its position, once for all layers of a step.
+ * A sequence has 65536 tokens at most: what belongs to those behind them is left as it is.
  *   parents    device int32 [tokens]: the parent's number within the sequence's tokens of this call.  A parent must come before
  *              its children; -1, and any number outside [0, own number), makes the token a root.
  *   starts     device int32 [sequences + 1], or NULL: one token each.  As in tom_oqm_pages_t.
@@ -497,8 +498,8 @@ tom_status_t tom_oqm_draft_tree(const int32_t* parents_device, const int32_t* st
  *   q, q_out   [H_q][tokens][channels], both or neither
  *   k, v       [heads][tokens][channels] of the pages' dtype, heads and channels
  * Inputs and q_out may have any strides and addresses that are multiples of the element size (16 bytes are fastest); q_out may
- * be q itself, with the same strides, and otherwise outputs overlap nothing that is read.  Sequences that are appended to share no
- * page that is written.  Other arguments, arithmetic and errors as there; UNSUPPORTED also where a layer's pages span 2^36 bytes
+ * be q itself, with the same strides, and otherwise outputs overlap nothing that is read.  A page that is written stands in one
+ * sequence's table, and there once.  Other arguments, arithmetic and errors as there; UNSUPPORTED also where a layer's pages span 2^36 bytes
  * and more, and beyond 2^20 sequences.
  */
 tom_status_t tom_oqm_append_rows(const tom_oqm_pages_t* pages, int32_t layer, const tom_oqm_rotary_t* rotary,
@@ -508,7 +509,8 @@ tom_status_t tom_oqm_append_rows(const tom_oqm_pages_t* pages, int32_t layer, co
                                  void* hip_stream);
 
 /* Bytes of device workspace tom_oqm_attend_pages needs for `tokens` new tokens of n_q_heads query heads on these pages.  It goes by
- * their sizes, not by what stands in rows or starts, and grows with the tokens and with the table.  0: none is needed, or arguments that call would refuse. */
+ * these sizes alone, not by what stands in rows or starts, but is not always larger for more tokens: ask for the sizes of each call, or keep the largest.  0: none is
+ * needed, or arguments that call would refuse. */
 size_t tom_oqm_attend_pages_workspace_bytes(const tom_oqm_pages_t* pages, int32_t tokens, int32_t n_q_heads);
 
 /*
@@ -551,7 +553,8 @@ tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, c
  *             appended them.  An index outside [i, the sequence's tokens) leaves row i as it is (any order that is not ascending leaves
  *             unspecified rows).
  *   counts    device int32 [sequences], cut to [0, width]
- *   rows_out  device int32 [sequences]; may be pages->rows itself (a second launch then writes it)
+ *   rows_out  device int32 [sequences]; may be pages->rows itself (a second launch then writes it), and otherwise overlaps nothing that is read
+ * A page that rows move to stands in one sequence's table, and there once.
  * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 sequences, or more 16-byte columns, sequences * layers * heads * 2 * channels / 8, than the
  * 2^32 - 1 lanes of a launch), HIP.  No sequences: a no-op.
  */

@@ -124,7 +124,7 @@ tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, c
     a.items = cuts.items;
     a.extra = cuts.extra;
     a.least = form.least;
-    a.sorted = cuts.extra == 0 && cuts.items * (uint64_t)pages->heads > 256;
+    a.sorted = cuts.extra == 0 && pages->sequences <= kMostSorted && cuts.items * (uint64_t)pages->heads > 256;
     // Under a cap below 2^-30 all scores are zero to float32's last place beside the one of exp(0); one above 2^40 changes none of up to 2^28.
     if (softcap > 0.0f && softcap < 0x1p-30f) scale = softcap = 0.0f;
     if (softcap > 0x1p40f) softcap = 0.0f;
@@ -133,6 +133,7 @@ tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, c
     constexpr float kLog2e = 1.4426950408889634f;
     a.scale_log2 = softcap > 0.0f ? 2.0f * kLog2e * scale / softcap : scale * kLog2e;
     a.cap_log2 = softcap * kLog2e;
+    a.by_terms = std::fabs(a.scale_log2) >= 0x1p-16f && std::fabs(a.scale_log2) <= 0x1p12f;
     (void)hipGetLastError();  // an error that an earlier call of the process left behind is not this launch's
     const hipError_t err = launch_attend_pages(a, form, pages->dtype, static_cast<hipStream_t>(hip_stream));
     if (err != hipSuccess) return fail(TOM_ERR_HIP, "attend_pages launch: %s", hipGetErrorString(err));

@@ -79,6 +79,21 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
         s = (int32_t)(x / tiles);
         in_sequence = x - (uint32_t)s * tiles;
         base = (uint32_t)s * tiles;
+    } else if (!g.extra && sequences > kMostSorted) {
+        // (a look at all of them by every workgroup would cost more than their order gives: x counts units, which some are nobody's of)
+        auto first_unit = [&](int32_t i) {
+            const int32_t at = start_of(g.p, i);
+            return (uint32_t)at * (uint32_t)g.repeat / QT + (uint32_t)min(i, at);
+        };
+        int32_t hi = sequences;  // the last that begins at or in front of x
+        s = 0;
+        while (hi - s > 1) {
+            const int32_t mid = (s + hi) >> 1;
+            if (first_unit(mid) <= x) s = mid;
+            else hi = mid;
+        }
+        base = first_unit(s);
+        in_sequence = x - base;
     } else {
         const int32_t per = (sequences + THREADS - 1) / THREADS, from = min(tid * per, sequences), to = min(from + per, sequences);
         auto shape = [&](int32_t i, uint32_t& tiles, uint32_t& rows) {

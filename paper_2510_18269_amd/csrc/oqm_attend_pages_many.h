@@ -147,16 +147,16 @@ struct PagedTiles {
                     for (int t = 0; t < 2; ++t) v[n][t] = values_of(lds + PART, n, 2 * b + t);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            // A bound of the scores' size: of what is not seen too, and of negative ones, so that it only says when to look closer.
+            // A bound of the scores' size, its own rounding counted in: of what is not seen too, and of negative ones, so that it only says when to look closer.
             float size = fabsf(d[0]);
 #pragma unroll
             for (int i = 1; i < 16; ++i) size = fmaxf(size, fabsf(d[i]));
-            size *= fabsf(g.scale_log2);
+            size *= fabsf(g.scale_log2) * (1.0f + 0x1p-20f);
             float w[16];
             if (g.cap_log2 == 0.0f) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[i] = __builtin_fmaf(d[i], g.scale_log2, -base);
-            } else if (!__any(size > kSmallTanh)) {
+            } else if (g.by_terms && !__any(size > kSmallTanh)) {
                 // softcap tanh(y) = softcap y (1 - y^2 / 3 + 2 y^4 / 15 - 17 y^6 / 315), y = z / (2 log2 e): the term left out is below 2^-21 of it
                 const float c0 = g.scale_log2 * g.cap_log2 * (0.5f * kLn2), y2 = g.scale_log2 * g.scale_log2 * (0.25f * kLn2 * kLn2);
                 const float c1 = c0 * y2 * (-1.0f / 3.0f), c2 = c0 * y2 * y2 * (2.0f / 15.0f), c3 = c0 * y2 * y2 * y2 * (-17.0f / 315.0f);
@@ -180,7 +180,7 @@ struct PagedTiles {
                     if (!(mine >> (8 * (i / 4) + i % 4) & 1u)) w[i] = -__builtin_inff();
             }
             const float level = (ref - base) + kRaised<T>;  // RAISED, or -infinity
-            if (__any((g.cap_log2 != 0.0f ? g.cap_log2 * (0.5f * kLn2) * size : size) > level + base + kSlack<T>)) {
+            if (__any((g.cap_log2 != 0.0f ? g.cap_log2 * (0.5f * kLn2) * size : size) - base > level + kSlack<T>)) {
                 float high = w[0];
 #pragma unroll
                 for (int i = 1; i < 16; ++i) high = fmaxf(high, w[i]);

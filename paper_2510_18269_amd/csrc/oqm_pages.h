@@ -99,7 +99,8 @@ __device__ __forceinline__ uint32_t place_of(const PagePlaces& p, const int32_t*
 __device__ __forceinline__ int32_t start_of(const PagePlaces& p, int32_t s) {
     return p.starts ? min(max(p.starts[s], 0), p.tokens) : min(s, p.tokens);
 }
-__device__ __forceinline__ int32_t rows_of(const PagePlaces& p, int32_t s) { return min(max(p.rows[s], 0), p.capacity); }// Whose token it is: the last sequence that starts at or in front of it, -1 where that has ended before (which with ascending starts is
+__device__ __forceinline__ int32_t rows_of(const PagePlaces& p, int32_t s) { return min(max(p.rows[s], 0), p.capacity); }
+// Whose token it is: the last sequence that starts at or in front of it, -1 where that has ended before (which with ascending starts is
 // nobody's).
 __device__ __forceinline__ int32_t sequence_of(const PagePlaces& p, int32_t token) {
     if (!p.starts) return token < p.sequences ? token : -1;

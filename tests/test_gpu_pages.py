@@ -328,3 +328,137 @@ def test_starts_that_are_wrong_stay_inside(oqm):
         call(oqm, b, pages)
     pages.rows.copy_(torch.tensor(b.rows, dtype=torch.int32))
     close(b, call(oqm, b, pages), b.attention(None, True, b.d ** -0.5, 0.0, None, one_part(b)))
+
+
+# Query rows of a KV head a sequence on average, and workgroups, that lead to each way of cutting: (heads, repeat, rows, new)
+FORMS = {
+    "a few": (2, 5, [70, 0, 33], [3, 1, 2]),
+    "up to 64": (3, 7, [150, 0, 333], [9, 1, 7]),
+    "halved tiles": (2, 7, [150, 0, 1333, 64], [40, 1, 77, 0]),
+    "many blocks": (8, 3, [(13 * i) % 97 for i in range(70)], [30 + i % 7 for i in range(70)]),
+    "prompts": (1, 7, [131, 0], [300, 333]),
+}
+
+
+@pytest.mark.parametrize("dtype,d,page_rows", [("bf16", 128, 50), ("f16", 72, 64), ("bf16", 256, 7), ("f16", 64, 196), ("bf16", 200, 64), ("f16", 128, 3)])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("kind", ["causal", "all", "bits, cap, prior"])
+def test_every_cut_of_the_rows(oqm, form, kind, dtype, d, page_rows):
+    heads, repeat, rows, new = FORMS[form]
+    if len(rows) > 10 and d > 128:
+        pytest.skip("takes the reference long, and the same kernel as halved tiles")
+    b = Batch(dtype=dtype, d=d, page_rows=page_rows, heads=heads, repeat=repeat, rows=rows, new=new, layers=1, layer=0, behind=2,
+              holes=[(0, 0)] + [(s, 1) for s in range(len(new)) if rows[s] + new[s] > page_rows][:1])
+    if kind != "bits, cap, prior":
+        return check(oqm, b, causal=kind == "causal")
+    g = torch.Generator().manual_seed(5)
+    prior = torch.randn(b.q.shape, generator=g).to(DTYPE[dtype]), torch.randn(b.q.shape[:2], generator=g) * 4
+    masks = [[j for j in range(n) if (i * 5 + j * 3) % 4 == 1 or j == i - 1] for n in new for i in range(n)]
+    check(oqm, b, masks=masks, prior=prior, softcap=2.0, scale=0.2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("falling", [False, True])
+def test_scores_that_float32_rounds(oqm, dtype, form, falling):
+    """Scores of 2^27 and more, of which the largest takes all: steps of 128 where float32 has steps of 16, so that a maximum that is kept in float32 may be off by
+    as much, but no probability beside the largest is above 2^-100.  What comes out is its value, off by a probability's rounding and the type's."""
+    heads, repeat, rows, new = FORMS[form]
+    b = Batch(dtype=dtype, d=64, heads=heads, repeat=repeat, rows=rows, new=new, layers=1, layer=0)
+    b.q = torch.zeros_like(b.q)
+    b.q[..., 0], b.q[..., 1] = 8192.0, 128.0
+    P, want, top = b.page_rows, torch.zeros(b.q.shape, dtype=torch.float64), torch.zeros(b.q.shape[:2], dtype=torch.float64)
+    for s in range(b.B):
+        n = rows[s] + new[s]
+        order = [(37 * i) % 211 for i in range(n)] if not falling else [max(0, 255 - i) for i in range(n)]
+        for i, j in enumerate(order):
+            key = torch.zeros(64)
+            key[0], key[1] = 16384.0, float(j)
+            b.k[0, b.table_list[s][i // P], :, i % P] = key.to(DTYPE[dtype])
+        for own in range(new[s]):
+            upto = order[:rows[s] + own + 1]
+            best = max(range(len(upto)), key=lambda i: upto[i])
+            same = [i for i in range(len(upto)) if upto[i] == upto[best]]
+            token = b.starts_list[s] + own
+            top[:, token] = 2.0 ** 27 + 128.0 * upto[best]
+            # equal scores may be weighted differently, since they are off by as much as float32 rounds them: then nothing is asked of the value
+            want[:, token] = b.v64[s][0, :, best].repeat_interleave(repeat, 0) if len(same) == 1 else math.nan
+    got, lse = call(oqm, b, b.pages(oqm), scale=1.0)
+    half = torch.finfo(DTYPE[dtype]).eps / 2
+    assert torch.isfinite(got).all() and torch.isfinite(lse).all()
+    one = ~want.isnan()
+    assert ((got.double() - want).abs() - (2 * half + 2.0 ** -16) * want.abs())[one].max() <= 0
+    assert ((lse.double() - top).abs() / top).max() <= 2.0 ** -21
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_scales_far_from_the_cap(oqm, dtype, form):
+    heads, repeat, rows, new = FORMS[form]
+    b = Batch(dtype=dtype, d=64, heads=heads, repeat=repeat, rows=rows, new=new, layers=1, layer=0, spread=3000.0)
+    check(oqm, b, softcap=1.0, scale=1e-6)
+    b.q = torch.zeros_like(b.q)          # every score is zero, whatever the powers of scale / cap are
+    for scale, cap in ((2.0 ** 40, 1.0), (2.0 ** 20, 2.0 ** -20), (1e-30, 1e-3), (1.0, 2.0 ** 39)):
+        check(oqm, b, softcap=cap, scale=scale)
+
+
+@pytest.mark.parametrize("form", ["up to 64", "halved tiles", "prompts"])
+def test_a_captured_call_of_many_rows_follows_starts(oqm, form):
+    heads, repeat, rows, new = FORMS[form]
+    b = Batch(heads=heads, repeat=repeat, rows=rows, new=new, layers=1, layer=0, d=64)
+    pages, Hq = b.pages(oqm), heads * repeat
+    q, out, lse = b.q.cuda(), torch.zeros(b.q.shape, dtype=torch.bfloat16, device="cuda"), torch.zeros((Hq, b.T), device="cuda")
+    ws = torch.empty(oqm.tom_oqm_attend_pages_workspace_bytes(pages, b.T, Hq), dtype=torch.uint8, device="cuda")
+    oqm.tom_oqm_attend_pages(pages, 0, q, out, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        oqm.tom_oqm_attend_pages(pages, 0, q, out, lse=lse, workspace=ws)
+    want = out.clone(), lse.clone()
+    # with fewer rows in front and fewer tokens the eager call says what a replay has to give, and with the first ones again the first results
+    for less in (1, 0, 2, 0):
+        pages.rows.copy_(torch.tensor([max(0, r - 40 * less) for r in rows], dtype=torch.int32))
+        pages.starts.copy_(torch.tensor([max(0, x - less) for x in b.starts_list], dtype=torch.int32))
+        out.zero_(), lse.zero_(), ws.fill_(255)
+        oqm.tom_oqm_attend_pages(pages, 0, q, out, lse=lse, workspace=ws)
+        eager = out.clone(), lse.clone()
+        out.zero_(), lse.zero_(), ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+        if less == 0:
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    close(b, (out.cpu(), lse.cpu()), b.attention(None, True, b.d ** -0.5, 0.0, None, one_part(b)))
+
+
+def test_two_calls_at_once(oqm):
+    """On two streams, each with a workspace of its own, on the same pages."""
+    b = Batch(rows=[9000, 300], new=[20, 3], heads=2, d=64, page_rows=50, layers=1, layer=0)
+    pages, Hq = b.pages(oqm), b.heads * b.repeat
+    want = call(oqm, b, pages)
+    q, size = b.q.cuda(), oqm.tom_oqm_attend_pages_workspace_bytes(pages, b.T, Hq)
+    outs = [(torch.zeros(q.shape, dtype=q.dtype, device="cuda"), torch.zeros((Hq, b.T), device="cuda"), torch.empty(size, dtype=torch.uint8, device="cuda")) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for stream, (out, lse, ws) in zip(streams, outs):
+            oqm.tom_oqm_attend_pages(pages, 0, q, out, lse=lse, workspace=ws, stream=stream)
+    torch.cuda.synchronize()
+    for out, lse, _ in outs:
+        assert torch.equal(out.cpu(), want[0]) and torch.equal(lse.cpu(), want[1])
+
+
+def test_sequences_that_share_pages(oqm):
+    """One prompt's pages in the tables of all, each with a last page of its own."""
+    b = Batch(rows=[64, 64, 64], new=[3, 3, 3], page_rows=16, layers=1, layer=0)
+    for s in (1, 2):
+        b.table_list[s][:4] = b.table_list[0][:4]
+        for mine, first in ((b.k64[s], b.k64[0]), (b.v64[s], b.v64[0])):
+            mine[:, :, :64] = first[:, :, :64]
+    check(oqm, b, parents=paged.tree(b.new, 3))
+
+
+def test_more_sequences_than_lanes_and_more_blocks_than_fit(oqm):
+    b = Batch(rows=[(i * i * 7) % 61 for i in range(1500)], new=[(i % 3) for i in range(1500)], heads=4, repeat=2, d=64, layers=1, layer=0, page_rows=32)
+    assert oqm.tom_oqm_attend_pages_workspace_bytes(b.pages(oqm), b.T, 8) == 0
+    check(oqm, b)

@@ -119,13 +119,12 @@ def test_without_starts_there_is_one_token_each(oqm):
     refuses(oqm, "without starts", lambda: oqm._check(oqm.lib.tom_oqm_draft_tree(0x1000, None, 3, 4, 0x2000, 1, None, None, None)))
 
 
-def test_workspaces_grow_with_tokens_and_tables(oqm):
+def test_workspaces_go_by_sizes(oqm):
     for heads in (2, 6, 14, 64):
-        last = 0
-        for tokens in (1, 2, 5, 16, 17, 40, 100, 500):
+        for tokens in (1, 2, 5, 16, 17, 40, 100, 500, 5000):
             n = oqm.tom_oqm_attend_pages_workspace_bytes(pages(oqm, table_pages=4000), tokens, heads)
-            assert n == 0 or n >= last or tokens * heads > 1000
-            last = n
+            assert n % 16 == 0 and n == oqm.tom_oqm_attend_pages_workspace_bytes(pages(oqm, table_pages=5000), tokens, heads)
+            assert n > 0 or tokens * heads > 1000
     assert oqm.tom_oqm_attend_pages_workspace_bytes(pages(oqm), 0, 6) == 0
     assert oqm.tom_oqm_attend_pages_workspace_bytes(pages(oqm), 7, 5) == 0
     assert oqm.tom_oqm_attend_pages_workspace_bytes(pages(oqm, table_pages=1), 7, 6) == 0   # nothing to be cut
