@@ -51,7 +51,7 @@ inline uint64_t pages_units(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_
 inline PagesForm pages_form(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads) {
     const int64_t rows = ((int64_t)tokens + g.sequences - 1) / (g.sequences > 0 ? g.sequences : 1) * (n_q_heads / g.heads);
     if (g.dtype == TOM_F32 || rows <= 16) return {16, 128, 1536, false};
-    if (rows <= 64) return {64, 256, 512, false};
+    if (rows <= 64) return {64, 256, 640, false};
     if (rows > 1024 && g.channels > 64 && g.channels <= 128) return {256, 256, 256, false};
     if (g.channels <= 128 && pages_units(g, tokens, n_q_heads, 128) * (uint64_t)g.heads < 512) return {128, 256, 256, true};
     return {128, 256, 512, false};
