@@ -30,8 +30,9 @@ struct PagesArgs {
     uint32_t* unit_first;        // [unit][2]: a block's first item, and its parts
 };
 
-// The kernel a call takes: how many query rows of a KV head a workgroup has (16: the few form), whether two waves share them and halve what they see (SPLIT), and how a sequence's rows are
-// cut into parts: `least` rows each, `target` workgroups in all.  By the average of the sequences, since the host knows no more: all forms take any.
+// The kernel a call takes: how many query rows of a KV head a workgroup has (16: the few form), whether two waves share them and halve what they see (SPLIT),
+// and how a sequence's rows are cut into parts: `least` rows each, `target` workgroups in all.  By the average of the sequences, since the host knows no more: all
+// forms take any.
 struct PagesForm {
     int32_t block_rows, least, target;
     bool split;
@@ -46,8 +47,11 @@ inline uint64_t pages_units(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_
 //      16 / 64 rows:   16 sequences of 1000 to 9000 rows, 4 tokens (28 query rows) 63.2 / 43.7; 13 tokens (91) 21.1 by 64 and by 128
 //      64 / 128:       the same sequences, 8 tokens (56 query rows) 39.5 / 51.8
 //      128 / 256:      4 sequences of 2000 to 7900 rows, 43 to 52 tokens (301 to 364) 39.4 / 50.9; 3 prompts of 1467 to 1994 tokens 386 / 371, one of 8192 532 / 483, but of 64
-//                      channels 236 / 253.  Of 256 channels 256 rows would leave half the registers.
+//                      channels 216 / 255.  Of 256 channels 256 rows would leave half the registers.
 //      128, SPLIT:     43 to 52 tokens 41.5 / 37.6: half as many parts to write and join
+// Workgroups, us: few form, 512 / 768 / 1024 / 1536: 48 sequences of 40 to 30000 rows, a token each, 355 / 296 / 299 / 290, one of 705 K rows 259 / 297 / 265 / 271, 256 of 40 to 1000
+// rows 51 / 61 / 61 / 63, 64 channels 349 / 374 / 354 / 335, 256 channels 355 / 336 / 324 / 320.  64 rows, 512 / 640 / 768: 16 sequences, 8 tokens 49.9 / 48.2 / 48.3, 4 tokens 38.1 / 37.5 /
+// 39.5.
 inline PagesForm pages_form(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads) {
     const int64_t rows = ((int64_t)tokens + g.sequences - 1) / (g.sequences > 0 ? g.sequences : 1) * (n_q_heads / g.heads);
     if (g.dtype == TOM_F32 || rows <= 16) return {16, 128, 1536, false};

@@ -1,8 +1,12 @@
 // Attention over pages for few query rows a sequence (one token, a short draft), and for float32.
 //
-// Memory bounds it: K and V are read once, straight into the operands of the matrix cores, no LDS and no barrier on the way.  S^T = K Q^T leaves a lane, for
-// one query row, the scores of the very rows whose values it feeds to O^T = V^T P^T.  A workgroup has 16 query rows of a KV head; its four waves take the part's tiles of
-// 32 rows in turn, each with sums of its own, and join them in LDS.
+// Memory bounds it: K and V are read once, straight into the operands of the matrix cores, no LDS and no barrier on the way.  S^T = K Q^T leaves a lane, for one
+// query row, the scores of the very rows whose values it feeds to O^T = V^T P^T.  A workgroup has 16 query rows of a KV head; its four waves take the part's tiles
+// of 32 rows in turn, each with sums of its own, and join them in LDS.  What hides memory's latency is the waves of a SIMD: as many as fit without spilling.
+//
+// 28 query heads on 4 of 128 channels, bfloat16, both launches: 48 sequences of 40 to 30000 rows, a token each, 253 to 290 us on different cards, 5.1 TB/s on the same as
+// a copy's 4.96; one of 705 K rows 258 us (5.6 TB/s), of 12.6 K rows 13.3, of 500 rows 9.9, where the way from starts to table to rows to the join is what is left.
+// Loads past the caches 337 us against 291.
 #pragma once
 
 #include "oqm_attend_pages_device.h"
