@@ -462,3 +462,46 @@ def test_more_sequences_than_lanes_and_more_blocks_than_fit(oqm):
     b = Batch(rows=[(i * i * 7) % 61 for i in range(1500)], new=[(i % 3) for i in range(1500)], heads=4, repeat=2, d=64, layers=1, layer=0, page_rows=32)
     assert oqm.tom_oqm_attend_pages_workspace_bytes(b.pages(oqm), b.T, 8) == 0
     check(oqm, b)
+
+
+@pytest.mark.parametrize("heads,repeat,rows,new,d,page_rows,parts", [
+    (32, 9, [2100 + i if i % 13 == 0 else 20 for i in range(40)], [2] * 40, 64, 32, False),
+    (8, 3, [2100 + i if i % 13 == 0 else 20 for i in range(90)], [33] * 90, 64, 50, False),
+    (1, 7, [30000], [1200], 72, 256, True)])
+def test_parts_of_more_rows_than_are_looked_up_at_a_time(oqm, heads, repeat, rows, new, d, page_rows, parts):
+    b = Batch(heads=heads, repeat=repeat, rows=rows, new=new, d=d, page_rows=page_rows, layers=1, layer=0, holes=[(0, 3), (0, 40)])
+    assert (oqm.tom_oqm_attend_pages_workspace_bytes(b.pages(oqm), b.T, heads * repeat) > 0) == parts
+    check(oqm, b)
+
+
+@pytest.mark.parametrize("new", [[1, 2], [9, 5], [70, 3]])
+def test_pools_whose_offsets_pass_32_bits(oqm, new):
+    """Pages at the ends of a pool of 40 GiB (places counted in 16 bytes pass 2^31), K and V beside each other in it: the same as in a small pool, bit for bit."""
+    b = Batch(rows=[200, 100], new=new, layers=1, layer=0, page_rows=64)
+    want = call(oqm, b, b.pages(oqm))
+    page = 2 * b.heads * b.page_rows * b.d
+    n = 40 * 2 ** 30 // (2 * page)
+    pool = torch.empty((n, 2, b.heads, b.page_rows, b.d), dtype=torch.bfloat16, device="cuda")
+    at = [p if p % 3 == 0 else n - 1 - p for p in range(b.n_pages)]
+    for p in range(b.n_pages):
+        pool[at[p], 0], pool[at[p], 1] = b.k[0, p].cuda(), b.v[0, p].cuda()
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = ints([[at[p] if 0 <= p < b.n_pages else -1 for p in t] for t in b.table_list])
+    pages = oqm.Pages.create(pool[:, 0][None], pool[:, 1][None], table, ints(b.rows), ints(b.starts_list))
+    got = call(oqm, b, pages)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    # the last token of each sequence is kept as its first, and rows appended behind it come back as they were given
+    idx, counts = ints([[x - 1] for x in new]), ints([1, 1])
+    oqm.tom_oqm_keep_rows(pages, idx, counts, pages.rows)
+    assert pages.rows.tolist() == [r + 1 for r in b.rows]
+    for s in range(2):
+        page_of = lambda r: at[b.table_list[s][r // 64]]  # noqa: E731
+        for half, source in ((0, b.k64), (1, b.v64)):
+            kept = pool[page_of(b.rows[s]), half, :, b.rows[s] % 64].cpu().double()
+            assert torch.equal(kept, source[s][0, :, b.rows[s] + new[s] - 1])
+    values = torch.randn((2, b.heads, b.d), dtype=torch.bfloat16, device="cuda")
+    pages = oqm.Pages.create(pool[:, 0][None], pool[:, 1][None], table, ints(b.rows), None)
+    oqm.tom_oqm_append_rows(pages, 0, oqm.Rotary.create(64), torch.zeros(2, dtype=torch.int64, device="cuda"), values, values)
+    for s in range(2):
+        for half in range(2):
+            assert torch.equal(pool[at[b.table_list[s][b.rows[s] // 64]], half, :, b.rows[s] % 64], values[s])
