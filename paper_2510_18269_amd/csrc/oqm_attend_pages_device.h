@@ -51,7 +51,7 @@ __device__ __forceinline__ uint32_t first_seeing(const PagesArgs& g, int32_t row
 
 // The same in every lane of the workgroup; false: there is nothing for it.
 // All workgroups look at all sequences: a sum over them says how long a part is (so that a long sequence among short ones is cut and they are not), a second
-// one where each one's items begin.  48 sequences cost two passes of one load a lane, 4.5 us; the host knows none of the lengths.
+// one where each one's items begin; the host knows none of the lengths.
 template <int QT, int KT, int THREADS>
 __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundItem& found, Block& b) {
     const int32_t sequences = g.p.sequences;
@@ -61,19 +61,58 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
     auto part_length = [&](uint64_t total) {  // whole tiles, above total / extra
         return (int32_t)min(max((total / g.extra + KT) / KT * KT, (uint64_t)g.least), (uint64_t)0x7fffffff);
     };
+    int32_t first_token = -1, tokens = 0, rows = 0;  // of s, once they are known
     if (sequences == 1) {
         s = 0;
-        in_sequence = x;
         base = 0;
-        if (!g.extra) {
-            const uint32_t tiles = tiles_of<QT>(g, max(start_of(g.p, 1) - start_of(g.p, 0), 0));
+        const int32_t n = max(start_of(g.p, 1) - start_of(g.p, 0), 0);
+        const uint32_t tiles = tiles_of<QT>(g, n);
+        in_sequence = x;
+        if (g.extra) {
+            chunk = part_length((uint64_t)tiles * (uint64_t)min((int64_t)rows_of(g.p, 0) + n, (int64_t)g.p.capacity));
+        } else {
             if (x >= tiles) return false;
             in_sequence = tiles - 1 - x;  // the longest first
-        } else {
-            const int32_t n = max(start_of(g.p, 1) - start_of(g.p, 0), 0);
-            const uint64_t total = (uint64_t)tiles_of<QT>(g, n) * (uint64_t)min((int64_t)rows_of(g.p, 0) + n, (int64_t)g.p.capacity);
-            chunk = part_length(total);
         }
+    } else if (sequences <= 64 && (g.p.starts || g.extra)) {
+        // One a lane, in every wave for itself: the same as below without LDS or a barrier, and what a lane has loaded is not loaded again.  4 drafts of 43 to 52 tokens, us,
+        // as below 37.6, so 35.9; three prompts 369 / 360; but one sequence 13.2 / 13.7 (and above 13.2).
+        const int32_t i = min(lane, sequences - 1), first = start_of(g.p, i), behind = start_of(g.p, i + 1);
+        const int32_t had = rows_of(g.p, i), n = lane < sequences ? max(behind - first, 0) : 0;
+        const uint32_t tiles = tiles_of<QT>(g, n), all = (uint32_t)min((int64_t)had + n, (int64_t)g.p.capacity);
+        uint32_t mine = tiles, level = 0;
+        if (g.extra) {
+            uint64_t total = (uint64_t)tiles * all;
+            for (int m = 32; m > 0; m /= 2) total += __shfl_xor(total, m, 64);
+            chunk = part_length(total);
+            mine *= max((all + (uint32_t)chunk - 1u) / (uint32_t)chunk, 1u);
+        } else if (g.sorted) {
+            auto seeing = [&](uint32_t steps) { return tiles - first_seeing<QT>(g, had, n, (int64_t)steps * 64); };
+            uint32_t x_from = 0;
+            for (uint32_t bit = 1u << (31 - __builtin_clz((uint32_t)g.p.capacity / 64 + 1)); bit > 0; bit /= 2) {
+                uint32_t all_seeing = seeing(level + bit);
+                for (int m = 32; m > 0; m /= 2) all_seeing += __shfl_xor(all_seeing, m, 64);
+                if (all_seeing > x) level += bit;
+                else x_from = all_seeing;
+            }
+            x -= x_from;
+            mine = seeing(level) - seeing(level + 1);
+        }
+        uint32_t before = mine;
+        for (int m = 1; m < 64; m *= 2) {
+            const uint32_t other = __shfl_up(before, m, 64);
+            if (lane >= m) before += other;
+        }
+        before -= mine;
+        const uint64_t hit = __ballot(x >= before && x < before + mine);
+        if (!hit) return false;
+        s = __builtin_ctzll(hit);
+        base = (uint32_t)__builtin_amdgcn_readlane((int)before, s);
+        first_token = __builtin_amdgcn_readlane(first, s);
+        tokens = __builtin_amdgcn_readlane(n, s);
+        rows = __builtin_amdgcn_readlane(had, s);
+        in_sequence = x - base;
+        if (g.sorted) in_sequence += first_seeing<QT>(g, rows, tokens, (int64_t)level * 64);
     } else if (!g.p.starts && g.extra == 0) {
         const uint32_t tiles = tiles_of<QT>(g, 1);
         s = (int32_t)(x / tiles);
@@ -177,10 +216,15 @@ __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundIt
         }
     }
     s = __builtin_amdgcn_readfirstlane(s);
+    if (first_token < 0) {
+        first_token = start_of(g.p, s);
+        tokens = max(start_of(g.p, s + 1) - first_token, 0);
+        rows = rows_of(g.p, s);
+    }
     b.sequence = s;
-    b.first_token = start_of(g.p, s);
-    b.tokens = max(start_of(g.p, s + 1) - b.first_token, 0);
-    b.rows = rows_of(g.p, s);
+    b.first_token = first_token;
+    b.tokens = tokens;
+    b.rows = rows;
     const int32_t all = (int32_t)min((int64_t)b.rows + b.tokens, (int64_t)g.p.capacity);
     b.parts = g.extra ? max(((uint32_t)all + (uint32_t)chunk - 1u) / (uint32_t)chunk, 1u) : 1u;
     b.tile = (int32_t)(in_sequence / b.parts);

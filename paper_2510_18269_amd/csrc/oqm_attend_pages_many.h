@@ -3,15 +3,15 @@
 // A workgroup has 32 query rows of a KV head for each of its NW waves, and its waves share staged tiles of KT rows, two in LDS: the next one is on its way (from
 // memory into LDS past the registers) while a tile is worked on.  S^T = K Q^T in products of 32 x 32 x 16 leaves a lane, for one query row, the scores of 4 of
 // each 8 rows; they become the operand of O^T = V^T P^T where they are, if V^T's rows are taken in the same order, which the transposing LDS read does.
-// Probabilities enter as one part of the type, off by half a step of it each (2^-9 in bfloat16, 2^-12 in binary16): their error is no larger than that of the output's own
+// Probabilities enter as one part of the type, off by half a step of it each (2^-8 in bfloat16, 2^-11 in binary16): their error is no larger than that of the output's own
 // rounding, and a second part would make the products of V twice as many.  Their sum is of the unrounded ones.
 //
 // In LDS a row lies as in memory, but its pieces of 16 bytes are exchanged by row, so that the lanes of a read, which differ in the row, do not meet in a bank.
 //
 // What bounds it.  28 query heads on 4, 128 channels: a prompt of 8192 tokens 481 to 502 us on different cards, 980 TFLOP/s where a product of 8192^3 reaches 1180 to 1407.  With
 // a part of the work left out: half of the products of K 134 us less, half of those of V 78, the staging 46, the exponentials 16, the reads of V 30, so it is the
-// matrix cores first.  Three prompts of 1467 to 1994 tokens 371 us: their 560 workgroups do not divide evenly by 256 compute units.  4 drafts of 43 to 52
-// tokens over 2000 to 7900 rows 37.3: 4.5 to find the part, 5.3 to the end of its first tile, 17.4 the others (16), 3.7 to write it, 7 to join; more tiles in LDS change nothing.
+// matrix cores first.  Three prompts of 1467 to 1994 tokens 360 us: their 560 workgroups do not divide evenly by 256 compute units.  4 drafts of 43 to 52
+// tokens over 2000 to 7900 rows 35.9: 3 to find the part, 5.3 to the end of its first tile, 17.4 the others (16), 3.7 to write it, 7 to join; more tiles in LDS change nothing.
 #pragma once
 
 #include "oqm_attend_pages_device.h"
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
     for (int32_t from = b.begin; from < b.end; from += F::PLACES) {
         const int32_t tiles = (min(b.end - from, F::PLACES) + KT - 1) / KT;
         if (from > b.begin) __syncthreads();  // the tiles and places before have been read
-        // Places are looked up at once, not on the way (where the division by a page's rows is a twelfth of a prompt's time: 380 us, 371 so); the first tile sets out with its
+        // Places are looked up at once, not on the way (prompts of 1467 to 1994 tokens 380 us, 371 so); the first tile sets out with its
         // own entries, and they are written while it is on its way.
         constexpr int kFirst = 4;
         int32_t pages[kFirst];

@@ -360,3 +360,57 @@ def test_a_step_of_drafts_over_stored_frames(oqm):
             assert (lse[:, s] - total).abs().max() < 2.0 ** -6
     for mem in memories:
         mem.close()
+
+
+@pytest.mark.parametrize("new", [[3, 1, 2], [40, 9, 30]])
+def test_a_captured_step_follows_parents_starts_rows_and_tables(oqm, new):
+    """Tree, rows appended, attention and kept rows as one graph, replayed for other conversations with eager work between: as the eager calls, bit for bit."""
+    b = Batch(rows=[70, 0, 333], new=new, d=64, heads=2, repeat=3, page_rows=16, spare=30)
+    t, T, H, Hq = DTYPE[b.dtype], b.T, 2, 6
+    g = torch.Generator().manual_seed(3)
+    base = b.pages(oqm)
+    k0, v0, rows, starts, table = base.k.clone(), base.v.clone(), base.rows, base.starts, base.table
+    k0.nan_to_num_(0.5), v0.nan_to_num_(0.5)
+    x = torch.randn((T, Hq + 2 * H, 64), generator=g).to(t).cuda()
+    parents, first = torch.zeros(T, dtype=torch.int32, device="cuda"), ints([100, 2000, 30], torch.int64)
+    mask, positions = torch.zeros((T, 1), dtype=torch.int64, device="cuda"), torch.zeros(T, dtype=torch.int64, device="cuda")
+    q_out, out, lse = torch.zeros((T, Hq, 64), dtype=t, device="cuda"), torch.zeros((T, Hq, 64), dtype=t, device="cuda"), torch.zeros((Hq, T), device="cuda")
+    idx, counts = ints([[0, 2, 5], [0, 1, 2], [1, 3, 29]]), ints([2, 1, 2])
+    ws = torch.empty(oqm.tom_oqm_attend_pages_workspace_bytes(base, T, Hq), dtype=torch.uint8, device="cuda")
+    rotary = oqm.Rotary.create(64)
+
+    def step():
+        oqm.tom_oqm_draft_tree(parents, starts, mask, positions, first)
+        for layer in range(b.layers):
+            oqm.tom_oqm_append_rows(base, layer, rotary, positions, x[:, Hq:Hq + H], x[:, Hq + H:], q=x[:, :Hq], q_out=q_out)
+            oqm.tom_oqm_attend_pages(base, layer, q_out.transpose(0, 1), out.transpose(0, 1), mask=mask, lse=lse, workspace=ws)
+        oqm.tom_oqm_keep_rows(base, idx, counts, rows)
+
+    def load(turn):
+        base.k.copy_(k0), base.v.copy_(v0)
+        shift = min(turn, 2)
+        starts.copy_(torch.tensor([max(0, s - shift) for s in b.starts_list], dtype=torch.int32))
+        rows.copy_(torch.tensor([max(0, r - 13 * turn) for r in b.rows], dtype=torch.int32))
+        table.copy_(torch.tensor(b.table_list, dtype=torch.int32).reshape(table.shape).roll(turn % 2, 0))
+        parents.copy_(torch.tensor(paged.tree(new, 5 + turn), dtype=torch.int32))
+        for y in (mask, positions, q_out, out, lse):
+            y.zero_()
+        ws.fill_(255)
+
+    results = lambda: [y.clone() for y in (mask, positions, q_out, out, lse, base.k, base.v, rows)]  # noqa: E731
+    load(0)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in (0, 1, 3, 0, 2):
+        load(turn)
+        step()
+        want = results()
+        load(turn)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, y in zip(results(), want):
+            assert torch.equal(got, y)
+    assert torch.isfinite(out).all() and (mask[:starts[-1]] != 0).any()
