@@ -8,10 +8,10 @@
 //
 // In LDS a row lies as in memory, but its pieces of 16 bytes are exchanged by row, so that the lanes of a read, which differ in the row, do not meet in a bank.
 //
-// What bounds it.  28 query heads on 4, 128 channels: a prompt of 8192 tokens 481 to 502 us on different cards, 980 TFLOP/s where a product of 8192^3 reaches 1180 to 1407.  With
+// What bounds it.  28 query heads on 4, 128 channels: a prompt of 8192 tokens 479 to 502 us on different cards, 960 to 1000 TFLOP/s where a product of 8192^3 reaches 1180 to 1407.  With
 // a part of the work left out: half of the products of K 134 us less, half of those of V 78, the staging 46, the exponentials 16, the reads of V 30, so it is the
-// matrix cores first.  Three prompts of 1467 to 1994 tokens 360 us: their 560 workgroups do not divide evenly by 256 compute units.  4 drafts of 43 to 52
-// tokens over 2000 to 7900 rows 35.9: 3 to find the part, 5.3 to the end of its first tile, 17.4 the others (16), 3.7 to write it, 7 to join; more tiles in LDS change nothing.
+// matrix cores first.  Three prompts of 1467 to 1994 tokens 354 to 363 us: their 560 workgroups do not divide evenly by 256 compute units.  4 drafts of 43 to 52
+// tokens over 2000 to 7900 rows 35.3: 3 to find the part, 5.3 to the end of its first tile, 17.4 the others (16), 3.7 to write it, 7 to join; more tiles in LDS change nothing.
 #pragma once
 
 #include "oqm_attend_pages_device.h"
@@ -55,6 +55,7 @@ struct PagedTiles {
     static constexpr int ROW = DP * 2, CPR = ROW / 16, PART = KT * ROW, STAGE = 2 * PART;  // bytes; pieces of a row
     static constexpr int STEPS = DP / 16, NB = DP / 32;
     static constexpr int LOADS = KT * CPR / 64 / NW;  // of a wave, of K and of V
+    static constexpr int WAVES = DP == 256 ? 1 : DP == 64 && NW < 8 ? 3 : 2;  // a SIMD, as many as their registers leave (64 channels of prompts, us, 2 / 3: 234 / 211)
     static constexpr int PLACES = NW == 8 ? 4096 : 1024;  // rows whose places are looked up at a time
 
     f32x16 o[NB];
@@ -230,7 +231,7 @@ struct PagedTiles {
 };
 
 template <typename F>
-__global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages_many_kernel(PagesArgs g) {
+__global__ __launch_bounds__(F::THREADS, F::WAVES) void attend_pages_many_kernel(PagesArgs g) {
     typedef typename F::T T;
     constexpr int KT = F::KT, QT = F::QT, STEPS = F::STEPS, NB = F::NB;
     __shared__ FoundItem found;
@@ -243,8 +244,8 @@ __global__ __launch_bounds__(F::THREADS, F::DP == 256 ? 1 : 2) void attend_pages
     tell_unit<QT>(g, b, x, head);
     const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     // Half of the waves go first, so that a SIMD's do not all want the matrix cores, and then the vector unit, at the same time.  Prompts of 1467 to 1994 tokens, us, without /
-    // with: 64 channels 233 / 216, 128 372 / 371, 256 1415 / 1199.
-    if (wave >= F::NW / 2) __builtin_amdgcn_s_setprio(1);
+    // with: 64 channels 223 / 211, 128 and 256 the same; 4 drafts in halves of tiles 35.2 / 35.8.
+    if (!F::SPLIT && wave >= F::NW / 2) __builtin_amdgcn_s_setprio(1);
     const int lane = (int)__lane_id(), half = lane >> 5;
     const int side = F::SPLIT ? wave / (F::NW / 2) : 0, row_wave = F::SPLIT ? wave % (F::NW / 2) : wave;
 
