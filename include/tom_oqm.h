@@ -522,8 +522,9 @@ size_t tom_oqm_attend_pages_workspace_bytes(const tom_oqm_pages_t* pages, int32_
  *   else if causal    those up to itself,
  *   else              all.
  * Query head i reads head i / (H_q / heads).  Scores, softmax and sums are float32.  Probabilities enter the products with 16-bit values as
- * two 16-bit parts (2^-17 of each; binary16 2^-23 of each, or 2^-39 of the largest) where the sequences have up to 16 query rows of a KV head on average, and
- * as one (off by 2^-8 of each at most; binary16 2^-11 of each, or 2^-39 of the largest) where they have more.
+ * two 16-bit parts (2^-17 of each; binary16 2^-23 of each, or 2^-39 of the largest) where the sequences have up to 16 query rows of a KV head on average
+ * (tokens * (H_q / heads) <= 16 * sequences, in whole numbers), and as one (off by 2^-8 of each at most; binary16 2^-11 of each, or 2^-39 of the largest) where
+ * they have more: for all of a call's sequences alike, so what a token gets has the bits that its call's average gives it.
  *   q, out     [H_q][tokens][channels] of the pages' dtype, any strides that are multiples of 16 bytes; out overlaps nothing
  *              that is read, but may be prior_out itself, with the same strides
  *   mask       device int64 [tokens][words] or NULL, words >= 1; tokens from number 64 * words on are seen by nobody

@@ -53,10 +53,11 @@ inline uint64_t pages_units(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_
 // rows 51 / 61 / 61 / 63, 64 channels 349 / 374 / 354 / 335, 256 channels 355 / 336 / 324 / 320.  64 rows, 512 / 640 / 768: 16 sequences, 8 tokens 49.9 / 48.2 / 48.3, 4 tokens 38.1 / 37.5 /
 // 39.5.
 inline PagesForm pages_form(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads) {
-    const int64_t rows = ((int64_t)tokens + g.sequences - 1) / (g.sequences > 0 ? g.sequences : 1) * (n_q_heads / g.heads);
-    if (g.dtype == TOM_F32 || rows <= 16) return {16, 128, 1536, false};
-    if (rows <= 64) return {64, 256, 640, false};
-    if (rows > 1024 && g.channels > 64 && g.channels <= 128) return {256, 256, 256, false};
+    const int64_t rows = (int64_t)tokens * (n_q_heads / g.heads);
+    auto on_average = [&](int64_t most) { return rows <= most * g.sequences; };  // not rounded: a token more in a batch must not move all of it to fewer bits
+    if (g.dtype == TOM_F32 || on_average(16)) return {16, 128, 1536, false};
+    if (on_average(64)) return {64, 256, 640, false};
+    if (!on_average(1024) && g.channels > 64 && g.channels <= 128) return {256, 256, 256, false};
     if (g.channels <= 128 && pages_units(g, tokens, n_q_heads, 128) * (uint64_t)g.heads < 512) return {128, 256, 256, true};
     return {128, 256, 512, false};
 }
