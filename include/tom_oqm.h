@@ -549,7 +549,7 @@ tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, c
 
 /*
  * Keeps accepted tokens of a draft and drops the others: row rows[s] + idx[s][i] moves to row rows[s] + i, i < counts[s], K and V of all
- * layers, in place.  The sequence then has rows_out[s] = rows[s] + counts[s] rows.
+ * layers, in place.  The sequence then has rows_out[s] = rows[s] + counts[s] rows, those behind its table's end counted too (2^31 - 1 at most).
  *   idx       device int32 [sequences][width], strictly ascending as far as counts[s]: numbers of the sequence's tokens in the call that
  *             appended them.  An index outside [i, the sequence's tokens) leaves row i as it is (any order that is not ascending leaves
  *             unspecified rows).

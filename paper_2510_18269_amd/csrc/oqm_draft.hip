@@ -95,12 +95,16 @@ struct KeepArgs {
 // later batches read: in place without a second copy, and no lane touches another's column.  64 sequences of up to 12 kept rows in 28 layers (44 MB), us: every row
 // looked up on the way by the wave 15.9, as it is 8.5.
 constexpr int kAhead = 8;
+// How many rows a sequence then has: all that it had count, those behind the table's end too.
+__device__ __forceinline__ int32_t rows_kept(const KeepArgs& g, int32_t s) {
+    return (int32_t)min((int64_t)max(g.p.rows[s], 0) + min(max(g.counts[s], 0), g.width), (int64_t)0x7fffffff);
+}
 __global__ __launch_bounds__(kBlock) void keep_rows_kernel(KeepArgs g) {
     __shared__ uint32_t source_of[kBlock], to_of[kBlock];
     const uint32_t s = div_by(blockIdx.x, g.blocks_per_sequence, g.inv_blocks), block = blockIdx.x - s * g.blocks_per_sequence;
     const uint32_t i = block * kBlock + threadIdx.x, plane = div_by(i, g.cols, g.inv_cols), col = i - plane * g.cols;
     const int32_t rows = rows_of(g.p, (int32_t)s), count = min(max(g.counts[s], 0), g.width);
-    if (g.rows_out && i == 0) g.rows_out[s] = rows + count;
+    if (g.rows_out && i == 0) g.rows_out[s] = rows_kept(g, (int32_t)s);
     const int32_t own = start_of(g.p, (int32_t)s + 1) - start_of(g.p, (int32_t)s);
     const uint32_t layer_head = plane >> 1, layer = div_by(layer_head, (uint32_t)g.heads, g.inv_heads), head = layer_head - layer * (uint32_t)g.heads;
     char* const base = ((plane & 1) ? g.v : g.k) + layer * g.layer_bytes + head * g.p.head_bytes + (int64_t)col * 16;
@@ -138,7 +142,7 @@ __global__ __launch_bounds__(kBlock) void keep_rows_kernel(KeepArgs g) {
 }
 __global__ __launch_bounds__(kBlock) void kept_rows_kernel(KeepArgs g, int32_t* rows_out) {
     const uint32_t s = blockIdx.x * kBlock + threadIdx.x;
-    if (s < (uint32_t)g.p.sequences) rows_out[s] = rows_of(g.p, (int32_t)s) + min(max(g.counts[s], 0), g.width);
+    if (s < (uint32_t)g.p.sequences) rows_out[s] = rows_kept(g, (int32_t)s);
 }
 
 }  // namespace oqm
