@@ -418,7 +418,7 @@ size_t tom_oqm_attend_workspace_bytes(const tom_oqm_t* h, int32_t t_q, int64_t r
  *              Keys that a token does not see may hold anything.  A value that is not finite, in a row that some
  *              of the tokens see, is unspecified for those too that see none of the row.  No row behind the last
  *              of a view is read.
- *   scale      a number below 2^50, and below 2^50 times the cap
+ *   scale      a number whose size is below 2^50, or below 2^50 times the cap where there is one
  *   softcap    0: none; above 2^40 none either, below 2^-30 every score is zero
  *   lse        device float32 [H_q][t_q] or NULL: the natural logarithm of the sum of exp(w_j).  Where a token sees
  *              nothing its output is 0 and its lse -inf.
@@ -528,7 +528,7 @@ size_t tom_oqm_attend_pages_workspace_bytes(const tom_oqm_pages_t* pages, int32_
  *   q, out     [H_q][tokens][channels] of the pages' dtype, any strides that are multiples of 16 bytes; out overlaps nothing
  *              that is read, but may be prior_out itself, with the same strides
  *   mask       device int64 [tokens][words] or NULL, words >= 1; tokens from number 64 * words on are seen by nobody
- *   scale      a number below 2^50, and below 2^50 times the cap
+ *   scale      a number whose size is below 2^50, or below 2^50 times the cap where there is one
  *   softcap    0: none; above 2^40 none either, below 2^-30 every score is zero
  *   prior_out, prior_lse   [H_q][tokens][channels] and [H_q][tokens][1], both or neither: softmax-weighted values over other rows, as
  *              tom_oqm_attend gives them over stored groups, and the natural logarithm of their sum of exponentials (-inf: nothing,
@@ -556,8 +556,8 @@ tom_status_t tom_oqm_attend_pages(const tom_oqm_pages_t* pages, int32_t layer, c
  *   counts    device int32 [sequences], cut to [0, width]
  *   rows_out  device int32 [sequences]; may be pages->rows itself (a second launch then writes it), and otherwise overlaps nothing that is read
  * A page that rows move to stands in one sequence's table, and there once.
- * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 sequences, or more 16-byte columns, sequences * layers * heads * 2 * channels / 8, than the
- * 2^32 - 1 lanes of a launch), HIP.  No sequences: a no-op.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 sequences; more 16-byte columns of a row, layers * heads * 2 * channels * element size / 16, than
+ * 2^31 - 1; or these, rounded up to 256, times the sequences above the 2^32 - 1 lanes of a launch), HIP.  No sequences: a no-op.
  */
 tom_status_t tom_oqm_keep_rows(const tom_oqm_pages_t* pages, const int32_t* idx_device, int32_t width, const int32_t* counts_device,
                                int32_t* rows_out_device, void* hip_stream);

@@ -1,0 +1,23 @@
+"""How much of a kind the calls on pages take, as the header counts it (no GPU is touched: every call here is refused)."""
+import pytest
+
+from tests.test_operator_refusals import Fake, refuses
+from tests.test_pages_refusals import I32, keeps, oqm, pages  # noqa: F401
+
+
+@pytest.mark.parametrize("dtype,channels,heads", [("f32", 256, 32), ("f32", 8, 1024), ("bf16", 256, 64), ("f16", 8, 2048)])
+def test_columns_of_kept_rows_go_by_the_element_size(oqm, dtype, channels, heads):  # noqa: F811
+    """2^12 columns of 16 bytes a row, in 2^20 sequences: a lane more than a launch has.  In float32 that is half as many channels as in 16 bits."""
+    n, e = 2 ** 20, 4 if dtype == "f32" else 2
+    assert heads * 2 * channels * e // 16 == 2 ** 12
+    p = pages(oqm, dtype={"f32": oqm.TOM_F32, "bf16": oqm.TOM_BF16, "f16": oqm.TOM_F16}[dtype], channels=channels, heads=heads, n_layers=1, n_pages=2, page_rows=1,
+              row_stride=channels, head_stride=channels, page_stride=heads * channels, layer_stride=2 * heads * channels, sequences=n, table_pages=1)
+    refuses(oqm, "lanes", keeps(oqm, p), oqm.TOM_ERR_UNSUPPORTED)
+
+
+def test_columns_of_a_row(oqm):  # noqa: F811
+    """2^31 of them, of one sequence."""
+    heads, layers = 2 ** 14, 2 ** 12
+    p = pages(oqm, dtype=oqm.TOM_F32, channels=64, heads=heads, n_layers=layers, n_pages=1, page_rows=1, row_stride=64, head_stride=64, page_stride=heads * 64,
+              layer_stride=heads * 64, sequences=1, table_pages=1)
+    refuses(oqm, "pieces", keeps(oqm, p, Fake((1, 3), I32), Fake((1,), I32), Fake((1,), I32)), oqm.TOM_ERR_UNSUPPORTED)
