@@ -320,7 +320,8 @@ __device__ __forceinline__ void put_channels(const PagesArgs& g, int32_t q_head,
     typedef typename Element<T>::type E;
     typedef E Vec __attribute__((ext_vector_type(4)));
     sum *= end.mine;
-    if (end.theirs != 0.0f) {
+    // Whether there is a prior is asked of the call, not of the weight: without one that is 0 * (1 / total), and no number where the total is none.
+    if (g.prior_out && end.theirs != 0.0f) {
         const Vec x = *reinterpret_cast<const Vec*>(g.prior_out + q_head * g.prior_head + token * g.prior_row + (int64_t)c * sizeof(E));
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(end.theirs, (float)x[i], sum[i]);
