@@ -9,6 +9,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <functional>
+#include <map>
 #include <vector>
 
 #define __device__
@@ -28,7 +29,6 @@ typedef int hipError_t;
 constexpr int hipSuccess = 0;
 inline int hipGetLastError() { return 0; }
 inline const char* hipGetErrorString(int) { return ""; }
-inline int hipLaunchKernel(const void*, dim3, dim3, void**, size_t, hipStream_t) { return 0; }
 
 namespace lanes {
 
@@ -71,7 +71,7 @@ inline std::vector<Lane> all;
 inline std::vector<Wave> waves;
 inline Lane* cur = nullptr;
 inline void* scheduler = nullptr;
-inline dim3 block_index, block_dim;
+inline dim3 block_index, block_dim, grid_dim;
 inline int at_barrier = 0, alive = 0;
 inline uint64_t barrier_turn = 0;
 inline std::function<void()> body;
@@ -153,11 +153,35 @@ T value(uint64_t b) {
     return v;
 }
 
+// Kernels that a launch by their address runs.
+inline std::map<const void*, std::function<void(void**)>> kernels;
+template <typename A>
+void runs(void (*kernel)(A)) {
+    kernels[reinterpret_cast<const void*>(kernel)] = [kernel](void** list) { kernel(*static_cast<A*>(list[0])); };
+}
+template <typename A, typename B>
+void runs(void (*kernel)(A, B)) {
+    kernels[reinterpret_cast<const void*>(kernel)] = [kernel](void** list) { kernel(*static_cast<A*>(list[0]), *static_cast<B*>(list[1])); };
+}
+
 }  // namespace lanes
+
+inline int hipLaunchKernel(const void* kernel, dim3 grid, dim3 block, void** list, size_t, hipStream_t) {
+    const auto found = lanes::kernels.find(kernel);
+    if (found == lanes::kernels.end()) std::abort();
+    lanes::grid_dim = grid;
+    for (uint32_t y = 0; y < grid.y; ++y)
+        for (uint32_t x = 0; x < grid.x; ++x) {
+            lanes::block_index = dim3(x, y);
+            lanes::run_block((int)block.x, [&] { found->second(list); });
+        }
+    return 0;
+}
 
 #define threadIdx (lanes::cur->tid)
 #define blockIdx (lanes::block_index)
 #define blockDim (lanes::block_dim)
+#define gridDim (lanes::grid_dim)
 
 inline int __lane_id() { return lanes::index() % 64; }
 inline void __syncthreads() { lanes::barrier(); }
@@ -208,6 +232,7 @@ inline uint32_t __builtin_amdgcn_perm(uint32_t hi, uint32_t lo, uint32_t select)
 #define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, ...) (c)
 inline uint32_t __float_as_uint(float f) { return lanes::value<uint32_t>(lanes::bits(f)); }
 inline int __float_as_int(float f) { return lanes::value<int>(lanes::bits(f)); }
+inline int __popcll(uint64_t x) { return __builtin_popcountll(x); }
 inline float __uint_as_float(uint32_t u) { return lanes::value<float>(u); }
 inline float __int_as_float(int u) { return lanes::value<float>((uint32_t)u); }
 inline uint32_t __umulhi(uint32_t a, uint32_t b) { return (uint32_t)((uint64_t)a * b >> 32); }
