@@ -376,6 +376,7 @@ class Pages:
         assert k.stride(4) == 1 and v.stride(4) == 1, "contiguous channel axis expected"
         assert all(n == 1 or a == b for n, a, b in zip(k.shape, k.stride(), v.stride())), "k and v must have the same strides"
         assert table.dim() == 2, "table: [sequences][table_pages]"
+        assert max(*k.shape, *table.shape) < 2 ** 31, "sizes of the pages and of the table must be below 2^31"  # the structure would keep their low bits
         sequences = table.shape[0]
         for name, t, n in (("table", table, table.numel()), ("rows", rows, sequences), ("starts", starts, sequences + 1)):
             if t is None and name == "starts":
@@ -391,6 +392,7 @@ def tom_oqm_draft_tree(parents, starts, mask, positions=None, first=None, stream
     """parents int32 [tokens], starts int32 [sequences + 1] or None (one token each) -> mask int64 [tokens][words], positions int64 [tokens]
     counted from first, int64 [sequences] or None (zeros)."""
     tokens = parents.numel()
+    assert tokens < 2 ** 31 and (starts is None or starts.numel() <= 2 ** 31), "fewer than 2^31 tokens and sequences expected"
     _native.draft_tree(parents, tokens, starts, tokens if starts is None else starts.numel() - 1, mask, first, positions, stream)
 
 
@@ -416,6 +418,7 @@ def tom_oqm_attend_pages(pages: Pages, layer: int, q, out, mask=None, causal: bo
 def tom_oqm_keep_rows(pages: Pages, idx, counts, rows_out, stream=None) -> None:
     """The rows idx[s][0 .. counts[s]) (int32 [sequences][width], ascending) of the call's tokens move together behind their sequences; rows_out
     (int32 [sequences], may be pages.rows) is how many rows each then has."""
+    assert idx.shape[1] < 2 ** 31, "idx: fewer than 2^31 columns expected"
     _native.keep_rows(C.addressof(pages.config), pages.config.sequences, idx, idx.shape[1], counts, rows_out, stream)
 
 
