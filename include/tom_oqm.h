@@ -538,7 +538,9 @@ size_t tom_oqm_attend_pages_workspace_bytes(const tom_oqm_pages_t* pages, int32_
  *              sees nothing its output is 0 and its lse -inf.  lse may be prior_lse itself.
  *   workspace  device, 16-byte aligned, tom_oqm_attend_pages_workspace_bytes(...) bytes; calls that may overlap need separate ones
  * A row that a token does not see has no part in what it gets, whatever the row holds; what a token that sees a row with
- * a value that is not finite gets is unspecified.
+ * a value that is not finite, or whose products with a row pass float32's range, gets is unspecified.
+ * One kernel is chosen for all of a call's sequences, by their average, and where they are many none is cut over several workgroups of a KV head: long
+ * prompts beside single tokens, or a sequence of very many rows beside hundreds of short ones, are faster in calls of their own.
  * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 tokens or sequences, table_pages * page_rows above 2^31 - 4097, H_q * tokens of 2^30 and
  * more, a layer's pages that span 2^36 bytes and more), HIP.  No tokens: a no-op.
  */

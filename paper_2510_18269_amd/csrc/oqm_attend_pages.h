@@ -49,6 +49,8 @@ inline uint64_t pages_units(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_
 //      128 / 256:      4 sequences of 2000 to 7900 rows, 43 to 52 tokens (301 to 364) 39.4 / 50.9; 3 prompts of 1467 to 1994 tokens 386 / 371, one of 8192 532 / 483, but of 64
 //                      channels 216 / 255.  Of 256 channels 256 rows would leave half the registers.
 //      128, SPLIT:     43 to 52 tokens 41.5 / 37.6: half as many parts to write and join
+// All of these are batches whose sequences are alike.  One form for all of a call costs those that are not: 63 tokens over 1000 to 30000 rows 435 us, a prompt of 4000 tokens 187, in one call
+// 994 (256 rows a workgroup, of which a token has 7); in a call each they take the sum.
 // Workgroups, us: few form, 512 / 768 / 1024 / 1536: 48 sequences of 40 to 30000 rows, a token each, 355 / 296 / 299 / 290, one of 705 K rows 259 / 297 / 265 / 271, 256 of 40 to 1000
 // rows 51 / 61 / 61 / 63, 64 channels 349 / 374 / 354 / 335, 256 channels 355 / 336 / 324 / 320.  64 rows, 512 / 640 / 768: 16 sequences, 8 tokens 49.9 / 48.2 / 48.3, 4 tokens 38.1 / 37.5 /
 // 39.5.
@@ -70,7 +72,9 @@ struct PagesCuts {
     uint32_t items, extra;
     uint64_t units;
 };
-// Items of a KV head: its blocks, and further ones that let long sequences be cut where the blocks do not fill the chip.
+// Items of a KV head: its blocks, and further ones that let long sequences be cut where the blocks do not fill the chip.  Where they do, by their number, nothing is cut, and a
+// sequence far longer than the others is read by one workgroup a KV head alone: 799 tokens over 40 to 600 rows each 120 us, with an 800th over 30000 rows 798, over 700 K rows 16.9 ms
+// (alone, cut over the chip, 260 us).  Such a sequence is better given a call of its own.
 inline PagesCuts pages_cuts(const tom_oqm_pages_t& g, int32_t tokens, int32_t n_q_heads, const PagesForm& f) {
     const uint64_t units = pages_units(g, tokens, n_q_heads, f.block_rows);
     const uint64_t most = (uint64_t)f.target / (uint64_t)g.heads;

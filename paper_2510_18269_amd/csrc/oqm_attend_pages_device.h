@@ -51,7 +51,7 @@ __device__ __forceinline__ uint32_t first_seeing(const PagesArgs& g, int32_t row
 
 // The same in every lane of the workgroup; false: there is nothing for it.
 // All workgroups look at all sequences: a sum over them says how long a part is (so that a long sequence among short ones is cut and they are not), a second
-// one where each one's items begin; the host knows none of the lengths.
+// one where each one's items begin; the host knows none of the lengths.  A call without parts (pages_cuts) cuts no sequence, however long one is among the others.
 template <int QT, int KT, int THREADS>
 __device__ __forceinline__ bool block_of(const PagesArgs& g, uint32_t x, FoundItem& found, Block& b) {
     const int32_t sequences = g.p.sequences;

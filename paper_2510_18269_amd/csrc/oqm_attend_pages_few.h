@@ -2,10 +2,11 @@
 //
 // Memory bounds it: K and V are read once, straight into the operands of the matrix cores, no LDS and no barrier on the way.  S^T = K Q^T leaves a lane, for one
 // query row, the scores of the very rows whose values it feeds to O^T = V^T P^T.  A workgroup has 16 query rows of a KV head; its four waves take the part's tiles
-// of 32 rows in turn, each with sums of its own, and join them in LDS.  What hides memory's latency is the waves of a SIMD: as many as fit without spilling.
+// of 32 rows in turn, each with sums of its own, and join them in LDS.  What hides memory's latency is the waves of a SIMD: as many as fit with no more than
+// four vector registers spilled (1 or 2 in 16 bits of 128 channels, 2 or 3 in float32 of 64, 4 of 256; at 16 bits of 256 channels some 300 scalar ones, into lanes of vector registers).
 //
-// 28 query heads on 4 of 128 channels, bfloat16, both launches: 48 sequences of 40 to 30000 rows, a token each, 253 to 290 us on different cards, 5.1 TB/s on the same as
-// a copy's 4.96; one of 705 K rows 258 us (5.6 TB/s), of 12.6 K rows 13.3, of 500 rows 9.9, where the way from starts to table to rows to the join is what is left.
+// 28 query heads on 4 of 128 channels, bfloat16, both launches: 48 sequences of 40 to 30000 rows, a token each, 257 us (253 to 290 on different cards), 4.9 TB/s, where on the same card
+// a copy reaches 4.98 and bare reads 6.76; one of 705 K rows 261 us (5.5 TB/s), of 12.6 K rows 13.1, of 500 rows 9.6, where the way from starts to table to rows to the join is what is left.
 // Loads past the caches 337 us against 291.
 #pragma once
 
@@ -20,7 +21,7 @@ struct PagedRows : Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> {
     typedef Sums<T_, DP_, (DP_ < 128 ? DP_ : 128), 1, 1, SERIES> S;
     using S::GS, S::VU, S::VN, S::STEPS, S::o;
     static constexpr int DP = DP_, E = elem_bytes<T>::value, KW = 8 * E / 16;  // KW: loads of 16 bytes of 8 channels
-    static constexpr int WAVES = DP == 256 ? 1 : DP == 128 ? (E == 4 ? 2 : 3) : 4;                  // a SIMD: as many as their registers leave without spilling
+    static constexpr int WAVES = DP == 256 ? 1 : DP == 128 ? (E == 4 ? 2 : 3) : 4;                  // a SIMD: as many as their registers leave, see above
     static constexpr int VW = VU * E / 4;                                      // words of a value piece
     typedef uint32_t Piece __attribute__((ext_vector_type(VW)));
     bool sees_odd;

@@ -55,7 +55,7 @@ struct PagedTiles {
     static constexpr int ROW = DP * 2, CPR = ROW / 16, PART = KT * ROW, STAGE = 2 * PART;  // bytes; pieces of a row
     static constexpr int STEPS = DP / 16, NB = DP / 32;
     static constexpr int LOADS = KT * CPR / 64 / NW;  // of a wave, of K and of V
-    static constexpr int WAVES = DP == 256 ? 1 : DP == 64 && NW < 8 ? 3 : 2;  // a SIMD, as many as their registers leave (64 channels of prompts, us, 2 / 3: 234 / 211)
+    static constexpr int WAVES = DP == 256 ? 1 : DP == 64 && NW < 8 ? 3 : 2;  // a SIMD, as many as their registers leave (two spilled at 128 channels and NW = 4; 64 channels of prompts, us, 2 / 3: 234 / 211)
     static constexpr int PLACES = NW == 8 ? 4096 : 1024;  // rows whose places are looked up at a time
 
     f32x16 o[NB];

@@ -15,7 +15,8 @@ struct TreeArgs {
 // A token's ancestors are looked for 64 tokens at a time.  A wave closes its 64 among themselves: with each token's own bit and its parent's number (its own where that
 // lies further back), six rounds of "take the ancestor's bits, then its ancestor" reach all.  What is left is a walk over the token's blocks, a word each: the bits of where it stands, then the parent
 // of the highest of them, which lies in an earlier block.  96 drafts of 5 to 200 tokens, us: a walk of a token at a time, some 45 dependent reads, 10.5; by blocks 3.3.
-// Tokens that have no mask bit for themselves, from 4096 on, walk a token at a time until they come to those that do.
+// Tokens that have no mask bit for themselves, from 4096 on, walk a token at a time until they come to those that do: a chain of 65536 takes 54 ms with 64 words, by
+// 16 workgroups, and 0.81 s with up to 4, by one.
 constexpr int kTreeBlock = 256, kStaged = 4096, kMostDrafted = 1 << 16;
 __global__ __launch_bounds__(kTreeBlock) void draft_tree_kernel(TreeArgs g) {
     __shared__ uint64_t bits_of[kStaged];
