@@ -8,9 +8,9 @@
 //
 // In LDS a row lies as in memory, but its pieces of 16 bytes are exchanged by row, so that the lanes of a read, which differ in the row, do not meet in a bank.
 //
-// What bounds it.  28 query heads on 4, 128 channels: a prompt of 8192 tokens 479 to 502 us on different cards, 960 to 1000 TFLOP/s where a product of 8192^3 reaches 1180 to 1407.  With
+// What bounds it.  28 query heads on 4, 128 channels: a prompt of 8192 tokens 472 to 502 us on different cards, 960 to 1020 TFLOP/s where a product of 8192^3 reaches 1180 to 1419.  With
 // a part of the work left out: half of the products of K 134 us less, half of those of V 78, the staging 46, the exponentials 16, the reads of V 30, so it is the
-// matrix cores first.  Three prompts of 1467 to 1994 tokens 354 to 363 us: their 560 workgroups do not divide evenly by 256 compute units.  4 drafts of 43 to 52
+// matrix cores first.  Three prompts of 1467 to 1994 tokens 348 to 363 us: their 560 workgroups do not divide evenly by 256 compute units.  4 drafts of 43 to 52
 // tokens over 2000 to 7900 rows 35.3: 3 to find the part, 5.3 to the end of its first tile, 17.4 the others (16), 3.7 to write it, 7 to join; more tiles in LDS change nothing.
 #pragma once
 
