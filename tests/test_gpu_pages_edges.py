@@ -207,3 +207,55 @@ def test_every_cut_repeats_itself_bit_for_bit(oqm, cut, dtype):  # noqa: F811
     for _ in range(5):
         again = pages_tests.call(oqm, b, pages, prior=prior, softcap=3.0)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+# ---- products that pass float32's range, and tables of no pages ------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cut", ["a few", "up to 64", "halved tiles", "prompts", "one each"])
+def test_a_token_whose_products_pass_the_range_leaves_the_others_alone(oqm, cut, dtype):  # noqa: F811
+    """The first token of each sequence has queries of 1e37: scores pass float32's range, or come near it, and there is no prior."""
+    heads, repeat, rows, new, one_each = CUTS[cut]
+    b = Batch(dtype=dtype, d=64, heads=heads, repeat=repeat, rows=rows, new=new, layers=1, layer=0, one_each=one_each)
+    for s in range(0, b.B, 2 if one_each else 1):
+        if new[s] > (0 if one_each else 1):
+            b.q[:, b.starts_list[s]] = 1e37 * torch.sign(b.q[:, b.starts_list[s]].float()).to(b.q.dtype)
+    keep = b.q.float().abs().amax((0, 2)) < 1e30
+    assert 0 < keep.sum() < b.T
+    for scale, softcap in ((0.125, 0.0), (10.0, 0.0), (0.125, 20.0)):
+        out, lse = pages_tests.call(oqm, b, b.pages(oqm), scale=scale, softcap=softcap)
+        b.q, q = torch.where(keep[None, :, None], b.q, 0.0), b.q
+        want = b.attention(None, True, scale, softcap, None, dtype != "f32" and not two_parts(b))
+        b.q = q
+        assert ((out.double() - want[0]).abs() / want[2])[:, keep].max() <= 1
+        seen = keep[None] & (want[1] > -math.inf)
+        assert ((lse.double() - want[1]).abs() / want[3])[seen].max() <= 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("cut", ["a few", "up to 64", "halved tiles", "many blocks", "prompts", "one each"])
+def test_tables_of_no_pages(oqm, cut, dtype):  # noqa: F811
+    """No row has a place: nothing but a prior is seen, nothing is written to the pool, and queries are turned all the same."""
+    heads, repeat, rows, new, one_each = CUTS[cut]
+    b = Batch(dtype=dtype, d=64, heads=heads, repeat=repeat, rows=rows, new=new, layers=1, layer=0, one_each=one_each)
+    full = b.pages(oqm)
+    pages = oqm.Pages.create(full.k, full.v, torch.empty((b.B, 0), dtype=torch.int32, device="cuda"), full.rows, full.starts)
+    out, lse = pages_tests.call(oqm, b, pages)
+    assert (out == 0).all() and (lse == -math.inf).all()
+    g = torch.Generator().manual_seed(1)
+    prior = torch.randn(b.q.shape, generator=g).to(paged.DTYPE[dtype]), torch.randn(b.q.shape[:2], generator=g)
+    out, lse = pages_tests.call(oqm, b, pages, prior=prior)
+    assert torch.equal(out, prior[0])
+    assert ((lse - prior[1]).abs() <= 2.0 ** -20 * (1 + prior[1].abs())).all()
+    before = pages.k.clone(), pages.v.clone()
+    x = torch.randn((b.T, heads * (repeat + 2), 64), device="cuda").to(paged.DTYPE[dtype])
+    q_out = torch.zeros((b.T, heads * repeat, 64), dtype=x.dtype, device="cuda")
+    oqm.tom_oqm_append_rows(pages, 0, oqm.Rotary.create(64), torch.zeros(b.T, dtype=torch.int64, device="cuda"), x[:, heads * repeat:heads * (repeat + 1)],
+                            x[:, heads * (repeat + 1):], q=x[:, :heads * repeat], q_out=q_out)
+    assert torch.equal(q_out, x[:, :heads * repeat])
+    kept = torch.full((b.B,), -3, dtype=torch.int32, device="cuda")
+    oqm.tom_oqm_keep_rows(pages, torch.ones((b.B, 2), dtype=torch.int32, device="cuda"), torch.ones(b.B, dtype=torch.int32, device="cuda"), kept)
+    assert kept.tolist() == [r + 1 for r in rows]
+    for t, y in zip((pages.k, pages.v), before):
+        assert torch.equal(t.nan_to_num(5.0), y.nan_to_num(5.0))
